@@ -298,6 +298,84 @@ gx_status gx_params_merge(const gx_layer_cfg* cfg, const gx_params* shard, const
                           void* hip_stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Around the block: what a decoder that reads an encoder's states needs besides it.  Token embedding
+ * (forward and the gradient of the table), norms of queries and keys with the position rotation, and
+ * attention to keys and values of another length.  The calls only enqueue kernels on `hip_stream`: no
+ * side stream, no event, no allocation.  Results are bitwise reproducible (no floating-point atomics).
+ * ------------------------------------------------------------------------------------------ */
+
+/* Embedding lookup with scaling:   y[t, :] = scale * table[ids[t] - first_row, :]
+ * and its gradient               dtable[v, :] = scale * sum over { t : ids[t] = first_row + v } of dy[t, :].
+ * A rank holds rows [first_row, first_row + rows) of the vocabulary.  An id of another shard (or of no
+ * row at all, negative ones included) gives a row of zeros in y, so that the ranks' outputs add up to the
+ * whole lookup, and no gradient.  pad_id (-1: none): tokens with this id are looked up like others but have
+ * no gradient.
+ *   ids [tokens] : int32 or int64 (id_bytes 4 or 8), aligned to itself       table [rows, hidden], y, dy [tokens, hidden] : dtype
+ *   dtable [rows, hidden] fp32, written whole (zeros where no token points) or, with GX_ACCUM_WGRAD, added to.
+ * Products and sums are fp32, y is rounded once.  A row's tokens are added in ascending order within fixed pieces of the
+ * sorted tokens, pieces in order: the same bits for the same sizes and ids.
+ * tokens may be 0.  hidden must be a multiple of 8 (bf16) or 4 (fp32), at most 65536; rows and tokens at most 2^24.
+ * gx_embed_bwd needs gx_embed_workspace_bytes(cfg) bytes of scratch (0 for an invalid cfg), which grow with the
+ * tokens and with hidden.  Errors: GX_ERR_NULL, GX_ERR_SHAPE, GX_ERR_DIVIS, GX_ERR_DTYPE (dtype, id_bytes),
+ * GX_ERR_ALIGN (16 bytes), GX_ERR_FLAGS, GX_ERR_ARCH, GX_ERR_LAUNCH. */
+typedef struct {
+  int32_t tokens, hidden, rows;
+  int32_t dtype;              /* gx_dtype of table, y and dy */
+  int32_t id_bytes;           /* 4 or 8 */
+  int32_t flags;              /* GX_ACCUM_WGRAD or 0 */
+  int64_t first_row, pad_id;
+  float scale;
+} gx_embed_cfg;
+size_t gx_embed_workspace_bytes(const gx_embed_cfg* cfg);
+gx_status gx_embed_fwd(const gx_embed_cfg* cfg, const void* table, const void* ids, void* y, void* hip_stream);
+gx_status gx_embed_bwd(const gx_embed_cfg* cfg, const void* ids, const void* dy, float* dtable, void* workspace,
+                       void* hip_stream);
+
+/* The heads of a tensor: element (sample b, token s, head h, column d) is data[b * batch + s * token + h * head + d],
+ * strides in elements.  Columns are contiguous; data and every stride that is used (its extent is not 1) must keep 16-byte
+ * alignment.  Tensors that are read may repeat (strides of 0 for samples and heads; for tokens too in gx_heads_norm_*);
+ * tensors that are written may not, and must not overlap ones that are read unless stated otherwise. */
+typedef struct {
+  void* data;
+  int64_t batch, token, head;
+} gx_heads;
+
+/* Per-head RMS norm of queries and keys with the position rotation, one pass over each:
+ *     u = x / sqrt(mean(x^2) + eps),   n = gain * u,   y = rotation of n by the token's position
+ * The first rot_dim columns are turned in pairs by the angles of the token's position p: columns (i, i + rot_dim / 2) or,
+ * with GX_ROPE_PAIRS, (2 i, 2 i + 1) become (a cos - b sin, b cos + a sin) with cos[p, i], sin[p, i] from two fp32
+ * tables [max_pos, rot_dim / 2].  rot_dim 0: norm only.
+ *   queries [batch, q_len, q_heads, head_dim], keys [batch, k_len, k_heads, head_dim] (k_len or k_heads 0, or q_len or q_heads
+ *   0: that side is left out and its pointers may be NULL); positions int32 [batch, len] (aligned to
+ *   themselves), NULL for p = s.  A position
+ *   outside [0, max_pos) gives a token of NaN.  gain [head_dim] in dtype, NULL for ones.
+ * gx_heads_norm_fwd writes q_out and k_out; they may be the inputs themselves (same data and strides).
+ * gx_heads_norm_bwd takes the inputs q, k again and the gradients dq_out, dk_out of the outputs; writes dq, dk (may be
+ * dq_out, dk_out themselves) and, where a gain is given, the gain's gradient fp32 [head_dim] (NULL to skip;
+ * GX_ACCUM_WGRAD adds to it).  Statistics, rotation and sums are fp32; every output is rounded once.
+ * head_dim: multiple of 8, at most 256; rot_dim: multiple of 16, at most head_dim.  Workspace (backward only):
+ * gx_heads_norm_workspace_bytes.  Errors as above. */
+enum { GX_ROPE_PAIRS = 1024 };
+typedef struct {
+  int32_t batch, q_len, k_len, q_heads, k_heads, head_dim, rot_dim, max_pos;
+  int32_t dtype;              /* gx_dtype */
+  int32_t flags;              /* GX_ROPE_PAIRS | GX_ACCUM_WGRAD */
+  float eps;
+} gx_heads_norm_cfg;
+typedef struct {
+  gx_heads q, k;
+  const void *q_gain, *k_gain;
+  const int32_t *q_pos, *k_pos;
+  const float *cos_table, *sin_table;
+} gx_heads_norm_in;
+size_t gx_heads_norm_workspace_bytes(const gx_heads_norm_cfg* cfg);
+gx_status gx_heads_norm_fwd(const gx_heads_norm_cfg* cfg, const gx_heads_norm_in* in, const gx_heads* q_out,
+                            const gx_heads* k_out, void* hip_stream);
+gx_status gx_heads_norm_bwd(const gx_heads_norm_cfg* cfg, const gx_heads_norm_in* in, const gx_heads* dq_out,
+                            const gx_heads* dk_out, const gx_heads* dq, const gx_heads* dk, float* dq_gain, float* dk_gain,
+                            void* workspace, void* hip_stream);
+
+/* ------------------------------------------------------------------------------------------
  * Layer-wise strategy plan (host only, no GPU involved).  The paper's strategy selector, in its
  * discovery phase (section 3, "Dynamic Strategy Selector"; section 2, "Layer-Specific Parallelism
  * Optimization"), prunes the candidate strategies with a decision tree and then runs a dynamic

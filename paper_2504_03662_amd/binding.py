@@ -22,6 +22,7 @@ GX_PHASE_ATTN, GX_PHASE_MLP = 1, 2
 GX_ROW_BIAS_ATTN, GX_ROW_BIAS_MLP = 4, 8
 GX_ACCUM_WGRAD, GX_RECOMPUTE, GX_GELU_TANH, GX_WGRAD_BF16, GX_DROPOUT, GX_FWD_SAVED_ONLY = 16, 32, 64, 128, 256, 512
 GX_FWD_PARTS = 4096
+GX_ROPE_PAIRS = 1024
 STATIC_SCRATCH_BYTES = 64 << 20        # GX_STATIC_SCRATCH_BYTES
 
 PARAM_NAMES = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o",
@@ -29,7 +30,8 @@ PARAM_NAMES = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o",
 EXPORTS = ("gx_layer_validate", "gx_layer_saved_bytes", "gx_layer_workspace_bytes", "gx_layer_fwd",
            "gx_layer_bwd", "gx_status_str", "gx_version", "gx_prof_enable", "gx_prof_collect", "gx_set_overlap",
            "gx_adamw_step", "gx_params_slice", "gx_params_merge", "gx_plan_search", "gx_strategy_cost", "gx_layer_bwd_static", "gx_peak_mfma", "gx_peak_copy",
-           "gx_stage_partition", "gx_stage_moves")
+           "gx_stage_partition", "gx_stage_moves", "gx_embed_workspace_bytes", "gx_embed_fwd", "gx_embed_bwd",
+           "gx_heads_norm_workspace_bytes", "gx_heads_norm_fwd", "gx_heads_norm_bwd")
 GX_KC_LN_FWD, GX_KC_LN_BWD, GX_KC_ATTN_FWD, GX_KC_ATTN_BWD, GX_KC_COLSUM, GX_KC_GEMM = 1, 2, 3, 4, 5, 100
 
 
@@ -78,6 +80,25 @@ class StrategyCosts(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("micro_batch_attn", "micro_batch_ffn", "attn_elems", "ffn_elems")] + \
                [(n, ctypes.c_double) for n in ("state_bytes", "tp_comm_ms", "dp_comm_ms", "switch_ms", "flops_attn",
                                                "flops_ffn")]
+
+
+class EmbedCfg(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "hidden", "rows", "dtype", "id_bytes", "flags")] + \
+               [("first_row", ctypes.c_int64), ("pad_id", ctypes.c_int64), ("scale", ctypes.c_float)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("batch", "token", "head")]
+
+
+class HeadsNormCfg(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "q_len", "k_len", "q_heads", "k_heads", "head_dim", "rot_dim",
+                                               "max_pos", "dtype", "flags")] + [("eps", ctypes.c_float)]
+
+
+class HeadsNormIn(ctypes.Structure):
+    _fields_ = [("q", Heads), ("k", Heads)] + [(n, ctypes.c_void_p) for n in ("q_gain", "k_gain", "q_pos", "k_pos",
+                                                                              "cos_table", "sin_table")]
 
 
 class GxError(RuntimeError):
@@ -144,6 +165,19 @@ def lib():
         L.gx_peak_copy.restype = ctypes.c_int
         L.gx_strategy_cost.argtypes = [ctypes.POINTER(StrategyQuery), ctypes.POINTER(StrategyCosts)]
         L.gx_strategy_cost.restype = ctypes.c_int
+        L.gx_embed_workspace_bytes.argtypes = [ctypes.POINTER(EmbedCfg)]
+        L.gx_embed_workspace_bytes.restype = ctypes.c_size_t
+        L.gx_embed_fwd.argtypes = [ctypes.POINTER(EmbedCfg), P, P, P, P]
+        L.gx_embed_fwd.restype = ctypes.c_int
+        L.gx_embed_bwd.argtypes = [ctypes.POINTER(EmbedCfg), P, P, P, P, P]
+        L.gx_embed_bwd.restype = ctypes.c_int
+        H = ctypes.POINTER(Heads)
+        L.gx_heads_norm_workspace_bytes.argtypes = [ctypes.POINTER(HeadsNormCfg)]
+        L.gx_heads_norm_workspace_bytes.restype = ctypes.c_size_t
+        L.gx_heads_norm_fwd.argtypes = [ctypes.POINTER(HeadsNormCfg), ctypes.POINTER(HeadsNormIn), H, H, P]
+        L.gx_heads_norm_fwd.restype = ctypes.c_int
+        L.gx_heads_norm_bwd.argtypes = [ctypes.POINTER(HeadsNormCfg), ctypes.POINTER(HeadsNormIn), H, H, H, H, P, P, P, P]
+        L.gx_heads_norm_bwd.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -364,3 +398,60 @@ def peak_copy(src, dst, nbytes, launches=20, stream=0):
         raise GxError(st, "gx_peak_copy")
     return out.value
 
+
+
+def heads(t):
+    """gx_heads of a tensor [batch, tokens, heads, columns] with contiguous columns (None: nothing)."""
+    if t is None:
+        return Heads(None, 0, 0, 0)
+    st = t.stride()
+    if len(st) != 4 or (st[3] != 1 and t.shape[3] > 1):
+        raise ValueError("a tensor [batch, tokens, heads, columns] with contiguous columns")
+    return Heads(t.data_ptr(), st[0], st[1], st[2])
+
+
+def embed_workspace_bytes(cfg):
+    return int(lib().gx_embed_workspace_bytes(ctypes.byref(cfg)))
+
+
+def embed_fwd(cfg, table, ids, y, stream=0, check=True):
+    st = lib().gx_embed_fwd(ctypes.byref(cfg), _ptr(table), _ptr(ids), _ptr(y), ctypes.c_void_p(stream))
+    if check and st != GX_OK:
+        raise GxError(st, "gx_embed_fwd")
+    return int(st)
+
+
+def embed_bwd(cfg, ids, dy, dtable, workspace, stream=0, check=True):
+    st = lib().gx_embed_bwd(ctypes.byref(cfg), _ptr(ids), _ptr(dy), _ptr(dtable), _ptr(workspace), ctypes.c_void_p(stream))
+    if check and st != GX_OK:
+        raise GxError(st, "gx_embed_bwd")
+    return int(st)
+
+
+def _addr(t):
+    return None if t is None else t if isinstance(t, int) else t.data_ptr()
+
+
+def heads_norm_in(q, k, q_gain, k_gain, q_pos, k_pos, cos_table, sin_table):
+    """q, k: tensors as `heads` takes them, or None."""
+    return HeadsNormIn(heads(q), heads(k), _addr(q_gain), _addr(k_gain), _addr(q_pos), _addr(k_pos), _addr(cos_table),
+                       _addr(sin_table))
+
+
+def heads_norm_workspace_bytes(cfg):
+    return int(lib().gx_heads_norm_workspace_bytes(ctypes.byref(cfg)))
+
+
+def heads_norm_fwd(cfg, inputs, q_out, k_out, stream=0, check=True):
+    st = lib().gx_heads_norm_fwd(ctypes.byref(cfg), ctypes.byref(inputs), heads(q_out), heads(k_out), ctypes.c_void_p(stream))
+    if check and st != GX_OK:
+        raise GxError(st, "gx_heads_norm_fwd")
+    return int(st)
+
+
+def heads_norm_bwd(cfg, inputs, dq_out, dk_out, dq, dk, dq_gain, dk_gain, workspace, stream=0, check=True):
+    st = lib().gx_heads_norm_bwd(ctypes.byref(cfg), ctypes.byref(inputs), heads(dq_out), heads(dk_out), heads(dq), heads(dk),
+                                 _ptr(dq_gain), _ptr(dk_gain), _ptr(workspace), ctypes.c_void_p(stream))
+    if check and st != GX_OK:
+        raise GxError(st, "gx_heads_norm_bwd")
+    return int(st)

@@ -1,0 +1,164 @@
+"""The operators around a block of a decoder that reads an encoder's states, on torch tensors: the token embedding and its
+gradient, norms of queries and keys with the position rotation, and cross attention.  Like `runtime`, this is plumbing: torch
+supplies device memory and the stream, shapes and types are checked here, and the library does all the compute.
+
+Every call works on the current stream and returns without waiting.  An object holds sizes and scratch memory only, one piece of
+scratch per stream, so that calls on different streams do not meet; tensors of another stream are the caller's to order, as
+everywhere in torch.  Outputs are new tensors unless `out`s are given."""
+from __future__ import annotations
+
+import torch
+
+from . import binding as gx
+
+_TYPES = {"bf16": (gx.GX_BF16, torch.bfloat16), "f32": (gx.GX_F32, torch.float32)}
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+class _Operator:
+    """Type, device and scratch of an operator."""
+
+    def __init__(self, dtype, device):
+        gx.lib()                                   # fail loudly if the library is not built
+        self.gtype, self.tdtype = _TYPES[dtype]
+        self.device = torch.device(device)
+        self._scratch = {}
+
+    def _workspace(self, nbytes, stream):
+        w = self._scratch.get(stream)
+        if w is None or w.numel() < nbytes:
+            w = self._scratch[stream] = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        return w
+
+    def _check(self, name, t, shape=None, dtype=None, contiguous=False):
+        _need(t.dtype == (dtype or self.tdtype), f"{name}: {t.dtype}, not {dtype or self.tdtype}")
+        _need(t.device == self.device, f"{name}: on {t.device}, not {self.device}")
+        _need(shape is None or tuple(t.shape) == tuple(shape), f"{name}: shape {tuple(t.shape)}, not {tuple(shape or ())}")
+        _need(not contiguous or t.is_contiguous(), f"{name}: not contiguous")
+
+    @staticmethod
+    def _stream():
+        return torch.cuda.current_stream().cuda_stream
+
+
+class DeviceEmbedding(_Operator):
+    """Rows [first_row, first_row + rows) of a vocabulary: y = scale * table[ids - first_row], zeros for ids of other shards, and
+    the table's gradient.  Tokens with `pad_id` have no gradient."""
+
+    def __init__(self, rows, hidden, dtype="bf16", scale=1.0, first_row=0, pad_id=-1, device="cuda:0"):
+        super().__init__(dtype, device)
+        self.rows, self.hidden, self.scale, self.first_row, self.pad_id = rows, hidden, scale, first_row, pad_id
+
+    def _cfg(self, ids, flags=0):
+        _need(ids.dtype in (torch.int32, torch.int64), f"ids: {ids.dtype}, not int32 or int64")
+        self._check("ids", ids, dtype=ids.dtype, contiguous=True)
+        return gx.EmbedCfg(ids.numel(), self.hidden, self.rows, self.gtype, ids.element_size(), flags, self.first_row, self.pad_id,
+                           self.scale)
+
+    def forward(self, table, ids, out=None):
+        """table [rows, hidden], ids of any shape -> [*ids.shape, hidden]"""
+        cfg, shape = self._cfg(ids), (*ids.shape, self.hidden)
+        self._check("table", table, (self.rows, self.hidden), contiguous=True)
+        if out is None:
+            out = torch.empty(shape, dtype=self.tdtype, device=self.device)
+        else:
+            self._check("out", out, shape, contiguous=True)
+        gx.embed_fwd(cfg, table, ids, out, self._stream())
+        return out
+
+    def backward(self, ids, dy, out=None, accumulate=False):
+        """dy [*ids.shape, hidden] -> fp32 gradient of the table, written to `out` whole or, with accumulate, added to it"""
+        cfg = self._cfg(ids, gx.GX_ACCUM_WGRAD if accumulate else 0)
+        self._check("dy", dy, (*ids.shape, self.hidden), contiguous=True)
+        _need(out is not None or not accumulate, "accumulate: into which gradient?")
+        if out is None:
+            out = torch.empty((self.rows, self.hidden), dtype=torch.float32, device=self.device)
+        else:
+            self._check("out", out, (self.rows, self.hidden), torch.float32, contiguous=True)
+        stream = self._stream()
+        gx.embed_bwd(cfg, ids, dy, out, self._workspace(gx.embed_workspace_bytes(cfg), stream), stream)
+        return out
+
+
+class DeviceHeadNorm(_Operator):
+    """RMS norm of every query and key head with a gain per column, then the rotation of the first `rot_dim` columns by the
+    token's position; columns (i, i + rot_dim / 2) turn together, or with `pairs` (2 i, 2 i + 1)."""
+
+    def __init__(self, head_dim, rot_dim=0, dtype="bf16", eps=1e-6, pairs=False, device="cuda:0"):
+        super().__init__(dtype, device)
+        self.head_dim, self.rot_dim, self.eps, self.pairs = head_dim, rot_dim, eps, pairs
+
+    def _args(self, q, k, gain_q, gain_k, cos, sin, q_pos, k_pos, flags):
+        _need(q is not None or k is not None, "queries or keys")
+        sizes = []
+        for name, x, gain, pos in (("q", q, gain_q, q_pos), ("k", k, gain_k, k_pos)):
+            if x is None:
+                sizes.append((None, 0, 0))
+                continue
+            _need(x.dim() == 4 and x.shape[3] == self.head_dim, f"{name}: not [batch, tokens, heads, {self.head_dim}]")
+            self._check(name, x)
+            if gain is not None:
+                self._check(name + " gain", gain, (self.head_dim,), contiguous=True)
+            if pos is not None:
+                self._check(name + " positions", pos, x.shape[:2], torch.int32, contiguous=True)
+            sizes.append(tuple(x.shape[:3]))
+        (bq, sq, hq), (bk, sk, hk) = sizes
+        _need(bq is None or bk is None or bq == bk, "queries and keys of as many samples")
+        max_pos = 0
+        if self.rot_dim:
+            _need(cos is not None and sin is not None, "tables of cosines and sines")
+            max_pos = cos.shape[0]
+            for name, t in (("cos", cos), ("sin", sin)):
+                self._check(name, t, (max_pos, self.rot_dim // 2), torch.float32, contiguous=True)
+        cfg = gx.HeadsNormCfg(bq or bk, sq, sk, hq, hk, self.head_dim, self.rot_dim, max_pos, self.gtype,
+                              flags | (gx.GX_ROPE_PAIRS if self.pairs else 0), self.eps)
+        return cfg, gx.heads_norm_in(q, k, gain_q, gain_k, q_pos, k_pos, cos if self.rot_dim else None,
+                                     sin if self.rot_dim else None)
+
+    def _outs(self, like, given, names):
+        outs = []
+        for x, o, name in zip(like, given, names):
+            if x is not None and o is None:
+                o = torch.empty(x.shape, dtype=self.tdtype, device=self.device)
+            elif x is not None:
+                self._check(name, o, x.shape)
+            outs.append(o if x is not None else None)
+        return outs
+
+    def forward(self, q, k=None, gain_q=None, gain_k=None, cos=None, sin=None, q_pos=None, k_pos=None, q_out=None, k_out=None):
+        """q [batch, tokens, heads, head_dim], k the same with its own tokens and heads, or either None; positions int32 [batch,
+        tokens] (None: 0, 1, ...); cos, sin fp32 [positions, rot_dim / 2].  Returns (q, k), normed and turned; q_out, k_out
+        may be q and k themselves."""
+        cfg, inputs = self._args(q, k, gain_q, gain_k, cos, sin, q_pos, k_pos, 0)
+        q_out, k_out = self._outs((q, k), (q_out, k_out), ("q_out", "k_out"))
+        gx.heads_norm_fwd(cfg, inputs, q_out, k_out, self._stream())
+        return q_out, k_out
+
+    def backward(self, q, k, dq_out, dk_out, gain_q=None, gain_k=None, cos=None, sin=None, q_pos=None, k_pos=None, dq=None, dk=None,
+                 dgain_q=None, dgain_k=None, accumulate=False):
+        """The forward pass's inputs and the gradients of its outputs -> (dq, dk, dgain_q, dgain_k); the gains' are fp32, None
+        without a gain, and added to with accumulate."""
+        cfg, inputs = self._args(q, k, gain_q, gain_k, cos, sin, q_pos, k_pos, gx.GX_ACCUM_WGRAD if accumulate else 0)
+        for name, x, d in (("dq_out", q, dq_out), ("dk_out", k, dk_out)):
+            if x is not None:
+                self._check(name, d, x.shape)
+        dq, dk = self._outs((q, k), (dq, dk), ("dq", "dk"))
+        dg = []
+        for x, gain, d, name in ((q, gain_q, dgain_q, "dgain_q"), (k, gain_k, dgain_k, "dgain_k")):
+            if x is None or gain is None:
+                d = None
+            elif d is None:
+                _need(not accumulate, f"accumulate: into which {name}?")
+                d = torch.empty(self.head_dim, dtype=torch.float32, device=self.device)
+            else:
+                self._check(name, d, (self.head_dim,), torch.float32, contiguous=True)
+            dg.append(d)
+        stream = self._stream()
+        ws = self._workspace(gx.heads_norm_workspace_bytes(cfg), stream)
+        gx.heads_norm_bwd(cfg, inputs, dq_out if q is not None else None, dk_out if k is not None else None, dq, dk, dg[0], dg[1],
+                          ws, stream)
+        return dq, dk, dg[0], dg[1]
