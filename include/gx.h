@@ -375,6 +375,38 @@ gx_status gx_heads_norm_bwd(const gx_heads_norm_cfg* cfg, const gx_heads_norm_in
                             const gx_heads* dk_out, const gx_heads* dq, const gx_heads* dk, float* dq_gain, float* dk_gain,
                             void* workspace, void* hip_stream);
 
+/* Cross attention: queries of one sequence, keys and values of another (an encoder's states), all keys visible that count.
+ *     O = softmax(scale Q K^T over the keys that count) V,   lse = log sum exp of the scaled scores that count
+ *   q, o [batch, q_len, q_heads, head_dim]; k, v [batch, k_len, k_heads, head_dim]; query head h reads key head
+ *   h / (q_heads / k_heads); lse fp32 [batch, q_heads, q_len], NULL to skip (the backward pass needs it).
+ *   key_lens int32 [batch] (NULL: all k_len): keys at and beyond a sample's length do not count (lengths are cut to 0 .. k_len);
+ *   key_mask bytes [batch, k_len] (NULL: all): keys whose byte is 0 do not count.  With both, a key counts if both say so.
+ * What does not count is never read into a sum: infinities and NaN there change nothing.  A query for which no key
+ * counts has O = 0, lse = -inf and no gradient, and so has one whose scores that count are all -inf; keys that do not
+ * count have dK = dV = 0.  gx_cross_bwd takes the forward pass's inputs, o and lse and writes dQ, dK, dV (all required).
+ * Element types: bf16 with fp32 scores, softmax and sums (probabilities and their gradients are rounded to bf16 as operands of
+ * the second products; head_dim 64 or 128) or fp32 throughout (head_dim a multiple of 4 up to 128).  scale > 0.
+ * k and v keep at least head_dim elements between tokens.  q_len or k_len may be 0.
+ * Limits: batch * q_heads and q_len * q_heads below 2^30, k_len at most 2^22, token strides up to 2^22 elements, head strides such that a
+ * group's heads span less than 2^28 elements.  Workspace: gx_cross_workspace_bytes (0 may be right; NULL is then allowed).
+ * Errors as above; key_lens are aligned to themselves. */
+typedef struct {
+  int32_t batch, q_len, k_len, q_heads, k_heads, head_dim;
+  int32_t dtype;              /* gx_dtype */
+  int32_t flags;              /* 0 */
+  float scale;
+} gx_cross_cfg;
+typedef struct {
+  gx_heads q, k, v;
+  const int32_t* key_lens;
+  const uint8_t* key_mask;
+} gx_cross_in;
+size_t gx_cross_workspace_bytes(const gx_cross_cfg* cfg, int is_backward);
+gx_status gx_cross_fwd(const gx_cross_cfg* cfg, const gx_cross_in* in, const gx_heads* o, float* lse, void* workspace,
+                       void* hip_stream);
+gx_status gx_cross_bwd(const gx_cross_cfg* cfg, const gx_cross_in* in, const gx_heads* o, const float* lse, const gx_heads* d_o,
+                       const gx_heads* dq, const gx_heads* dk, const gx_heads* dv, void* workspace, void* hip_stream);
+
 /* ------------------------------------------------------------------------------------------
  * Layer-wise strategy plan (host only, no GPU involved).  The paper's strategy selector, in its
  * discovery phase (section 3, "Dynamic Strategy Selector"; section 2, "Layer-Specific Parallelism

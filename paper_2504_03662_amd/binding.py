@@ -31,7 +31,8 @@ EXPORTS = ("gx_layer_validate", "gx_layer_saved_bytes", "gx_layer_workspace_byte
            "gx_layer_bwd", "gx_status_str", "gx_version", "gx_prof_enable", "gx_prof_collect", "gx_set_overlap",
            "gx_adamw_step", "gx_params_slice", "gx_params_merge", "gx_plan_search", "gx_strategy_cost", "gx_layer_bwd_static", "gx_peak_mfma", "gx_peak_copy",
            "gx_stage_partition", "gx_stage_moves", "gx_embed_workspace_bytes", "gx_embed_fwd", "gx_embed_bwd",
-           "gx_heads_norm_workspace_bytes", "gx_heads_norm_fwd", "gx_heads_norm_bwd")
+           "gx_heads_norm_workspace_bytes", "gx_heads_norm_fwd", "gx_heads_norm_bwd",
+           "gx_cross_workspace_bytes", "gx_cross_fwd", "gx_cross_bwd")
 GX_KC_LN_FWD, GX_KC_LN_BWD, GX_KC_ATTN_FWD, GX_KC_ATTN_BWD, GX_KC_COLSUM, GX_KC_GEMM = 1, 2, 3, 4, 5, 100
 
 
@@ -99,6 +100,15 @@ class HeadsNormCfg(ctypes.Structure):
 class HeadsNormIn(ctypes.Structure):
     _fields_ = [("q", Heads), ("k", Heads)] + [(n, ctypes.c_void_p) for n in ("q_gain", "k_gain", "q_pos", "k_pos",
                                                                               "cos_table", "sin_table")]
+
+
+class CrossCfg(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "q_len", "k_len", "q_heads", "k_heads", "head_dim", "dtype", "flags")] + \
+               [("scale", ctypes.c_float)]
+
+
+class CrossIn(ctypes.Structure):
+    _fields_ = [("q", Heads), ("k", Heads), ("v", Heads), ("key_lens", ctypes.c_void_p), ("key_mask", ctypes.c_void_p)]
 
 
 class GxError(RuntimeError):
@@ -178,6 +188,12 @@ def lib():
         L.gx_heads_norm_fwd.restype = ctypes.c_int
         L.gx_heads_norm_bwd.argtypes = [ctypes.POINTER(HeadsNormCfg), ctypes.POINTER(HeadsNormIn), H, H, H, H, P, P, P, P]
         L.gx_heads_norm_bwd.restype = ctypes.c_int
+        L.gx_cross_workspace_bytes.argtypes = [ctypes.POINTER(CrossCfg), ctypes.c_int]
+        L.gx_cross_workspace_bytes.restype = ctypes.c_size_t
+        L.gx_cross_fwd.argtypes = [ctypes.POINTER(CrossCfg), ctypes.POINTER(CrossIn), H, P, P, P]
+        L.gx_cross_fwd.restype = ctypes.c_int
+        L.gx_cross_bwd.argtypes = [ctypes.POINTER(CrossCfg), ctypes.POINTER(CrossIn), H, P, H, H, H, H, P, P]
+        L.gx_cross_bwd.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -454,4 +470,28 @@ def heads_norm_bwd(cfg, inputs, dq_out, dk_out, dq, dk, dq_gain, dk_gain, worksp
                                  _ptr(dq_gain), _ptr(dk_gain), _ptr(workspace), ctypes.c_void_p(stream))
     if check and st != GX_OK:
         raise GxError(st, "gx_heads_norm_bwd")
+    return int(st)
+
+
+def cross_in(q, k, v, key_lens=None, key_mask=None):
+    """q, k, v: tensors as `heads` takes them."""
+    return CrossIn(heads(q), heads(k), heads(v), _addr(key_lens), _addr(key_mask))
+
+
+def cross_workspace_bytes(cfg, is_backward):
+    return int(lib().gx_cross_workspace_bytes(ctypes.byref(cfg), int(bool(is_backward))))
+
+
+def cross_fwd(cfg, inputs, o, lse, workspace, stream=0, check=True):
+    st = lib().gx_cross_fwd(ctypes.byref(cfg), ctypes.byref(inputs), heads(o), _ptr(lse), _ptr(workspace), ctypes.c_void_p(stream))
+    if check and st != GX_OK:
+        raise GxError(st, "gx_cross_fwd")
+    return int(st)
+
+
+def cross_bwd(cfg, inputs, o, lse, d_o, dq, dk, dv, workspace, stream=0, check=True):
+    st = lib().gx_cross_bwd(ctypes.byref(cfg), ctypes.byref(inputs), heads(o), _ptr(lse), heads(d_o), heads(dq), heads(dk),
+                            heads(dv), _ptr(workspace), ctypes.c_void_p(stream))
+    if check and st != GX_OK:
+        raise GxError(st, "gx_cross_bwd")
     return int(st)

@@ -1,0 +1,394 @@
+// fp32 cross attention on v_mfma_f32_32x32x2_f32: every product and sum is a full fp32 one, in a fixed order.
+//
+// As in the causal fp32 kernels a workgroup owns 32 rows (forward, dQ) or 32 keys (dK / dV) of a (sample, key head) pair and
+// its 4 wavefronts take every 4th 32-wide tile of the other side; scores are taken transposed to the owner, so that an accumulator
+// register is, as it stands, an operand of the next product (register v of a lane in half g holds tile row 8 (v / 4) + 4 g + v % 4)
+// and operands come straight from global memory.  The parts' results are merged through LDS in wavefront order.  Head dimensions
+// up to 128 (multiples of 4) are padded with zeros to 32, 64 or 128.
+// Keys that do not count have bits of a 32-bit word per tile: their scores are left out by selection, and what is read of them
+// is replaced by zeros before it becomes an operand.
+#include "cross.h"
+
+namespace gx {
+namespace {
+
+constexpr int PARTS = 4;          // wavefronts of a workgroup
+constexpr unsigned ALL = 0xFFFFFFFFu;
+
+GX_DEVINL f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int v = 0; v < 16; v++) z[v] = 0.f;
+  return z;
+}
+GX_DEVINL int acc_row(int v, int g) { return 8 * (v >> 2) + 4 * g + (v & 3); }
+GX_DEVINL bool bit_of(unsigned bits, int v, int g) { return (bits >> acc_row(v, g)) & 1u; }
+GX_DEVINL f32x16 mfma(float a, float b, const f32x16& c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+
+// One lane's share of 32 rows by DHP columns whose reduction index is the column: chunk c holds columns 8 c + 4 g .. + 3
+template <int DHP>
+GX_DEVINL void load_rows(const float* row, int dh, int g, f32x4 (&out)[DHP / 8]) {
+#pragma unroll
+  for (int c = 0; c < DHP / 8; c++) {
+    const int d = 8 * c + 4 * g;
+    out[c] = d < dh ? *reinterpret_cast<const f32x4*>(row + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+}
+// 32 x 32 scores: sum over columns of a[row] * b[col]
+template <int DHP>
+GX_DEVINL f32x16 row_product(const f32x4 (&a)[DHP / 8], const f32x4 (&b)[DHP / 8]) {
+  f32x16 s = zero16();
+#pragma unroll
+  for (int c = 0; c < DHP / 8; c++)
+#pragma unroll
+    for (int e = 0; e < 4; e++) s = mfma(a[c][e], b[c][e], s);
+  return s;
+}
+// acc[dt][d][col] += sum over the tile's 32 rows of x[row][d] * w[row][col]; row_at(v) gives the address of the row of register v,
+// which counts if its bit does (else zero stands for it)
+template <int DHP, class RowAt>
+GX_DEVINL void col_product(f32x16 (&acc)[DHP / 32], const f32x16& w, RowAt row_at, unsigned bits, int dh, int g, int l32) {
+  constexpr int CH = DHP >= 64 ? 2 : 1;                      // column blocks in registers at a time
+  const float* rows[16];
+#pragma unroll
+  for (int v = 0; v < 16; v++) rows[v] = row_at(v);
+#pragma unroll
+  for (int d0 = 0; d0 < DHP / 32; d0 += CH) {
+    float x[CH][16];
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+      const int dd = 32 * (d0 + c) + l32, d = dd < dh ? dd : dh - 1;    // columns beyond dh are never stored
+#pragma unroll
+      for (int v = 0; v < 16; v++) x[c][v] = rows[v][d];
+    }
+    if (bits != ALL) {
+#pragma unroll
+      for (int v = 0; v < 16; v++)
+        if (!bit_of(bits, v, g)) {
+#pragma unroll
+          for (int c = 0; c < CH; c++) x[c][v] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < 16; v++)
+#pragma unroll
+      for (int c = 0; c < CH; c++) acc[d0 + c] = mfma(x[c][v], w[v], acc[d0 + c]);
+  }
+}
+// Adds the parts' accumulators in the order of the wavefronts; the sum is complete in wavefront 0.
+template <int DT>
+GX_DEVINL void merge_parts(f32x16 (&acc)[DT], float* park, int part, int lane) {
+  __syncthreads();
+  if (part > 0)
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) park[((part - 1) * DT * 16 + 16 * dt + v) * 64 + lane] = acc[dt][v];
+  __syncthreads();
+  if (part == 0)
+    for (int p = 0; p < PARTS - 1; p++)
+#pragma unroll
+      for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) acc[dt][v] += park[(p * DT * 16 + 16 * dt + v) * 64 + lane];
+}
+// one column (= one row of the tensor) of a transposed result: dst[d] = acc * scale
+template <int DHP>
+GX_DEVINL void store_column(const f32x16 (&acc)[DHP / 32], float* dst, float scale, int dh, int g) {
+#pragma unroll
+  for (int dt = 0; dt < DHP / 32; dt++)
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+      const int d = 32 * dt + 8 * q + 4 * g;
+      if (d < dh)
+        *reinterpret_cast<f32x4*>(dst + d) = f32x4{acc[dt][4 * q] * scale, acc[dt][4 * q + 1] * scale, acc[dt][4 * q + 2] * scale,
+                                                   acc[dt][4 * q + 3] * scale};
+    }
+}
+
+// the pair, tile and split of a workgroup, and the keys that count
+struct Where {
+  int b, kh, pair, tile, split, len;
+  GX_DEVINL Where(const CrossArgs& a, int tiles) {
+    const int npair = a.B * a.hk, rest = blockIdx.x / npair;
+    pair = blockIdx.x % npair;
+    tile = rest % tiles;
+    split = rest / tiles;
+    kh = pair % a.hk;
+    b = pair / a.hk;
+    len = keys_of(a, b);
+  }
+};
+// bits of the 32 keys from key j0 on; the same in every lane
+GX_DEVINL unsigned key_bits(const CrossArgs& a, int b, int j0, int len, int l32) {
+  const int j = j0 + l32;
+  bool on = j < len;
+  if (a.key_mask && on) on = a.key_mask[(long)b * a.Sk + j] != 0;
+  return (unsigned)__builtin_amdgcn_ballot_w64(on);
+}
+GX_DEVINL const float* f32_of(const void* p) { return static_cast<const float*>(p); }
+
+// what exponents are taken relative to while a row has seen no key, or only scores of -inf
+GX_DEVINL float finite_ref(float m) { return m == -INFINITY ? 0.f : m; }
+
+template <int DHP>
+__global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_fwd_f32_kernel(CrossArgs a) {
+  constexpr int VALS = DHP / 2 + 2;
+  __shared__ float lds[(PARTS - 1) * VALS * 64];
+  const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 5, l32 = lane & 31;
+  const Where w(a, (a.rows + 31) / 32);
+  const int r = 32 * w.tile + l32, rc = r < a.rows ? r : a.rows - 1;
+  f32x4 qf[DHP / 8];
+  load_rows<DHP>(f32_of(a.q) + pair_offset(a.sq, w.b, w.kh * a.group) + row_offset(a.sq, a.group, rc), a.dh, g, qf);
+  f32x16 o[DHP / 32];
+#pragma unroll
+  for (int dt = 0; dt < DHP / 32; dt++) o[dt] = zero16();
+  float m = -INFINITY, l = 0.f;
+  const float* const kb = f32_of(a.k) + pair_offset(a.sk, w.b, w.kh);
+  const float* const vb = f32_of(a.v) + pair_offset(a.sv, w.b, w.kh);
+  const int nt = (w.len + 31) / 32;
+  const int t0 = (int)((long)nt * w.split / a.splits), t1 = (int)((long)nt * (w.split + 1) / a.splits);
+  for (int t = t0 + part; t < t1; t += PARTS) {
+    const int j0 = 32 * t;
+    const unsigned bits = key_bits(a, w.b, j0, w.len, l32);
+    f32x4 kf[DHP / 8];
+    load_rows<DHP>(kb + (long)min(j0 + l32, w.len - 1) * a.sk.t, a.dh, g, kf);
+    f32x16 s = row_product<DHP>(kf, qf);                         // S^T[j][i]
+    float mx = -INFINITY;
+    const float mold = m;
+#pragma unroll
+    for (int v = 0; v < 16; v++) {
+      s[v] = bit_of(bits, v, g) ? s[v] * a.scale : -INFINITY;
+      mx = fmaxf(mx, s[v]);
+    }
+    m = fmaxf(m, max_across_halves(mx));
+    const float ref = finite_ref(m), alpha = expf(mold - ref);
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; v++) {
+      s[v] = expf(s[v] - ref);
+      sum += s[v];
+    }
+    l = l * alpha + sum;
+#pragma unroll
+    for (int dt = 0; dt < DHP / 32; dt++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) o[dt][v] *= alpha;
+    col_product<DHP>(o, s, [&](int v) { return vb + (long)min(j0 + acc_row(v, g), w.len - 1) * a.sv.t; }, bits, a.dh, g, l32);
+  }
+  // merge the parts' (m, l, O); a part without a key has m = -inf, l = 0, O = 0 and adds nothing
+  if (part > 0) {
+    float* p = lds + (part - 1) * VALS * 64 + lane;
+    p[0] = m;
+    p[64] = l;
+#pragma unroll
+    for (int dt = 0; dt < DHP / 32; dt++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) p[(2 + 16 * dt + v) * 64] = o[dt][v];
+  }
+  __syncthreads();
+  if (part > 0) return;
+  for (int pp = 0; pp < PARTS - 1; pp++) {
+    const float* p = lds + pp * VALS * 64 + lane;
+    const float mm = fmaxf(m, p[0]), ref = finite_ref(mm), a0 = expf(m - ref), a1 = expf(p[0] - ref);
+    l = l * a0 + p[64] * a1;
+    m = mm;
+#pragma unroll
+    for (int dt = 0; dt < DHP / 32; dt++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) o[dt][v] = o[dt][v] * a0 + p[(2 + 16 * dt + v) * 64] * a1;
+  }
+  l += __shfl_xor(l, 32, 64);
+  if (r >= a.rows) return;
+  if (a.splits > 1) {
+    const long npair = (long)a.B * a.hk, at = (w.split * npair + w.pair) * a.rows + r;
+    store_column<DHP>(o, a.part + at * a.dh, 1.0f, a.dh, g);
+    if (g == 0) *reinterpret_cast<f32x2*>(a.part + a.splits * npair * a.rows * a.dh + at * 2) = f32x2{m, l};
+    return;
+  }
+  store_column<DHP>(o, static_cast<float*>(a.out) + pair_offset(a.so, w.b, w.kh * a.group) + row_offset(a.so, a.group, r),
+                    l == 0.f ? 0.f : 1.0f / l, a.dh, g);
+  if (a.lse && g == 0) {
+    const int i = r / a.group, h = w.kh * a.group + (r - i * a.group);
+    a.lse[((long)w.b * a.hk * a.group + h) * a.Sq + i] = l == 0.f ? -INFINITY : m + logf(l);
+  }
+}
+
+// D = rowsum(dO * O), dS = P (dP - D), dQ = scale dS K; leaves D and lse (+inf for a row without a key) in row order
+template <int DHP>
+__global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dq_f32_kernel(CrossArgs a) {
+  __shared__ float lds[(PARTS - 1) * (DHP / 2) * 64];
+  const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 5, l32 = lane & 31;
+  const Where w(a, (a.rows + 31) / 32);
+  const int r = 32 * w.tile + l32, rc = r < a.rows ? r : a.rows - 1, head0 = w.kh * a.group;
+  f32x4 qf[DHP / 8], dof[DHP / 8];
+  load_rows<DHP>(f32_of(a.q) + pair_offset(a.sq, w.b, head0) + row_offset(a.sq, a.group, rc), a.dh, g, qf);
+  load_rows<DHP>(f32_of(a.d_o) + pair_offset(a.sdo, w.b, head0) + row_offset(a.sdo, a.group, rc), a.dh, g, dof);
+  float dd = 0.f;
+  {
+    f32x4 of[DHP / 8];
+    load_rows<DHP>(f32_of(a.o) + pair_offset(a.so, w.b, head0) + row_offset(a.so, a.group, rc), a.dh, g, of);
+#pragma unroll
+    for (int c = 0; c < DHP / 8; c++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) dd = fmaf(dof[c][e], of[c][e], dd);
+  }
+  dd += __shfl_xor(dd, 32, 64);
+  const int i = rc / a.group, h = head0 + (rc - i * a.group);
+  float lse = a.lse[((long)w.b * a.hk * a.group + h) * a.Sq + i];
+  if (lse == -INFINITY) lse = INFINITY;
+  if (w.split == 0 && part == 0 && g == 0 && r < a.rows) {
+    a.drow[(long)w.pair * a.rows + r] = dd;
+    a.lrow[(long)w.pair * a.rows + r] = lse;
+  }
+  f32x16 dq[DHP / 32];
+#pragma unroll
+  for (int dt = 0; dt < DHP / 32; dt++) dq[dt] = zero16();
+  const float* const kb = f32_of(a.k) + pair_offset(a.sk, w.b, w.kh);
+  const float* const vb = f32_of(a.v) + pair_offset(a.sv, w.b, w.kh);
+  const int nt = (w.len + 31) / 32;
+  const int t0 = (int)((long)nt * w.split / a.splits), t1 = (int)((long)nt * (w.split + 1) / a.splits);
+  for (int t = t0 + part; t < t1; t += PARTS) {
+    const int j0 = 32 * t;
+    const unsigned bits = key_bits(a, w.b, j0, w.len, l32);
+    const long jr = min(j0 + l32, w.len - 1);
+    f32x16 s, dp;
+    {
+      f32x4 kf[DHP / 8];
+      load_rows<DHP>(kb + jr * a.sk.t, a.dh, g, kf);
+      s = row_product<DHP>(kf, qf);                              // S^T[j][i]
+      if (DHP > 64) __builtin_amdgcn_sched_barrier(0);           // one operand in registers at a time
+      load_rows<DHP>(vb + jr * a.sv.t, a.dh, g, kf);
+      dp = row_product<DHP>(kf, dof);                            // dP^T[j][i]
+    }
+#pragma unroll
+    for (int v = 0; v < 16; v++) s[v] = bit_of(bits, v, g) ? expf(s[v] * a.scale - lse) * (dp[v] - dd) : 0.f;
+    if (DHP > 64) __builtin_amdgcn_sched_barrier(0);
+    col_product<DHP>(dq, s, [&](int v) { return kb + (long)min(j0 + acc_row(v, g), w.len - 1) * a.sk.t; }, bits, a.dh, g, l32);
+  }
+  merge_parts(dq, lds, part, lane);
+  if (part != 0 || r >= a.rows) return;
+  if (a.splits > 1) store_column<DHP>(dq, a.part + (((long)w.split * a.B * a.hk + w.pair) * a.rows + r) * a.dh, 1.0f, a.dh, g);
+  else store_column<DHP>(dq, static_cast<float*>(a.dq) + pair_offset(a.sdq, w.b, head0) + row_offset(a.sdq, a.group, r), a.scale,
+                         a.dh, g);
+}
+
+// dV_j = sum_i P_ij dO_i, dK_j = scale sum_i dS_ij Q_i over the pair's rows.  A lane owns a key; what the lanes of keys that do not
+// count compute stays in their columns, and zeros are stored for them.
+template <int DHP>
+__global__ void __launch_bounds__(64 * PARTS, 1) cross_dkv_f32_kernel(CrossArgs a) {
+  __shared__ float lds[(PARTS - 1) * (DHP / 2) * 64];
+  const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 5, l32 = lane & 31;
+  const Where w(a, (a.Sk + 31) / 32);
+  const int j0 = 32 * w.tile, j = j0 + l32, head0 = w.kh * a.group;
+  const long jc = min(j, a.Sk - 1);
+  const unsigned bits = key_bits(a, w.b, j0, w.len, l32);
+  const bool on = (bits >> l32) & 1u;
+  f32x16 dk[DHP / 32], dv[DHP / 32];
+#pragma unroll
+  for (int dt = 0; dt < DHP / 32; dt++) dk[dt] = dv[dt] = zero16();
+  if (bits) {                                                    // the same for the whole workgroup
+    f32x4 kf[DHP / 8], vf[DHP / 8];
+    load_rows<DHP>(f32_of(a.k) + pair_offset(a.sk, w.b, w.kh) + jc * a.sk.t, a.dh, g, kf);
+    load_rows<DHP>(f32_of(a.v) + pair_offset(a.sv, w.b, w.kh) + jc * a.sv.t, a.dh, g, vf);
+    const float* const qb = f32_of(a.q) + pair_offset(a.sq, w.b, head0);
+    const float* const dob = f32_of(a.d_o) + pair_offset(a.sdo, w.b, head0);
+    const float* const lrow = a.lrow + (long)w.pair * a.rows;
+    const float* const drow = a.drow + (long)w.pair * a.rows;
+    const int nt = (a.rows + 31) / 32;
+    const int t0 = (int)((long)nt * w.split / a.splits), t1 = (int)((long)nt * (w.split + 1) / a.splits);
+    for (int t = t0 + part; t < t1; t += PARTS) {
+      const int i0 = 32 * t, left = a.rows - i0, ir = min(i0 + l32, a.rows - 1);
+      const unsigned rbits = left >= 32 ? ALL : (1u << left) - 1u;
+      f32x16 p, ds;
+      {
+        f32x4 xf[DHP / 8];
+        load_rows<DHP>(qb + row_offset(a.sq, a.group, ir), a.dh, g, xf);
+        p = row_product<DHP>(xf, kf);                            // S[i][j]
+        if (DHP > 64) __builtin_amdgcn_sched_barrier(0);         // one operand in registers at a time
+        load_rows<DHP>(dob + row_offset(a.sdo, a.group, ir), a.dh, g, xf);
+        ds = row_product<DHP>(xf, vf);                           // dP[i][j]
+      }
+#pragma unroll
+      for (int v = 0; v < 16; v++) {
+        const int i = min(i0 + acc_row(v, g), a.rows - 1);
+        p[v] = bit_of(rbits, v, g) ? expf(p[v] * a.scale - lrow[i]) : 0.f;
+        ds[v] = bit_of(rbits, v, g) ? p[v] * (ds[v] - drow[i]) : 0.f;
+      }
+      if (DHP >= 64) __builtin_amdgcn_sched_barrier(0);
+      col_product<DHP>(dv, p, [&](int v) { return dob + row_offset(a.sdo, a.group, min(i0 + acc_row(v, g), a.rows - 1)); }, rbits,
+                       a.dh, g, l32);
+      if (DHP > 64) __builtin_amdgcn_sched_barrier(0);
+      col_product<DHP>(dk, ds, [&](int v) { return qb + row_offset(a.sq, a.group, min(i0 + acc_row(v, g), a.rows - 1)); }, rbits,
+                       a.dh, g, l32);
+    }
+  }
+  merge_parts(dk, lds, part, lane);
+  merge_parts(dv, lds, part, lane);
+  if (part != 0 || j >= a.Sk) return;
+  if (a.splits > 1) {
+    if (!on) return;                                             // the launch that joins the splits stores zeros
+    float* dst = a.part + (((long)w.split * a.B * a.hk + w.pair) * a.Sk + j) * 2 * a.dh;
+    store_column<DHP>(dk, dst, a.scale, a.dh, g);
+    store_column<DHP>(dv, dst + a.dh, 1.0f, a.dh, g);
+    return;
+  }
+  if (!on) {
+#pragma unroll
+    for (int dt = 0; dt < DHP / 32; dt++) dk[dt] = dv[dt] = zero16();
+  }
+  store_column<DHP>(dk, static_cast<float*>(a.dk) + pair_offset(a.sdk, w.b, w.kh) + (long)j * a.sdk.t, a.scale, a.dh, g);
+  store_column<DHP>(dv, static_cast<float*>(a.dv) + pair_offset(a.sdv, w.b, w.kh) + (long)j * a.sdv.t, 1.0f, a.dh, g);
+}
+
+int parts(long blocks, long units, long want, long least) {
+  long n = blocks >= want || blocks == 0 ? 1 : want / blocks;
+  if (n > units / least) n = units / least;
+  return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+}
+
+#define GX_CROSS_F32(KERNEL, TILES)                                                                       \
+  do {                                                                                                    \
+    const dim3 grid((unsigned)((long)a.B * a.hk * (TILES) * a.splits)), block(64 * PARTS);                \
+    if (a.dh <= 32) hipLaunchKernelGGL(KERNEL<32>, grid, block, 0, s, a);                                 \
+    else if (a.dh <= 64) hipLaunchKernelGGL(KERNEL<64>, grid, block, 0, s, a);                            \
+    else hipLaunchKernelGGL(KERNEL<128>, grid, block, 0, s, a);                                           \
+  } while (0)
+
+}  // namespace
+
+CrossSplits cross_splits_f32(const CrossArgs& a) {
+  const long pairs = (long)a.B * a.hk;
+  return CrossSplits{parts(pairs * cdiv(a.rows, 32), cdiv(a.Sk, 32), 512, 8), parts(pairs * cdiv(a.rows, 32), cdiv(a.Sk, 32), 512, 8),
+                     parts(pairs * cdiv(a.Sk, 32), cdiv(a.rows, 32), 256, 8)};
+}
+
+hipError_t cross_fwd_f32(const CrossArgs& args, hipStream_t s) {
+  CrossArgs a = args;
+  a.splits = cross_splits_f32(a).fwd;
+  GX_CROSS_F32(cross_fwd_f32_kernel, cdiv(a.rows, 32));
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || a.splits == 1 ? e : cross_join_fwd(false, a, s);
+}
+
+hipError_t cross_bwd_f32(const CrossArgs& args, hipStream_t s) {
+  CrossArgs a = args;
+  const CrossSplits n = cross_splits_f32(a);
+  hipError_t e = hipSuccess;
+  if (a.rows > 0) {
+    a.splits = n.dq;
+    GX_CROSS_F32(cross_dq_f32_kernel, cdiv(a.rows, 32));
+    e = hipGetLastError();
+    if (e == hipSuccess && a.splits > 1) e = cross_join_dq(false, a, s);
+  }
+  if (e != hipSuccess || a.Sk == 0) return e;
+  a.splits = n.dkv;
+  GX_CROSS_F32(cross_dkv_f32_kernel, cdiv(a.Sk, 32));
+  e = hipGetLastError();
+  return e != hipSuccess || a.splits == 1 ? e : cross_join_dkv(false, a, s);
+}
+
+}  // namespace gx

@@ -162,3 +162,59 @@ class DeviceHeadNorm(_Operator):
         gx.heads_norm_bwd(cfg, inputs, dq_out if q is not None else None, dk_out if k is not None else None, dq, dk, dg[0], dg[1],
                           ws, stream)
         return dq, dk, dg[0], dg[1]
+
+
+class DeviceCrossAttention(_Operator):
+    """softmax(scale Q K^T over the keys that count) V for queries and keys of different sequences; query head h reads key head
+    h // (query heads / key heads).  scale: 1 / sqrt(head_dim) unless given."""
+
+    def __init__(self, head_dim, dtype="bf16", scale=None, device="cuda:0"):
+        super().__init__(dtype, device)
+        self.head_dim, self.scale = head_dim, head_dim ** -0.5 if scale is None else scale
+
+    def _args(self, q, k, v, key_lens, key_mask):
+        for name, x in (("q", q), ("k", k), ("v", v)):
+            _need(x.dim() == 4 and x.shape[3] == self.head_dim, f"{name}: not [batch, tokens, heads, {self.head_dim}]")
+            self._check(name, x)
+        b, n, hq, _ = q.shape
+        m, hk = k.shape[1], k.shape[2]
+        _need(k.shape[0] == b and k.shape == v.shape, "keys and values of one shape, as many samples as queries")
+        if key_lens is not None:
+            self._check("key_lens", key_lens, (b,), torch.int32, contiguous=True)
+        if key_mask is not None:
+            _need(key_mask.dtype in (torch.bool, torch.uint8), f"key_mask: {key_mask.dtype}, not bool or uint8")
+            self._check("key_mask", key_mask, (b, m), key_mask.dtype, contiguous=True)
+        cfg = gx.CrossCfg(b, n, m, hq, hk, self.head_dim, self.gtype, 0, self.scale)
+        return cfg, gx.cross_in(q, k, v, key_lens, key_mask)
+
+    def forward(self, q, k, v, key_lens=None, key_mask=None, want_lse=True, out=None):
+        """q [batch, queries, heads, head_dim], k, v [batch, keys, key heads, head_dim], key_lens int32 [batch], key_mask bool or bytes
+        [batch, keys] -> (o, lse); lse fp32 [batch, heads, queries] is for the backward pass, None without want_lse"""
+        cfg, inputs = self._args(q, k, v, key_lens, key_mask)
+        if out is None:
+            out = torch.empty(q.shape, dtype=self.tdtype, device=self.device)
+        else:
+            self._check("out", out, q.shape)
+        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=self.device) if want_lse else None
+        stream = self._stream()
+        nbytes = gx.cross_workspace_bytes(cfg, False)
+        gx.cross_fwd(cfg, inputs, out, lse, self._workspace(nbytes, stream) if nbytes else None, stream)
+        return out, lse
+
+    def backward(self, q, k, v, o, lse, do, key_lens=None, key_mask=None, dq=None, dk=None, dv=None):
+        """The forward pass's inputs and outputs and the gradient of o -> (dq, dk, dv)"""
+        cfg, inputs = self._args(q, k, v, key_lens, key_mask)
+        self._check("o", o, q.shape)
+        self._check("do", do, q.shape)
+        self._check("lse", lse, (q.shape[0], q.shape[2], q.shape[1]), torch.float32, contiguous=True)
+        outs = []
+        for x, d, name in ((q, dq, "dq"), (k, dk, "dk"), (v, dv, "dv")):
+            if d is None:
+                d = torch.empty(x.shape, dtype=self.tdtype, device=self.device)
+            else:
+                self._check(name, d, x.shape)
+            outs.append(d)
+        stream = self._stream()
+        ws = self._workspace(gx.cross_workspace_bytes(cfg, True), stream)
+        gx.cross_bwd(cfg, inputs, o, lse, do, *outs, ws, stream)
+        return tuple(outs)

@@ -124,3 +124,66 @@ def test_head_norm_pointers_and_strides():
     assert gx.heads_norm_bwd(c, _norm_in(), _View(), _View(), _View(), _View(), P + 4, P, P, check=False) == 5
     with pytest.raises(ValueError, match="contiguous columns"):
         gx.heads(_View(strides=(4096, 1024, 64, 2)))
+
+
+def _cross(**kw):
+    d = dict(batch=2, q_len=3, k_len=3, q_heads=8, k_heads=8, head_dim=64, dtype=gx.GX_BF16, flags=0, scale=0.125)
+    d.update(kw)
+    return gx.CrossCfg(*d.values())
+
+
+def _cross_in(q=None, k=None, v=None, lens=None, mask=None):
+    return gx.cross_in(q or _View(), k or _View(), v or _View(), lens, mask)
+
+
+def _cross_both(c, i, out=None):
+    o = out or _View()
+    return {gx.cross_fwd(c, i, o, P, P, check=False), gx.cross_bwd(c, i, _View(), P, _View(), o, o, o, P, check=False)}
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(batch=0), 2), (dict(q_len=-1), 2), (dict(k_len=-1), 2), (dict(k_len=(1 << 22) + 1), 2), (dict(q_heads=0), 2),
+    (dict(k_heads=3), 3), (dict(q_heads=4), 3), (dict(head_dim=96), 2), (dict(head_dim=256), 2),
+    (dict(head_dim=62, dtype=gx.GX_F32), 3), (dict(head_dim=132, dtype=gx.GX_F32), 2), (dict(dtype=3), 4), (dict(flags=1), 6),
+    (dict(scale=0.0), 2), (dict(scale=-1.0), 2), (dict(scale=float("nan")), 2), (dict(scale=float("inf")), 2),
+    (dict(q_len=1 << 28), 2), (dict(batch=1 << 22, k_len=4096), 2)])
+def test_cross_attention_refuses(kw, status):
+    assert _cross_both(_cross(**kw), _cross_in()) == {status}
+    assert gx.cross_workspace_bytes(_cross(**kw), False) == gx.cross_workspace_bytes(_cross(**kw), True) == 0
+
+
+def test_cross_attention_pointers_and_strides():
+    c = _cross()
+    assert _cross_both(c, _cross_in(k=_View(address=0))) == {1}
+    assert _cross_both(c, _cross_in(v=_View(address=P + 8))) == {5}
+    assert _cross_both(c, _cross_in(lens=P + 2)) == {5}
+    assert _cross_both(c, _cross_in(q=_View(strides=(4096, 1022, 64, 1)))) == {5}
+    assert _cross_both(c, _cross_in(k=_View(strides=(4096, 32, 64, 1)))) == {2}          # tokens of keys overlap
+    assert _cross_both(c, _cross_in(v=_View(strides=(4096, 1 << 23, 64, 1)))) == {2}
+    assert _cross_both(c, _cross_in(), _View(strides=(0, 1024, 64, 1))) == {2}             # outputs that repeat
+    far = _View(strides=(1 << 34, 1024, 1 << 31, 1))
+    assert gx.cross_fwd(_cross(k_heads=1), _cross_in(q=far), _View(), P, P, check=False) == 2
+    good = _View()
+    assert gx.cross_bwd(c, _cross_in(), good, None, good, good, good, good, P, check=False) == 1
+    assert gx.cross_bwd(c, _cross_in(), good, P, good, good, good, good, None, check=False) == 1
+    assert gx.cross_bwd(c, _cross_in(), good, P, _View(address=0), good, good, good, P, check=False) == 1
+    assert gx.cross_fwd(c, _cross_in(), good, P + 2, P, check=False) == 5
+    import torch
+    if not torch.cuda.is_available():                              # the last check before a launch
+        assert _cross_both(c, _cross_in(k=_View(strides=(0, 1024, 0, 1)))) == {7}
+        assert _cross_both(_cross(k_len=0), _cross_in(k=_View(address=0), v=_View(address=0))) == {7}
+        assert gx.cross_fwd(c, _cross_in(), good, None, None, check=False) == 7
+
+
+def test_cross_attention_scratch():
+    # one query against a long cache is split and needs room for the parts: sums, reference and total of a row each
+    one = _cross(batch=1, q_len=1, k_len=8192, q_heads=8, k_heads=8)
+    n = gx.cross_workspace_bytes(one, False)
+    assert n > 0 and n % (8 * (64 + 2) * 4) == 0
+    # work for the whole chip is not
+    assert gx.cross_workspace_bytes(_cross(batch=8, q_len=2048, k_len=2048, q_heads=16, k_heads=16), False) == 0
+    for dtype in (gx.GX_BF16, gx.GX_F32):
+        for q, k in ((0, 0), (0, 100), (100, 0)):
+            assert gx.cross_workspace_bytes(_cross(q_len=q, k_len=k, dtype=dtype), False) >= 0
+        # D and lse of every row at least
+        assert gx.cross_workspace_bytes(_cross(q_len=500, k_len=64, dtype=dtype), True) >= 2 * 4 * 2 * 8 * 500
