@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libgx.so")
@@ -83,32 +84,18 @@ class StrategyCosts(ctypes.Structure):
                                                "flops_ffn")]
 
 
-class EmbedCfg(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "hidden", "rows", "dtype", "id_bytes", "flags")] + \
-               [("first_row", ctypes.c_int64), ("pad_id", ctypes.c_int64), ("scale", ctypes.c_float)]
+# Records of the operators around a block, packed as C lays them out ("0q": padded to 8 bytes); they are made anew for every call,
+# which a ctypes.Structure takes several times as long for.
+def _record(fmt):
+    return struct.Struct("@" + fmt + "0q").pack
 
 
-class Heads(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("batch", "token", "head")]
-
-
-class HeadsNormCfg(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "q_len", "k_len", "q_heads", "k_heads", "head_dim", "rot_dim",
-                                               "max_pos", "dtype", "flags")] + [("eps", ctypes.c_float)]
-
-
-class HeadsNormIn(ctypes.Structure):
-    _fields_ = [("q", Heads), ("k", Heads)] + [(n, ctypes.c_void_p) for n in ("q_gain", "k_gain", "q_pos", "k_pos",
-                                                                              "cos_table", "sin_table")]
-
-
-class CrossCfg(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "q_len", "k_len", "q_heads", "k_heads", "head_dim", "dtype", "flags")] + \
-               [("scale", ctypes.c_float)]
-
-
-class CrossIn(ctypes.Structure):
-    _fields_ = [("q", Heads), ("k", Heads), ("v", Heads), ("key_lens", ctypes.c_void_p), ("key_mask", ctypes.c_void_p)]
+EmbedCfg = _record("6i2qf")         # tokens, hidden, rows, dtype, id_bytes, flags, first_row, pad_id, scale
+HeadsNormCfg = _record("10if")      # batch, q_len, k_len, q_heads, k_heads, head_dim, rot_dim, max_pos, dtype, flags, eps
+CrossCfg = _record("8if")           # batch, q_len, k_len, q_heads, k_heads, head_dim, dtype, flags, scale
+_Heads = _record("P3q")             # data, strides of batch, token, head
+_HeadsNormIn = _record("P3qP3q6P")
+_CrossIn = _record("P3qP3qP3q2P")
 
 
 class GxError(RuntimeError):
@@ -175,25 +162,13 @@ def lib():
         L.gx_peak_copy.restype = ctypes.c_int
         L.gx_strategy_cost.argtypes = [ctypes.POINTER(StrategyQuery), ctypes.POINTER(StrategyCosts)]
         L.gx_strategy_cost.restype = ctypes.c_int
-        L.gx_embed_workspace_bytes.argtypes = [ctypes.POINTER(EmbedCfg)]
-        L.gx_embed_workspace_bytes.restype = ctypes.c_size_t
-        L.gx_embed_fwd.argtypes = [ctypes.POINTER(EmbedCfg), P, P, P, P]
-        L.gx_embed_fwd.restype = ctypes.c_int
-        L.gx_embed_bwd.argtypes = [ctypes.POINTER(EmbedCfg), P, P, P, P, P]
-        L.gx_embed_bwd.restype = ctypes.c_int
-        H = ctypes.POINTER(Heads)
-        L.gx_heads_norm_workspace_bytes.argtypes = [ctypes.POINTER(HeadsNormCfg)]
-        L.gx_heads_norm_workspace_bytes.restype = ctypes.c_size_t
-        L.gx_heads_norm_fwd.argtypes = [ctypes.POINTER(HeadsNormCfg), ctypes.POINTER(HeadsNormIn), H, H, P]
-        L.gx_heads_norm_fwd.restype = ctypes.c_int
-        L.gx_heads_norm_bwd.argtypes = [ctypes.POINTER(HeadsNormCfg), ctypes.POINTER(HeadsNormIn), H, H, H, H, P, P, P, P]
-        L.gx_heads_norm_bwd.restype = ctypes.c_int
-        L.gx_cross_workspace_bytes.argtypes = [ctypes.POINTER(CrossCfg), ctypes.c_int]
-        L.gx_cross_workspace_bytes.restype = ctypes.c_size_t
-        L.gx_cross_fwd.argtypes = [ctypes.POINTER(CrossCfg), ctypes.POINTER(CrossIn), H, P, P, P]
-        L.gx_cross_fwd.restype = ctypes.c_int
-        L.gx_cross_bwd.argtypes = [ctypes.POINTER(CrossCfg), ctypes.POINTER(CrossIn), H, P, H, H, H, H, P, P]
-        L.gx_cross_bwd.restype = ctypes.c_int
+        for name, n in (("embed_fwd", 5), ("embed_bwd", 6), ("heads_norm_fwd", 5), ("heads_norm_bwd", 10), ("cross_fwd", 6),
+                        ("cross_bwd", 10)):
+            f = getattr(L, "gx_" + name)
+            f.argtypes, f.restype = [P] * n, ctypes.c_int
+        for name, more in (("embed", []), ("heads_norm", []), ("cross", [ctypes.c_int])):
+            f = getattr(L, f"gx_{name}_workspace_bytes")
+            f.argtypes, f.restype = [P] + more, ctypes.c_size_t
         _lib = L
     return _lib
 
@@ -416,82 +391,74 @@ def peak_copy(src, dst, nbytes, launches=20, stream=0):
 
 
 
-def heads(t):
-    """gx_heads of a tensor [batch, tokens, heads, columns] with contiguous columns (None: nothing)."""
+def _heads(t):
     if t is None:
-        return Heads(None, 0, 0, 0)
+        return 0, 0, 0, 0
     st = t.stride()
     if len(st) != 4 or (st[3] != 1 and t.shape[3] > 1):
         raise ValueError("a tensor [batch, tokens, heads, columns] with contiguous columns")
-    return Heads(t.data_ptr(), st[0], st[1], st[2])
+    return t.data_ptr(), st[0], st[1], st[2]
 
 
-def embed_workspace_bytes(cfg):
-    return int(lib().gx_embed_workspace_bytes(ctypes.byref(cfg)))
-
-
-def embed_fwd(cfg, table, ids, y, stream=0, check=True):
-    st = lib().gx_embed_fwd(ctypes.byref(cfg), _ptr(table), _ptr(ids), _ptr(y), ctypes.c_void_p(stream))
-    if check and st != GX_OK:
-        raise GxError(st, "gx_embed_fwd")
-    return int(st)
-
-
-def embed_bwd(cfg, ids, dy, dtable, workspace, stream=0, check=True):
-    st = lib().gx_embed_bwd(ctypes.byref(cfg), _ptr(ids), _ptr(dy), _ptr(dtable), _ptr(workspace), ctypes.c_void_p(stream))
-    if check and st != GX_OK:
-        raise GxError(st, "gx_embed_bwd")
-    return int(st)
+def heads(t):
+    """gx_heads of a tensor [batch, tokens, heads, columns] with contiguous columns (None: nothing)."""
+    return None if t is None else _Heads(*_heads(t))
 
 
 def _addr(t):
-    return None if t is None else t if isinstance(t, int) else t.data_ptr()
+    return 0 if t is None else t if isinstance(t, int) else t.data_ptr()
+
+
+def _checked(st, where, check):
+    if check and st != GX_OK:
+        raise GxError(st, where)
+    return st
+
+
+def embed_workspace_bytes(cfg):
+    return lib().gx_embed_workspace_bytes(cfg)
+
+
+def embed_fwd(cfg, table, ids, y, stream=0, check=True):
+    return _checked(lib().gx_embed_fwd(cfg, _addr(table), _addr(ids), _addr(y), stream), "gx_embed_fwd", check)
+
+
+def embed_bwd(cfg, ids, dy, dtable, workspace, stream=0, check=True):
+    return _checked(lib().gx_embed_bwd(cfg, _addr(ids), _addr(dy), _addr(dtable), _addr(workspace), stream), "gx_embed_bwd", check)
 
 
 def heads_norm_in(q, k, q_gain, k_gain, q_pos, k_pos, cos_table, sin_table):
     """q, k: tensors as `heads` takes them, or None."""
-    return HeadsNormIn(heads(q), heads(k), _addr(q_gain), _addr(k_gain), _addr(q_pos), _addr(k_pos), _addr(cos_table),
-                       _addr(sin_table))
+    return _HeadsNormIn(*_heads(q), *_heads(k), _addr(q_gain), _addr(k_gain), _addr(q_pos), _addr(k_pos), _addr(cos_table),
+                        _addr(sin_table))
 
 
 def heads_norm_workspace_bytes(cfg):
-    return int(lib().gx_heads_norm_workspace_bytes(ctypes.byref(cfg)))
+    return lib().gx_heads_norm_workspace_bytes(cfg)
 
 
 def heads_norm_fwd(cfg, inputs, q_out, k_out, stream=0, check=True):
-    st = lib().gx_heads_norm_fwd(ctypes.byref(cfg), ctypes.byref(inputs), heads(q_out), heads(k_out), ctypes.c_void_p(stream))
-    if check and st != GX_OK:
-        raise GxError(st, "gx_heads_norm_fwd")
-    return int(st)
+    return _checked(lib().gx_heads_norm_fwd(cfg, inputs, heads(q_out), heads(k_out), stream), "gx_heads_norm_fwd", check)
 
 
 def heads_norm_bwd(cfg, inputs, dq_out, dk_out, dq, dk, dq_gain, dk_gain, workspace, stream=0, check=True):
-    st = lib().gx_heads_norm_bwd(ctypes.byref(cfg), ctypes.byref(inputs), heads(dq_out), heads(dk_out), heads(dq), heads(dk),
-                                 _ptr(dq_gain), _ptr(dk_gain), _ptr(workspace), ctypes.c_void_p(stream))
-    if check and st != GX_OK:
-        raise GxError(st, "gx_heads_norm_bwd")
-    return int(st)
+    return _checked(lib().gx_heads_norm_bwd(cfg, inputs, heads(dq_out), heads(dk_out), heads(dq), heads(dk), _addr(dq_gain),
+                                            _addr(dk_gain), _addr(workspace), stream), "gx_heads_norm_bwd", check)
 
 
 def cross_in(q, k, v, key_lens=None, key_mask=None):
     """q, k, v: tensors as `heads` takes them."""
-    return CrossIn(heads(q), heads(k), heads(v), _addr(key_lens), _addr(key_mask))
+    return _CrossIn(*_heads(q), *_heads(k), *_heads(v), _addr(key_lens), _addr(key_mask))
 
 
 def cross_workspace_bytes(cfg, is_backward):
-    return int(lib().gx_cross_workspace_bytes(ctypes.byref(cfg), int(bool(is_backward))))
+    return lib().gx_cross_workspace_bytes(cfg, bool(is_backward))
 
 
 def cross_fwd(cfg, inputs, o, lse, workspace, stream=0, check=True):
-    st = lib().gx_cross_fwd(ctypes.byref(cfg), ctypes.byref(inputs), heads(o), _ptr(lse), _ptr(workspace), ctypes.c_void_p(stream))
-    if check and st != GX_OK:
-        raise GxError(st, "gx_cross_fwd")
-    return int(st)
+    return _checked(lib().gx_cross_fwd(cfg, inputs, heads(o), _addr(lse), _addr(workspace), stream), "gx_cross_fwd", check)
 
 
 def cross_bwd(cfg, inputs, o, lse, d_o, dq, dk, dv, workspace, stream=0, check=True):
-    st = lib().gx_cross_bwd(ctypes.byref(cfg), ctypes.byref(inputs), heads(o), _ptr(lse), heads(d_o), heads(dq), heads(dk),
-                            heads(dv), _ptr(workspace), ctypes.c_void_p(stream))
-    if check and st != GX_OK:
-        raise GxError(st, "gx_cross_bwd")
-    return int(st)
+    return _checked(lib().gx_cross_bwd(cfg, inputs, heads(o), _addr(lse), heads(d_o), heads(dq), heads(dk), heads(dv),
+                                       _addr(workspace), stream), "gx_cross_bwd", check)
