@@ -1,8 +1,8 @@
 // Token embedding: lookup with scaling, and the gradient of the table by sorted tokens.
 //
 // y[t] = s E[id_t - first] is a gather of rows, bound by memory.  Its transpose, dE[v] = s sum_{id_t = first + v} dy[t], has
-// outputs of very uneven length: text repeats few tokens very often.  So the tokens are sorted by row first (stable, so that
-// a row's tokens keep their order), the sorted tokens are cut into pieces of equal length, whoever they belong to,
+// outputs of very uneven length: text repeats few tokens very often.  So the tokens are sorted by row first (stably: a row's
+// tokens keep their order), the sorted tokens are cut into pieces of equal length, whoever they belong to,
 // and every piece adds up its runs of equal rows: a run that lies inside a piece is stored, one that crosses the piece's ends leaves
 // a partial sum, and the partial sums of a run are added in order afterwards.  No floating-point atomics; the order of every
 // sum depends on sizes and ids alone.
@@ -21,160 +21,217 @@ template <typename T> struct Lanes;                            // elements of 16
 template <> struct Lanes<float> { static constexpr int N = 4; typedef f32x4 type; };
 template <> struct Lanes<bf16> { static constexpr int N = 8; typedef bf16x8 type; };
 
-// The row of this shard that token t points to, or -1
+// Ids of type I (a template argument throughout: a choice at run time keeps loads from being issued together); the row
+// of this shard that token t points to, or -1
+template <typename I>
 struct Ids {
-  const void* p;
-  int bytes;
+  const I* p;
   long first, rows;
-  GX_DEVINL long row(int t) const {
-    const long id = bytes == 8 ? static_cast<const long*>(p)[t] : (long)static_cast<const int*>(p)[t];
-    const unsigned long r = (unsigned long)id - (unsigned long)first;
+  GX_DEVINL long row_of(I id) const {
+    const unsigned long r = (unsigned long)(long)id - (unsigned long)first;
     return r < (unsigned long)rows ? (long)r : -1;
   }
+  GX_DEVINL long row(int t) const { return row_of(p[t]); }
 };
 
 // ------------------------------------------------------------------------------- forward
-// `lpr` lanes (a power of two) to a row, 16 bytes each at a time
-template <typename T>
-__global__ void __launch_bounds__(256) embed_fwd_kernel(const T* __restrict__ table, Ids ids, T* __restrict__ y, int tokens,
+// `lpr` lanes (a power of two) to a row, 16 bytes each at a time; a lane's ROWS tokens are looked up together, so that as many
+// dependent pairs of loads (id, then row) are in flight.  Few tokens take one a lane and spread their columns over blockIdx.y.
+template <typename T, typename I, int ROWS>
+__global__ void __launch_bounds__(256) embed_fwd_kernel(const T* __restrict__ table, Ids<I> ids, T* __restrict__ y, int tokens,
                                                         int hidden, int lpr_log, float scale) {
   constexpr int V = Lanes<T>::N;
   typedef typename Lanes<T>::type Raw;
-  const int lpr = 1 << lpr_log, c0 = threadIdx.x & (lpr - 1), chunks = hidden / V;
-  const int t = (blockIdx.x << (8 - lpr_log)) + (threadIdx.x >> lpr_log);
-  if (t >= tokens) return;
-  const long r = ids.row(t);
-  const T* src = table + (size_t)(r < 0 ? 0 : r) * hidden;
-  T* dst = y + (size_t)t * hidden;
-  for (int c = c0 + blockIdx.y * lpr; c < chunks; c += lpr * gridDim.y) {
-    Raw v = {};
-    if (r >= 0) {
-      v = *reinterpret_cast<const Raw*>(src + (size_t)c * V);
+  const int lpr = 1 << lpr_log, chunks = hidden / V, step = 256 >> lpr_log;
+  const int t0 = blockIdx.x * (step * ROWS) + (threadIdx.x >> lpr_log);
+  long r[ROWS];
 #pragma unroll
-      for (int e = 0; e < V; e++) v[e] = from_f32<T>(to_f32(v[e]) * scale);
+  for (int k = 0; k < ROWS; k++) r[k] = t0 + k * step < tokens ? ids.row(t0 + k * step) : -1;
+  for (int c = (threadIdx.x & (lpr - 1)) + blockIdx.y * lpr; c < chunks; c += lpr * gridDim.y) {
+    Raw v[ROWS];
+#pragma unroll
+    for (int k = 0; k < ROWS; k++) {
+      v[k] = Raw{};
+      if (r[k] >= 0) v[k] = *reinterpret_cast<const Raw*>(table + (size_t)r[k] * hidden + (size_t)c * V);
     }
-    *reinterpret_cast<Raw*>(dst + (size_t)c * V) = v;
+#pragma unroll
+    for (int k = 0; k < ROWS; k++) {
+      if (r[k] >= 0)
+#pragma unroll
+        for (int e = 0; e < V; e++) v[k][e] = from_f32<T>(to_f32(v[k][e]) * scale);
+      if (t0 + k * step < tokens) *reinterpret_cast<Raw*>(y + (size_t)(t0 + k * step) * hidden + (size_t)c * V) = v[k];
+    }
   }
 }
 
 // ------------------------------------------------------------------------------- backward: sort
-// Stable radix sort of (row, token) by row, digits of up to 9 bits from the lowest up; tokens without a gradient sort behind
-// the last row.  A block owns TPB consecutive tokens, its wavefronts consecutive parts of them, 64 at a time: a token's place among
-// those of its digit is the count of earlier ones in the wavefront (kept in LDS, one counter per wavefront and
-// digit), plus those of earlier wavefronts, plus those of earlier blocks, plus those of lower digits.
-constexpr int DIGIT_BITS = 9, DIGITS = 1 << DIGIT_BITS;
-constexpr int SORT_WAVES = 8, SORT_THREADS = 64 * SORT_WAVES, ROUNDS = 8, TPB = SORT_THREADS * ROUNDS;
-static_assert(SORT_THREADS == DIGITS, "one thread to a digit");
+// Every workgroup owns `span` consecutive rows of the table and sorts the tokens that point to them, all by itself: it looks
+// at all the ids, counts those of earlier rows (its place in the result) and its own, lists its own in order, and sorts the list by
+// row, stably.  A wavefront takes a consecutive part of what is gone over each time, 64 at a time: a token's place is that of its
+// row's first one, plus the count of that row's tokens in earlier wavefronts, plus those before it in its own (the lanes with the
+// same row, found by ballots over the row's bits).
+// The ids are read once by each workgroup, from L2: 64 workgroups and 8192 ids 4 MB, for which the rest of the pass moves hundreds.
+// 8192 tokens, 32768 rows: 9 us (a radix sort over blocks of tokens, two launches to a digit, took 28).  Ids that are not all requested
+// before the first is looked at cost another 5.
+constexpr int SORT_WAVES = 8, SORT_THREADS = 64 * SORT_WAVES, MAX_SPAN = 2048;
 
+template <typename I>
 struct SortArgs {
-  Ids ids;
+  Ids<I> ids;
   long pad_row;                    // relative to the shard, -1: none
-  int tokens, shift, mask;
-  const unsigned *key_in, *tok_in; // null in the first pass: keys come from the ids, tokens are in order
-  unsigned *key_out, *tok_out;
-  unsigned* hist;                  // [blocks][DIGITS]
+  int tokens, span, span_log;
+  unsigned *list_key, *list_tok;   // the workgroups' lists, unsorted
+  unsigned *key, *tok;             // the result: rows and tokens, sorted
+  unsigned* start;                 // [rows + 1]: where a row's tokens start; the last one says how many there are in all
 };
-GX_DEVINL unsigned key_of(const SortArgs& a, int i) {
-  if (a.key_in) return a.key_in[i];
-  const long r = a.ids.row(i);
-  return r < 0 || r == a.pad_row ? (unsigned)a.ids.rows : (unsigned)r;
-}
 
-__global__ void __launch_bounds__(SORT_THREADS) embed_count_kernel(SortArgs a) {
-  __shared__ unsigned n[DIGITS];
-  n[threadIdx.x] = 0;
-  __syncthreads();
-  const int i0 = blockIdx.x * TPB + threadIdx.x;
-#pragma unroll
-  for (int r = 0; r < ROUNDS; r++) {
-    const int i = i0 + r * SORT_THREADS;
-    if (i < a.tokens) atomicAdd(&n[(key_of(a, i) >> a.shift) & a.mask], 1u);      // whole numbers: any order gives the same
-  }
-  __syncthreads();
-  a.hist[(size_t)blockIdx.x * DIGITS + threadIdx.x] = n[threadIdx.x];
-}
-
-__global__ void __launch_bounds__(SORT_THREADS) embed_place_kernel(SortArgs a, int blocks) {
-  __shared__ unsigned count[SORT_WAVES][DIGITS];
-  __shared__ unsigned wave_total[SORT_WAVES];
+template <typename I>
+__global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(SortArgs<I> a) {
+  __shared__ unsigned count[SORT_WAVES][MAX_SPAN];
+  __shared__ unsigned lower[SORT_WAVES], mine[SORT_WAVES], sums[SORT_WAVES];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int d0 = threadIdx.x;
-  // this thread's digit: how many in the whole, how many in the blocks before this one
-  unsigned before = 0, total = 0;
-  for (int b = 0; b < blocks; b++) {
-    const unsigned c = a.hist[(size_t)b * DIGITS + d0];
-    if (b < (int)blockIdx.x) before += c;
-    total += c;
-  }
+  const long lo = (long)blockIdx.x * a.span;
+  const int own_rows = (int)(a.ids.rows - lo < a.span ? a.ids.rows - lo : a.span);
+  const unsigned long long before_me = (1ull << lane) - 1ull;
+  for (int i = threadIdx.x; i < SORT_WAVES * a.span; i += SORT_THREADS) count[i >> a.span_log][i & (a.span - 1)] = 0;
+  // rows among this workgroup's, or beyond them, of tokens t, t + 64, ...: negative if it is an earlier one.  The loads are
+  // unconditional, so that all of them are in flight
+  constexpr int NONE = 1 << 30, AHEAD = 16;
+  auto rows_from = [&](int t, int end, int (&r)[AHEAD]) {
+    I id[AHEAD];
 #pragma unroll
-  for (int w = 0; w < SORT_WAVES; w++) count[w][d0] = 0;
-  __syncthreads();
-  unsigned key[ROUNDS], tok[ROUNDS], rank[ROUNDS];
-  const int i0 = blockIdx.x * TPB + wave * (64 * ROUNDS) + lane;
+    for (int u = 0; u < AHEAD; u++) id[u] = a.ids.p[min(t + 64 * u, end - 1)];
 #pragma unroll
-  for (int r = 0; r < ROUNDS; r++) {
-    const int i = i0 + 64 * r;
-    key[r] = i < a.tokens ? key_of(a, i) : 0u;
-    tok[r] = i < a.tokens ? (a.tok_in ? a.tok_in[i] : (unsigned)i) : 0u;
-  }
-#pragma unroll
-  for (int r = 0; r < ROUNDS; r++) {
-    const bool live = i0 + 64 * r < a.tokens;
-    const unsigned d = (key[r] >> a.shift) & a.mask;
-    unsigned long long same = __builtin_amdgcn_ballot_w64(live);
-#pragma unroll
-    for (int bit = 0; bit < DIGIT_BITS; bit++) {
-      const unsigned long long set = __builtin_amdgcn_ballot_w64((d >> bit) & 1u);
-      same &= ((d >> bit) & 1u) ? set : ~set;
+    for (int u = 0; u < AHEAD; u++) {
+      const long x = a.ids.row_of(id[u]);
+      r[u] = x < 0 || x == a.pad_row || t + 64 * u >= end ? NONE : (int)x - (int)lo;
     }
-    const unsigned earlier = __popcll(same & ((1ull << lane) - 1ull));
-    volatile unsigned* n = &count[wave][d];
-    const unsigned old = *n;
-    rank[r] = old + earlier;
-    if (live && earlier == 0) *n = old + (unsigned)__popcll(same);
-    __builtin_amdgcn_wave_barrier();
+  };
+  // this wavefront's part of the tokens
+  const int per = ((a.tokens + SORT_THREADS - 1) / SORT_THREADS) * 64;
+  const int t0 = min(wave * per, a.tokens), t1 = min(t0 + per, a.tokens);
+  unsigned below = 0, own = 0;
+  for (int t = t0 + lane; t < t1; t += 64 * AHEAD) {
+    int r[AHEAD];
+    rows_from(t, t1, r);
+#pragma unroll
+    for (int u = 0; u < AHEAD; u++) {
+      below += r[u] < 0;
+      own += (unsigned)r[u] < (unsigned)own_rows;
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    below += __shfl_xor(below, o, 64);
+    own += __shfl_xor(own, o, 64);
+  }
+  if (lane == 0) {
+    lower[wave] = below;
+    mine[wave] = own;
   }
   __syncthreads();
-  // places: exclusive sum of the totals over the digits, the earlier blocks, then wavefront by wavefront
+  unsigned base = 0, n = 0, before = 0;
+#pragma unroll
+  for (int w = 0; w < SORT_WAVES; w++) {
+    base += lower[w];
+    if (w < wave) before += mine[w];
+    n += mine[w];
+  }
+  // this wavefront's part of the list, in the order of the tokens, and the count of every row in it
+  unsigned* const list_key = a.list_key + base + before;
+  unsigned* const list_tok = a.list_tok + base + before;
+  if (own > 0) {
+    unsigned at = 0;
+    for (int t = t0 + lane; t < t0 + per; t += 64 * AHEAD) {
+      int r[AHEAD];
+      rows_from(t, t1, r);
+#pragma unroll
+      for (int u = 0; u < AHEAD; u++) {
+        const bool in = (unsigned)r[u] < (unsigned)own_rows;
+        const unsigned long long all = __builtin_amdgcn_ballot_w64(in);
+        if (in) {
+          const unsigned p = at + __popcll(all & before_me);
+          list_key[p] = (unsigned)r[u];
+          list_tok[p] = (unsigned)(t + 64 * u);
+          atomicAdd(&count[wave][r[u]], 1u);                       // whole numbers: any order gives the same
+        }
+        at += __popcll(all);
+      }
+    }
+  }
+  __syncthreads();
+  // places: a thread takes consecutive rows
+  const int rpt = (a.span + SORT_THREADS - 1) / SORT_THREADS, r0 = threadIdx.x * rpt;
+  unsigned total = 0;
+  for (int r = r0; r < r0 + rpt && r < a.span; r++)
+#pragma unroll
+    for (int w = 0; w < SORT_WAVES; w++) total += count[w][r];
   unsigned run = total;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const unsigned up = __shfl_up(run, o, 64);
     if (lane >= o) run += up;
   }
-  if (lane == 63) wave_total[wave] = run;
+  if (lane == 63) sums[wave] = run;
   __syncthreads();
-  unsigned place = run - total + before;
-  for (int w = 0; w < wave; w++) place += wave_total[w];
+  unsigned place = base + run - total;
 #pragma unroll
-  for (int w = 0; w < SORT_WAVES; w++) {
-    const unsigned c = count[w][d0];
-    count[w][d0] = place;
-    place += c;
-  }
-  __syncthreads();
+  for (int w = 0; w < SORT_WAVES; w++)
+    if (w < wave) place += sums[w];
+  for (int r = r0; r < r0 + rpt && r < a.span; r++) {
+    if (r < own_rows) a.start[lo + r] = place;
 #pragma unroll
-  for (int r = 0; r < ROUNDS; r++)
-    if (i0 + 64 * r < a.tokens) {
-      const unsigned at = count[wave][(key[r] >> a.shift) & a.mask] + rank[r];
-      a.key_out[at] = key[r];
-      a.tok_out[at] = tok[r];
+    for (int w = 0; w < SORT_WAVES; w++) {
+      const unsigned c = count[w][r];
+      count[w][r] = place;
+      place += c;
     }
+  }
+  if (lo + own_rows == a.ids.rows && threadIdx.x == 0) a.start[a.ids.rows] = base + n;
+  __syncthreads();
+  for (int i = lane; i < (int)((own + 63) & ~63u); i += 64 * 8) {
+    unsigned key[8], tok[8];
+#pragma unroll
+    for (int u = 0; u < 8; u++) {
+      const bool live = i + 64 * u < (int)own;
+      key[u] = live ? list_key[i + 64 * u] : 0u;
+      tok[u] = live ? list_tok[i + 64 * u] : 0u;
+    }
+#pragma unroll
+    for (int u = 0; u < 8; u++) {
+      const bool live = i + 64 * u < (int)own;
+      const unsigned d = key[u];
+      unsigned long long same = __builtin_amdgcn_ballot_w64(live);
+      if (same == 0) break;
+      for (int bit = 0; bit < a.span_log; bit++) {
+        const unsigned long long set = __builtin_amdgcn_ballot_w64((d >> bit) & 1u);
+        same &= ((d >> bit) & 1u) ? set : ~set;
+      }
+      const unsigned earlier = __popcll(same & before_me);
+      volatile unsigned* next = &count[wave][d];
+      const unsigned first = *next;
+      if (live) {
+        a.key[first + earlier] = (unsigned)lo + d;
+        a.tok[first + earlier] = tok[u];
+        if (earlier == 0) *next = first + (unsigned)__popcll(same);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
 }
 
 // ------------------------------------------------------------------------------- backward: sums
-__global__ void __launch_bounds__(256) embed_zero_kernel(f32x4* __restrict__ p, size_t n) {
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-}
-
 struct SumArgs {
   const unsigned *key, *tok;       // sorted
+  const unsigned* start;           // [rows + 1]
   const void* dy;
   float* dtable;
   float* part;                     // [piece][2][hidden]: a run that began before the piece, a run that goes on behind it
-  int tokens, hidden, rows, piece, pieces, accumulate;
+  int tokens, hidden, rows, pieces, accumulate;
+  int sum_blocks, fill_rows;       // workgroups that add; rows of the table that each of the others clears
   float scale;
 };
+constexpr int PIECE = 16;          // tokens of a piece: as many row loads in flight as a lane has registers for
 
 // Stores or adds a run's sum: 16 bytes of fp32 per lane and half of a bf16 chunk
 template <int V>
@@ -188,42 +245,62 @@ GX_DEVINL void put_row(float* dst, const float (&s)[V], float scale, bool accumu
   }
 }
 
-// `lpr` lanes own a piece of the sorted tokens and 16 bytes of every row each
+// The first workgroups: `lpr` lanes own a piece of the sorted tokens and 16 bytes of every row each.  The others clear the
+// rows to which no token points, so that the one's reads and the other's writes share the memory's time.
 template <typename T>
-__global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a, int lpr_log) {
-  constexpr int V = Lanes<T>::N, AHEAD = 4;
+__global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a, int lpr_log, int col_blocks) {
+  constexpr int V = Lanes<T>::N;
   typedef typename Lanes<T>::type Raw;
-  const int lpr = 1 << lpr_log;
-  const int p = (blockIdx.x << (8 - lpr_log)) + (threadIdx.x >> lpr_log);
-  const int c = (threadIdx.x & (lpr - 1)) + blockIdx.y * lpr;
+  if ((int)blockIdx.x >= a.sum_blocks) {
+    const int first = (blockIdx.x - a.sum_blocks) * a.fill_rows, chunks = a.hidden / 4;
+    const int log = min(8, 32 - __clz(chunks - 1)), lanes = 1 << log, c0 = threadIdx.x & (lanes - 1);
+    for (int r = first + (threadIdx.x >> log); r < min(first + a.fill_rows, a.rows); r += 256 >> log)
+      if (a.start[r] == a.start[r + 1]) {
+        f32x4* row = reinterpret_cast<f32x4*>(a.dtable + (size_t)r * a.hidden);
+        for (int c = c0; c < chunks; c += lanes) row[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    return;
+  }
+  const int lpr = 1 << lpr_log, pb = blockIdx.x / col_blocks, cb = blockIdx.x - pb * col_blocks;
+  const int p = (pb << (8 - lpr_log)) + (threadIdx.x >> lpr_log);
+  const int c = (threadIdx.x & (lpr - 1)) + cb * lpr;
+  const int i0 = p * PIECE;
   if (p >= a.pieces || c >= a.hidden / V) return;
-  const int i0 = p * a.piece, i1 = min(i0 + a.piece, a.tokens);
   const T* dy = static_cast<const T*>(a.dy) + (size_t)c * V;
-  const unsigned none = (unsigned)a.rows;
-  const bool from_before = i0 > 0 && a.key[i0 - 1] == a.key[i0];
-  const bool goes_on = i1 < a.tokens && a.key[i1] == a.key[i1 - 1];
+  unsigned k[PIECE + 1];
+  Raw x[PIECE];
+  const unsigned earlier = a.key[max(i0 - 1, 0)];
+  const int n = (int)a.start[a.rows];
+  int left;
+  {
+    unsigned t[PIECE];
+#pragma unroll
+    for (int u = 0; u <= PIECE; u++) {                 // all of them before n is known: what lies beyond is not used
+      const int i = min(i0 + u, a.tokens - 1);
+      k[u] = a.key[i];
+      if (u < PIECE) t[u] = a.tok[i];
+    }
+    left = min(PIECE, n - i0);
+    if (left <= 0) return;
+#pragma unroll
+    for (int u = 0; u < PIECE; u++) x[u] = *reinterpret_cast<const Raw*>(dy + (size_t)(u < left ? t[u] : t[0]) * a.hidden);
+  }
+  const bool from_before = i0 > 0 && earlier == k[0];
+  const bool goes_on = i0 + left < n && k[left] == k[left - 1];
   bool first_run = true;
   float s[V];
 #pragma unroll
   for (int e = 0; e < V; e++) s[e] = 0.f;
-  for (int i = i0; i < i1; i += AHEAD) {
-    Raw x[AHEAD];
-    unsigned k[AHEAD + 1];
 #pragma unroll
-    for (int u = 0; u <= AHEAD; u++) k[u] = i + u < i1 ? a.key[i + u] : none;
-    if (k[0] == none) break;                           // sorted: nothing that counts follows
-#pragma unroll
-    for (int u = 0; u < AHEAD; u++)
-      if (k[u] != none) x[u] = *reinterpret_cast<const Raw*>(dy + (size_t)a.tok[i + u] * a.hidden);
-#pragma unroll
-    for (int u = 0; u < AHEAD; u++) {
-      if (k[u] == none) break;
+  for (int u = 0; u < PIECE; u++) {
+    if (u < left) {
 #pragma unroll
       for (int e = 0; e < V; e++) s[e] += to_f32(x[u][e]);
-      const bool piece_end = i + u + 1 == i1;
+      const bool piece_end = u + 1 == left;
       if (piece_end || k[u + 1] != k[u]) {             // the run ends here, or is cut
-        if (first_run && from_before) put_row<V>(a.part + ((size_t)p * 2) * a.hidden + (size_t)c * V, s, 1.f, false);
-        else if (piece_end && goes_on) put_row<V>(a.part + ((size_t)p * 2 + 1) * a.hidden + (size_t)c * V, s, 1.f, false);
+        float* const part = a.part + (size_t)p * 2 * a.hidden + (size_t)c * V;
+        if (first_run && from_before) put_row<V>(part, s, 1.f, false);
+        else if (piece_end && goes_on) put_row<V>(part + a.hidden, s, 1.f, false);
         else put_row<V>(a.dtable + (size_t)k[u] * a.hidden + (size_t)c * V, s, a.scale, a.accumulate);
         first_run = false;
 #pragma unroll
@@ -233,24 +310,30 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a, int lpr_log) 
   }
 }
 
-// One block per piece: if a run begins in it and goes on behind it, adds the run's partial sums, piece by piece
+// One workgroup per piece and 256 columns: if a run begins in the piece and goes on behind it, adds the run's partial sums.  Each
+// wavefront takes a consecutive quarter of them, and the quarters are added in order.
 __global__ void __launch_bounds__(256) embed_join_kernel(SumArgs a) {
-  const int p = blockIdx.x, c = blockIdx.y * 256 + threadIdx.x;
-  const int i0 = p * a.piece, i1 = min(i0 + a.piece, a.tokens);
+  __shared__ f32x4 red[3][64];
+  const int p = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.y * 64 + lane;
+  const int i1 = (p + 1) * PIECE;
   if (i1 >= a.tokens) return;
-  const unsigned key = a.key[i1 - 1];
-  if (key >= (unsigned)a.rows || a.key[i1] != key) return;                 // nothing goes on
-  if (i0 > 0 && a.key[i0 - 1] == key) return;                              // it began in an earlier piece
-  // the run's last piece: the last one whose first token has this key
-  int lo = p + 1, hi = a.pieces - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (a.key[mid * a.piece] == key) lo = mid;
-    else hi = mid - 1;
+  const int n = (int)a.start[a.rows];
+  const unsigned key = a.key[i1 - 1], next = a.key[i1];
+  if (i1 >= n || next != key) return;                                      // nothing goes on
+  const int first = (int)a.start[key], end = (int)a.start[key + 1];
+  if (first < p * PIECE) return;                                           // it began in an earlier piece
+  const int last = (end - 1) / PIECE, rows = last - p + 1, per = (rows + 3) / 4;
+  const int q0 = p + min(wave * per, rows), q1 = min(q0 + per, last + 1);
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (c < a.hidden / 4) {
+#pragma unroll 8
+    for (int q = q0; q < q1; q++) s += reinterpret_cast<const f32x4*>(a.part + ((size_t)q * 2 + (q == p)) * a.hidden)[c];
   }
-  if (c >= a.hidden / 4) return;
-  f32x4 s = reinterpret_cast<const f32x4*>(a.part + ((size_t)p * 2 + 1) * a.hidden)[c];
-  for (int q = p + 1; q <= lo; q++) s += reinterpret_cast<const f32x4*>(a.part + ((size_t)q * 2) * a.hidden)[c];
+  if (wave > 0) red[wave - 1][lane] = s;
+  __syncthreads();
+  if (wave > 0 || c >= a.hidden / 4) return;
+#pragma unroll
+  for (int w = 0; w < 3; w++) s += red[w][lane];
   const float v[4] = {s[0], s[1], s[2], s[3]};
   put_row<4>(a.dtable + (size_t)key * a.hidden + (size_t)c * 4, v, a.scale, a.accumulate);
 }
@@ -262,29 +345,29 @@ int lanes_log(int chunks) {
   return l;
 }
 
-constexpr int PIECE = 16;          // tokens of a piece
+constexpr long FEW_WGS = 2048;             // workgroups of a lookup with one token a lane: all on the chip at once
+constexpr long FILL_BYTES = 32 << 10;      // of the table, for each workgroup that clears
 
 size_t align_up(size_t v) { return (v + 255) & ~(size_t)255; }
 
 struct Plan {
-  int pieces, blocks, passes, digit;
-  size_t key[2], tok[2], hist, part, bytes;
+  int pieces, span, span_log;
+  size_t list_key, list_tok, key, tok, start, part, bytes;
 };
+// Rows of the table that a workgroup of the sort owns: about 128 workgroups, which each look at all ids
 Plan plan_of(const gx_embed_cfg& c) {
   Plan p;
   p.pieces = cdiv(c.tokens, PIECE);
-  p.blocks = cdiv(c.tokens, TPB);
-  int bits = 1;
-  while (((unsigned)c.rows >> bits) != 0) bits++;              // keys are 0 .. rows
-  p.passes = cdiv(bits, DIGIT_BITS);
-  p.digit = cdiv(bits, p.passes);
+  p.span_log = 6;
+  while ((1 << p.span_log) < MAX_SPAN && ((long)128 << p.span_log) < c.rows) p.span_log++;
+  p.span = 1 << p.span_log;
   size_t at = 0;
   auto take = [&](size_t n) { const size_t was = at; at += align_up(n); return was; };
-  for (int k = 0; k < 2; k++) {
-    p.key[k] = take((size_t)c.tokens * 4);
-    p.tok[k] = take((size_t)c.tokens * 4);
-  }
-  p.hist = take((size_t)p.blocks * DIGITS * 4);
+  p.list_key = take((size_t)c.tokens * 4);
+  p.list_tok = take((size_t)c.tokens * 4);
+  p.key = take((size_t)c.tokens * 4);
+  p.tok = take((size_t)c.tokens * 4);
+  p.start = take(((size_t)c.rows + 1) * 4);
   p.part = take((size_t)p.pieces * 2 * c.hidden * 4);
   p.bytes = at;
   return p;
@@ -302,7 +385,8 @@ gx_status check(const gx_embed_cfg* c) {
   return GX_OK;
 }
 bool ids_misaligned(const gx_embed_cfg& c, const void* ids) { return reinterpret_cast<uintptr_t>(ids) % c.id_bytes != 0; }
-Ids ids_of(const gx_embed_cfg& c, const void* ids) { return Ids{ids, c.id_bytes, (long)c.first_row, (long)c.rows}; }
+template <typename I>
+Ids<I> ids_of(const gx_embed_cfg& c, const void* ids) { return Ids<I>{static_cast<const I*>(ids), (long)c.first_row, (long)c.rows}; }
 
 gx_status launched() { return hipGetLastError() == hipSuccess ? GX_OK : GX_ERR_LAUNCH; }
 
@@ -321,14 +405,22 @@ gx_status gx_embed_fwd(const gx_embed_cfg* cfg, const void* table, const void* i
   if (!device_is_gfx950()) return GX_ERR_ARCH;
   const bool bf = cfg->dtype == GX_BF16;
   const int chunks = cfg->hidden / (bf ? 8 : 4), log = lanes_log(chunks);
-  const dim3 grid(cdiv(cfg->tokens, 256 >> log), 1);
+  const long wgs = cdiv(cfg->tokens, 256 >> log);              // with one token a lane
+  const bool few = wgs * cdiv(chunks, 256) < FEW_WGS;
+  const dim3 grid(few ? (unsigned)wgs : (unsigned)cdiv(cfg->tokens, (256 >> log) * 4), few ? cdiv(chunks, 1 << log) : 1);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (bf)
-    hipLaunchKernelGGL((embed_fwd_kernel<bf16>), grid, dim3(256), 0, s, static_cast<const bf16*>(table), ids_of(*cfg, ids),
-                       static_cast<bf16*>(y), cfg->tokens, cfg->hidden, log, cfg->scale);
-  else
-    hipLaunchKernelGGL((embed_fwd_kernel<float>), grid, dim3(256), 0, s, static_cast<const float*>(table), ids_of(*cfg, ids),
-                       static_cast<float*>(y), cfg->tokens, cfg->hidden, log, cfg->scale);
+  auto go = [&](auto type, auto id) {
+    typedef decltype(type) T;
+    typedef decltype(id) I;
+    if (few)
+      hipLaunchKernelGGL((embed_fwd_kernel<T, I, 1>), grid, dim3(256), 0, s, static_cast<const T*>(table), ids_of<I>(*cfg, ids),
+                         static_cast<T*>(y), cfg->tokens, cfg->hidden, log, cfg->scale);
+    else
+      hipLaunchKernelGGL((embed_fwd_kernel<T, I, 4>), grid, dim3(256), 0, s, static_cast<const T*>(table), ids_of<I>(*cfg, ids),
+                         static_cast<T*>(y), cfg->tokens, cfg->hidden, log, cfg->scale);
+  };
+  if (cfg->id_bytes == 8) bf ? go(bf16(), 0l) : go(0.f, 0l);
+  else bf ? go(bf16(), 0) : go(0.f, 0);
   return launched();
 }
 
@@ -336,40 +428,33 @@ gx_status gx_embed_bwd(const gx_embed_cfg* cfg, const void* ids, const void* dy,
                        void* hip_stream) {
   const gx_status st = check(cfg);
   if (st != GX_OK) return st;
-  if (!dtable || (cfg->tokens > 0 && (!ids || !dy || !workspace))) return GX_ERR_NULL;
+  if (!dtable || !workspace || (cfg->tokens > 0 && (!ids || !dy))) return GX_ERR_NULL;
   if (misaligned(dtable) || ids_misaligned(*cfg, ids) || misaligned(dy) || misaligned(workspace)) return GX_ERR_ALIGN;
   if (!device_is_gfx950()) return GX_ERR_ARCH;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const bool accumulate = cfg->flags & GX_ACCUM_WGRAD, bf = cfg->dtype == GX_BF16;
-  if (!accumulate) {
-    const size_t n = (size_t)cfg->rows * cfg->hidden / 4;
-    const size_t wgs = (n + 256 * 4 - 1) / (256 * 4);
-    hipLaunchKernelGGL(embed_zero_kernel, dim3((unsigned)(wgs > 65536 ? 65536 : wgs)), dim3(256), 0, s,
-                       reinterpret_cast<f32x4*>(dtable), n);
-  }
-  if (cfg->tokens == 0) return launched();
   const Plan p = plan_of(*cfg);
   char* ws = static_cast<char*>(workspace);
   auto u32 = [&](size_t at) { return reinterpret_cast<unsigned*>(ws + at); };
-  SortArgs a{ids_of(*cfg, ids), cfg->pad_id < 0 ? -1 : (long)(cfg->pad_id - cfg->first_row), cfg->tokens, 0, (1 << p.digit) - 1,
-             nullptr, nullptr, nullptr, nullptr, u32(p.hist)};
-  for (int k = 0; k < p.passes; k++) {
-    a.shift = k * p.digit;
-    a.key_in = k ? u32(p.key[(k - 1) & 1]) : nullptr;
-    a.tok_in = k ? u32(p.tok[(k - 1) & 1]) : nullptr;
-    a.key_out = u32(p.key[k & 1]);
-    a.tok_out = u32(p.tok[k & 1]);
-    hipLaunchKernelGGL(embed_count_kernel, dim3(p.blocks), dim3(SORT_THREADS), 0, s, a);
-    hipLaunchKernelGGL(embed_place_kernel, dim3(p.blocks), dim3(SORT_THREADS), 0, s, a, p.blocks);
+  auto sort = [&](auto id) {
+    typedef decltype(id) I;
+    const SortArgs<I> a{ids_of<I>(*cfg, ids), cfg->pad_id < 0 ? -1 : (long)(cfg->pad_id - cfg->first_row), cfg->tokens, p.span,
+                        p.span_log, u32(p.list_key), u32(p.list_tok), u32(p.key), u32(p.tok), u32(p.start)};
+    hipLaunchKernelGGL(embed_sort_kernel<I>, dim3(cdiv(cfg->rows, p.span)), dim3(SORT_THREADS), 0, s, a);
+  };
+  cfg->id_bytes == 8 ? sort(0l) : sort(0);
+  SumArgs m{u32(p.key), u32(p.tok), u32(p.start), dy, dtable, reinterpret_cast<float*>(ws + p.part), cfg->tokens, cfg->hidden, cfg->rows,
+            p.pieces, accumulate, 0, 0, cfg->scale};
+  const int chunks = cfg->hidden / (bf ? 8 : 4), log = lanes_log(chunks), cols = cdiv(chunks, 1 << log);
+  m.sum_blocks = cdiv(p.pieces, 256 >> log) * cols;
+  m.fill_rows = cdiv(FILL_BYTES, (long)cfg->hidden * 4);
+  const dim3 grid(m.sum_blocks + (accumulate ? 0 : cdiv(cfg->rows, m.fill_rows)));
+  if (grid.x > 0) {
+    if (bf) hipLaunchKernelGGL((embed_sum_kernel<bf16>), grid, dim3(256), 0, s, m, log, cols);
+    else hipLaunchKernelGGL((embed_sum_kernel<float>), grid, dim3(256), 0, s, m, log, cols);
   }
-  SumArgs m{a.key_out, a.tok_out, dy, dtable, reinterpret_cast<float*>(ws + p.part), cfg->tokens, cfg->hidden, cfg->rows, PIECE,
-            p.pieces, accumulate, cfg->scale};
-  const int chunks = cfg->hidden / (bf ? 8 : 4), log = lanes_log(chunks);
-  const dim3 grid(cdiv(p.pieces, 256 >> log), cdiv(chunks, 1 << log));
-  if (bf) hipLaunchKernelGGL((embed_sum_kernel<bf16>), grid, dim3(256), 0, s, m, log);
-  else hipLaunchKernelGGL((embed_sum_kernel<float>), grid, dim3(256), 0, s, m, log);
   if (p.pieces > 1)
-    hipLaunchKernelGGL(embed_join_kernel, dim3(p.pieces, cdiv(cfg->hidden / 4, 256)), dim3(256), 0, s, m);
+    hipLaunchKernelGGL(embed_join_kernel, dim3(p.pieces, cdiv(cfg->hidden / 4, 64)), dim3(256), 0, s, m);
   return launched();
 }
 
