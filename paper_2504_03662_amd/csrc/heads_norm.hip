@@ -5,8 +5,9 @@
 // neighbouring pairs, 8 c and 8 c + rot / 2 as well: either chunk then turns in itself), so that a rotation needs no other lane's
 // columns; in the rest two neighbouring chunks.  LPH lanes (a power of two) share a head, 64 / LPH heads a wavefront; the
 // mean of squares is a sum over LPH lanes.  A lane's columns are the same for every head and token it meets: the gain
-// stays in registers, the token's cosines and sines are read once for all of its heads, and the gain's gradient is a sum in
-// registers, added up over lanes, wavefronts and blocks in a fixed order at the end.
+// stays in registers, the token's cosines and sines are read once for all the heads that a wavefront takes of it, and the gain's
+// gradient is a sum in registers, added up over lanes, wavefronts and blocks in a fixed order at the end.
+// A unit of work is 64 / LPH heads of a token; a wavefront takes a run of units, and queries and keys get workgroups in proportion.
 #include "../../include/gx.h"
 #include "gx_kernels.h"
 
@@ -18,20 +19,29 @@ bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) !=
 
 typedef float Chunk[8];
 
-template <typename T> GX_DEVINL void load8(const T* p, Chunk& o);
-template <> GX_DEVINL void load8<bf16>(const bf16* p, Chunk& o) {
-  const bf16x8 v = *reinterpret_cast<const bf16x8*>(p);
+// Eight columns as they lie in memory
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16> {
+  bf16x8 v;
+  GX_DEVINL void load(const bf16* p) { v = *reinterpret_cast<const bf16x8*>(p); }
+  GX_DEVINL void zero() { v = bf16x8{}; }
+  GX_DEVINL void widen(Chunk& o) const {
 #pragma unroll
-  for (int e = 0; e < 8; e++) o[e] = (float)v[e];
-}
-template <> GX_DEVINL void load8<float>(const float* p, Chunk& o) {
-#pragma unroll
-  for (int h = 0; h < 2; h++) {
-    const f32x4 v = reinterpret_cast<const f32x4*>(p)[h];
-#pragma unroll
-    for (int e = 0; e < 4; e++) o[4 * h + e] = v[e];
+    for (int e = 0; e < 8; e++) o[e] = (float)v[e];
   }
-}
+};
+template <> struct Raw8<float> {
+  f32x4 v[2];
+  GX_DEVINL void load(const float* p) {
+#pragma unroll
+    for (int h = 0; h < 2; h++) v[h] = reinterpret_cast<const f32x4*>(p)[h];
+  }
+  GX_DEVINL void zero() { v[0] = v[1] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+  GX_DEVINL void widen(Chunk& o) const {
+#pragma unroll
+    for (int e = 0; e < 8; e++) o[e] = v[e >> 2][e & 3];
+  }
+};
 GX_DEVINL void store8(bf16* p, const Chunk& x) {
   bf16x8 v;
 #pragma unroll
@@ -53,6 +63,8 @@ struct Side {
   const int* pos;
   float* part;                     // backward: partial gain gradients, [blocks of this side][head_dim], or null
   int len, heads, blocks;          // blocks: how many of the launch work on this side
+  int per_token;                   // units of a token
+  long units;
 };
 struct NormArgs {
   Side side[2];                    // queries, keys: the first side[0].blocks blocks take queries
@@ -89,13 +101,16 @@ struct Place {
 
 // The angles of a lane's columns at a token.  PAIRS: four for each chunk; else the same eight for both.
 struct Angles {
-  Chunk c, s;
+  f32x4 c[2], s[2];
   template <bool PAIRS>
   GX_DEVINL void load(const NormArgs& a, const Place& p, int pos) {
     if (!p.turned) return;
-    if (pos < 0 || pos >= a.max_pos) {
+    const bool there = pos >= 0 && pos < a.max_pos;
+    if (!there) {
 #pragma unroll
-      for (int e = 0; e < 8; e++) c[e] = s[e] = __builtin_nanf("");
+      for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) c[h][e] = s[h][e] = __builtin_nanf("");
       return;
     }
     const float* cr = a.cos + (size_t)pos * (a.rot / 2);
@@ -103,12 +118,8 @@ struct Angles {
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       const int at = PAIRS ? (h ? p.ang_b : p.ang_a) : p.ang_a + 4 * h;
-      const f32x4 x = *reinterpret_cast<const f32x4*>(cr + at), y = *reinterpret_cast<const f32x4*>(sr + at);
-#pragma unroll
-      for (int e = 0; e < 4; e++) {
-        c[4 * h + e] = x[e];
-        s[4 * h + e] = y[e];
-      }
+      c[h] = *reinterpret_cast<const f32x4*>(cr + at);
+      s[h] = *reinterpret_cast<const f32x4*>(sr + at);
     }
   }
   // x -> R x, or with BACK R^T x
@@ -117,12 +128,12 @@ struct Angles {
     if (PAIRS) {
 #pragma unroll
       for (int i = 0; i < 4; i++) {
-        one<BACK>(a[2 * i], a[2 * i + 1], c[i], s[i]);
-        one<BACK>(b[2 * i], b[2 * i + 1], c[4 + i], s[4 + i]);
+        one<BACK>(a[2 * i], a[2 * i + 1], c[0][i], s[0][i]);
+        one<BACK>(b[2 * i], b[2 * i + 1], c[1][i], s[1][i]);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; i++) one<BACK>(a[i], b[i], c[i], s[i]);
+      for (int i = 0; i < 8; i++) one<BACK>(a[i], b[i], c[i >> 2][i & 3], s[i >> 2][i & 3]);
     }
   }
   template <bool BACK>
@@ -139,13 +150,16 @@ GX_DEVINL float head_sum(float v, int lph) {
 }
 
 template <typename T>
-GX_DEVINL void load_pair(const char* head, const Place& p, Chunk& a, Chunk& b) {
-  const T* row = reinterpret_cast<const T*>(head);
-#pragma unroll
-  for (int e = 0; e < 8; e++) a[e] = b[e] = 0.f;
-  if (p.has_a) load8<T>(row + p.a, a);
-  if (p.has_b) load8<T>(row + p.b, b);
-}
+struct RawPair {
+  Raw8<T> a, b;
+  GX_DEVINL void load(const char* head, const Place& p) {
+    const T* row = reinterpret_cast<const T*>(head);
+    a.zero();
+    b.zero();
+    if (p.has_a) a.load(row + p.a);
+    if (p.has_b) b.load(row + p.b);
+  }
+};
 template <typename T>
 GX_DEVINL void store_pair(char* head, const Place& p, const Chunk& a, const Chunk& b) {
   T* row = reinterpret_cast<T*>(head);
@@ -153,13 +167,32 @@ GX_DEVINL void store_pair(char* head, const Place& p, const Chunk& a, const Chun
   if (p.has_b) store8(row + p.b, b);
 }
 
-// A wavefront takes tokens in a grid stride and goes over all heads of each.
+// What a wavefront works on next: unit after unit, token after token
+struct Cursor {
+  long t;
+  int b, i, hb;
+  GX_DEVINL void start(const Side& s, long u) {
+    t = u / s.per_token;
+    hb = (int)(u - t * s.per_token);
+    b = (int)(t / s.len);
+    i = (int)(t - (long)b * s.len);
+  }
+  GX_DEVINL void next(const Side& s) {
+    if (++hb < s.per_token) return;
+    hb = 0;
+    t++;
+    if (++i == s.len) {
+      i = 0;
+      b++;
+    }
+  }
+  GX_DEVINL long at(const Heads& x, int h) const { return b * x.batch + i * x.token + h * x.head; }
+};
+
+// A unit's loads are issued before the unit before it is worked on; its angles with them, for which the position has
+// been read one unit earlier still.
 template <typename T, bool PAIRS, bool BACK>
-__global__ void __launch_bounds__(256) heads_norm_kernel(NormArgs a) {
-  __shared__ float red[4][256];
-  const bool keys = (int)blockIdx.x >= a.side[0].blocks;
-  const Side& s = a.side[keys];
-  const int blk = blockIdx.x - (keys ? a.side[0].blocks : 0);
+GX_DEVINL void work_on(const NormArgs& a, const Side& s, int blk, float (&red)[4][256]) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lph = 1 << a.lph_log, sub = lane & (lph - 1), slot = lane >> a.lph_log, slots = 64 >> a.lph_log;
   const Place p = Place::of<PAIRS>(sub, a.dh, a.rot);
@@ -169,53 +202,87 @@ __global__ void __launch_bounds__(256) heads_norm_kernel(NormArgs a) {
     ga[e] = gb[e] = 1.f;
     sum_a[e] = sum_b[e] = 0.f;
   }
-  if (s.gain) load_pair<T>(static_cast<const char*>(s.gain), p, ga, gb);
+  const int w = blk * 4 + wave, waves = s.blocks * 4;
+  const long u0 = s.units * w / waves, u1 = s.units * (w + 1) / waves;
+  Cursor now;
+  now.start(s, u0 < s.units ? u0 : 0);
+  Cursor ahead = now;
+  auto pos_of = [&](const Cursor& c) { return s.pos ? s.pos[c.t] : c.i; };
+  RawPair<T> x, d;
+  Angles ang;
+  auto fetch = [&](const Cursor& c, int pos, RawPair<T>& xr, RawPair<T>& dr, Angles& an) {
+    const int h = min(c.hb * slots + slot, s.heads - 1);      // a lane without a head reads another one's
+    xr.load(s.x.p + c.at(s.x, h), p);
+    if (BACK) dr.load(s.dy.p + c.at(s.dy, h), p);
+    an.load<PAIRS>(a, p, pos);
+  };
+  fetch(now, pos_of(now), x, d, ang);
+  if (s.gain) {
+    RawPair<T> g;
+    g.load(static_cast<const char*>(s.gain), p);
+    g.a.widen(ga);
+    g.b.widen(gb);
+  }
   const float inv = 1.0f / (float)a.dh;
-  const long tokens = (long)a.batch * s.len;
-  for (long t = (long)blk * 4 + wave; t < tokens; t += (long)s.blocks * 4) {
-    const long b = t / s.len, i = t - b * s.len;
-    Angles ang;
-    ang.load<PAIRS>(a, p, s.pos ? s.pos[t] : (int)i);
-    for (int h = slot; h < s.heads; h += slots) {
-      Chunk xa, xb;
-      load_pair<T>(s.x.p + b * s.x.batch + i * s.x.token + h * s.x.head, p, xa, xb);
-      float q = 0.f;
+  if (u0 + 1 < u1) ahead.next(s);
+  int pos = pos_of(ahead);
+  for (long u = u0; u < u1; u++) {
+    RawPair<T> xn = x, dn = d;
+    Angles an = ang;
+    const Cursor then = ahead;
+    if (u + 1 < u1) {
+      fetch(ahead, pos, xn, dn, an);
+      if (u + 2 < u1) ahead.next(s);
+      pos = pos_of(ahead);
+    }
+    const int h = now.hb * slots + slot;
+    const bool live = h < s.heads;                    // the same for all lanes of a head
+    Chunk xa, xb;
+    x.a.widen(xa);
+    x.b.widen(xb);
+    float q = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; e++) q = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], q));
-      const float r = rsqrtf(fmaf(head_sum(q, lph), inv, a.eps));
-      char* const out = s.out.p + b * s.out.batch + i * s.out.token + h * s.out.head;
-      if (!BACK) {
+    for (int e = 0; e < 8; e++) q = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], q));
+    const float r = rsqrtf(fmaf(head_sum(q, lph), inv, a.eps));
+    char* const out = s.out.p + now.at(s.out, h);
+    if (!BACK) {
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-          xa[e] *= r * ga[e];
-          xb[e] *= r * gb[e];
-        }
-        if (p.turned) ang.turn<PAIRS, false>(xa, xb);
-        store_pair<T>(out, p, xa, xb);
-      } else {
-        Chunk da, db;
-        load_pair<T>(s.dy.p + b * s.dy.batch + i * s.dy.token + h * s.dy.head, p, da, db);
-        if (p.turned) ang.turn<PAIRS, true>(da, db);
-        float m = 0.f;
+      for (int e = 0; e < 8; e++) {
+        xa[e] *= r * ga[e];
+        xb[e] *= r * gb[e];
+      }
+      if (p.turned) ang.turn<PAIRS, false>(xa, xb);
+      if (live) store_pair<T>(out, p, xa, xb);
+    } else {
+      Chunk da, db;
+      d.a.widen(da);
+      d.b.widen(db);
+      if (p.turned) ang.turn<PAIRS, true>(da, db);
+      float m = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-          xa[e] *= r;                                 // u
-          xb[e] *= r;
+      for (int e = 0; e < 8; e++) {
+        xa[e] *= r;                                   // u
+        xb[e] *= r;
+        if (live) {
           sum_a[e] = fmaf(da[e], xa[e], sum_a[e]);
           sum_b[e] = fmaf(db[e], xb[e], sum_b[e]);
-          da[e] *= ga[e];                             // the gradient reaching u
-          db[e] *= gb[e];
-          m = fmaf(da[e], xa[e], fmaf(db[e], xb[e], m));
         }
-        m = head_sum(m, lph) * inv;
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          da[e] = r * fmaf(-xa[e], m, da[e]);
-          db[e] = r * fmaf(-xb[e], m, db[e]);
-        }
-        store_pair<T>(out, p, da, db);
+        da[e] *= ga[e];                               // the gradient reaching u
+        db[e] *= gb[e];
+        m = fmaf(da[e], xa[e], fmaf(db[e], xb[e], m));
       }
+      m = head_sum(m, lph) * inv;
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        da[e] = r * fmaf(-xa[e], m, da[e]);
+        db[e] = r * fmaf(-xb[e], m, db[e]);
+      }
+      if (live) store_pair<T>(out, p, da, db);
     }
+    x = xn;
+    d = dn;
+    ang = an;
+    now = then;
   }
   if (BACK && s.part) {
 #pragma unroll
@@ -237,14 +304,72 @@ __global__ void __launch_bounds__(256) heads_norm_kernel(NormArgs a) {
   }
 }
 
-// ------------------------------------------------------------------------------- host
-constexpr int MAX_BLOCKS = 1024;           // of a side, backward: as many partial rows of the gain's gradient
+// Queries first; two calls, so that neither side's record is picked by an index (and copied to memory for that)
+template <typename T, bool PAIRS, bool BACK>
+__global__ void __launch_bounds__(256) heads_norm_kernel(NormArgs a) {
+  __shared__ float red[4][256];
+  const int blk = blockIdx.x;
+  if (blk < a.side[0].blocks) work_on<T, PAIRS, BACK>(a, a.side[0], blk, red);
+  else work_on<T, PAIRS, BACK>(a, a.side[1], blk - a.side[0].blocks, red);
+}
 
-int blocks_of(const gx_heads_norm_cfg& c, bool keys, bool backward) {
-  const long len = keys ? c.k_len : c.q_len, heads = keys ? c.k_heads : c.q_heads;
-  if (len == 0 || heads == 0) return 0;
-  const long wgs = ((long)c.batch * len + 3) / 4, most = backward ? MAX_BLOCKS : 65536;
-  return (int)(wgs < most ? wgs : most);
+// Sum of a side's partial rows, in order: 8 lanes of 4 columns, 32 runs of rows
+struct GainArgs {
+  struct { const float* part; float* out; int blocks; } side[2];
+  int dh, accumulate;
+};
+__global__ void __launch_bounds__(256) heads_gain_kernel(GainArgs a) {
+  __shared__ f32x4 red[32][8];
+  const float* part = blockIdx.y ? a.side[1].part : a.side[0].part;
+  float* out = blockIdx.y ? a.side[1].out : a.side[0].out;
+  const int blocks = blockIdx.y ? a.side[1].blocks : a.side[0].blocks;
+  const int x = threadIdx.x & 7, y = threadIdx.x >> 3, c = blockIdx.x * 32 + x * 4;
+  if (!out) return;
+  const int per = (blocks + 31) / 32, r0 = min(y * per, blocks), r1 = min(r0 + per, blocks);
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (c < a.dh) {
+#pragma unroll 8
+    for (int r = r0; r < r1; r++) s += *reinterpret_cast<const f32x4*>(part + (size_t)r * a.dh + c);
+  }
+  red[y][x] = s;
+  __syncthreads();
+  if (y > 0 || c >= a.dh) return;
+#pragma unroll
+  for (int k = 1; k < 32; k++) s += red[k][x];
+  f32x4* o = reinterpret_cast<f32x4*>(out + c);
+  if (a.accumulate) s += *o;
+  *o = s;
+}
+
+// ------------------------------------------------------------------------------- host
+// Workgroups of a pass with more units than they have wavefronts (backward: as many partial rows of the gains' gradients).  Two to
+// four wavefronts per SIMD, each with the next unit's loads in flight, are enough; more of them have shorter runs, and read a
+// token's angles more often.  Forward and backward, us, 4096 tokens of 40 heads of 128 (bf16) / 3003 of 32 of 64 (fp32): 1024 and 512
+// workgroups 58.6 / 35.1, 2048 and 512 59.2 / 36.1, 2560 and 640 57.3 / 39.3, 4096 and 384 66.2 / 39.1, 2560 and 256 75.9 / 37.4,
+// 5120 and 1536 67.1 / 43.2.  Without the loads ahead of the unit before, 2048 and 1024: 81.9 / 38.9.
+constexpr int FWD_BLOCKS = 1024, BACK_BLOCKS = 512;
+
+struct Shares {
+  int lph_log, per_token[2], blocks[2];
+  long units[2];
+};
+Shares shares_of(const gx_heads_norm_cfg& c, bool backward) {
+  Shares l = {};
+  const int lanes = c.rot_dim / 16 + cdiv(c.head_dim - c.rot_dim, 16);
+  while ((1 << l.lph_log) < lanes) l.lph_log++;
+  for (int k = 0; k < 2; k++) {
+    l.per_token[k] = cdiv(k ? c.k_heads : c.q_heads, 64 >> l.lph_log);
+    l.units[k] = (long)c.batch * (k ? c.k_len : c.q_len) * l.per_token[k];
+  }
+  const long all = l.units[0] + l.units[1];
+  // one unit a wavefront while all of them find a place together; then runs of units, which read a token's angles once
+  const long most = backward ? BACK_BLOCKS : FWD_BLOCKS;
+  for (int k = 0; k < 2; k++) {
+    if (l.units[k] == 0) continue;
+    const long one_each = (l.units[k] + 3) / 4, share = (most * l.units[k] + all - 1) / all;
+    l.blocks[k] = (int)(one_each < share ? one_each : share);
+  }
+  return l;
 }
 
 gx_status check(const gx_heads_norm_cfg* c) {
@@ -292,17 +417,21 @@ gx_status run(const gx_heads_norm_cfg* c, const gx_heads_norm_in* in, const gx_h
     if (!a.cos || !a.sin) return GX_ERR_NULL;
     if (misaligned(a.cos) || misaligned(a.sin)) return GX_ERR_ALIGN;
   }
-  const int lanes = c->rot_dim / 16 + cdiv(c->head_dim - c->rot_dim, 16);
-  while ((1 << a.lph_log) < lanes) a.lph_log++;
-  FinishSeg seg[2];
-  int nseg = 0;
+  const Shares l = shares_of(*c, backward);
+  a.lph_log = l.lph_log;
+  GainArgs gains = {};
+  gains.dh = c->head_dim;
+  gains.accumulate = (c->flags & GX_ACCUM_WGRAD) != 0;
+  bool any_gain = false;
   float* part = static_cast<float*>(workspace);
   for (int k = 0; k < 2; k++) {
     Side& s = a.side[k];
     const gx_heads& x = k ? in->k : in->q;
     s.len = k ? c->k_len : c->q_len;
     s.heads = k ? c->k_heads : c->q_heads;
-    s.blocks = blocks_of(*c, k, backward);
+    s.blocks = l.blocks[k];
+    s.per_token = l.per_token[k];
+    s.units = l.units[k];
     if (s.blocks == 0) continue;
     bad = check_heads(&x, c->batch, s.len, s.heads, c->head_dim, e, false);
     if (bad == GX_OK) bad = check_heads(out[k], c->batch, s.len, s.heads, c->head_dim, e, true);
@@ -319,7 +448,8 @@ gx_status run(const gx_heads_norm_cfg* c, const gx_heads_norm_in* in, const gx_h
       if (misaligned(dgain[k]) || misaligned(workspace)) return GX_ERR_ALIGN;
       s.part = part;
       part += (size_t)s.blocks * c->head_dim;
-      seg[nseg++] = FinishSeg{s.part, dgain[k], s.blocks, c->head_dim, (c->flags & GX_ACCUM_WGRAD) != 0, 0};
+      gains.side[k] = {s.part, dgain[k], s.blocks};
+      any_gain = true;
     }
   }
   if (!device_is_gfx950()) return GX_ERR_ARCH;
@@ -335,8 +465,8 @@ gx_status run(const gx_heads_norm_cfg* c, const gx_heads_norm_in* in, const gx_h
     else pairs ? go(heads_norm_kernel<float, true, false>) : go(heads_norm_kernel<float, false, false>);
   }
   if (hipGetLastError() != hipSuccess) return GX_ERR_LAUNCH;
-  if (nseg > 0 && colsum_finish(seg, nseg, st) != hipSuccess) return GX_ERR_LAUNCH;
-  return GX_OK;
+  if (any_gain) hipLaunchKernelGGL(heads_gain_kernel, dim3(cdiv(c->head_dim, 32), 2), dim3(256), 0, st, gains);
+  return hipGetLastError() == hipSuccess ? GX_OK : GX_ERR_LAUNCH;
 }
 
 }  // namespace
@@ -345,7 +475,8 @@ extern "C" {
 
 size_t gx_heads_norm_workspace_bytes(const gx_heads_norm_cfg* cfg) {
   if (check(cfg) != GX_OK) return 0;
-  return (size_t)(blocks_of(*cfg, false, true) + blocks_of(*cfg, true, true)) * cfg->head_dim * 4;
+  const Shares l = shares_of(*cfg, true);
+  return (size_t)(l.blocks[0] + l.blocks[1]) * cfg->head_dim * 4;
 }
 
 gx_status gx_heads_norm_fwd(const gx_heads_norm_cfg* cfg, const gx_heads_norm_in* in, const gx_heads* q_out,
