@@ -2,6 +2,14 @@
 // dimension, inside a namespace of its own, with GX_ATTN_DH defined.
 #include "attn_bf16_tiles.h"
 
+// A value that is the same in all lanes, in a scalar register whatever the compiler thinks (a descriptor in vector registers makes
+// it wrap every load that uses it in a loop)
+GX_DEVINL unsigned uniform(unsigned x) { return __builtin_amdgcn_readfirstlane(x); }
+GX_DEVINL const char* uniform(const char* p) {
+  const unsigned long u = (unsigned long)p;
+  return reinterpret_cast<const char*>((unsigned long)uniform((unsigned)u) | ((unsigned long)uniform((unsigned)(u >> 32)) << 32));
+}
+
 // ------------------------------------------------------------------------------- keys
 // Tiles of ROWS keys of K or V.  A tile has a buffer descriptor of its own (64-bit base, so that a cache may be of any
 // length) that ends with the keys there are: rows beyond read as zeros.  Keys whose mask bit is clear are not read either: their
@@ -31,7 +39,7 @@ struct KeyTiles {
   struct Tile { const char* p; unsigned bytes; };
   GX_DEVINL Tile tile(int t) const {
     const int left = len - t * ROWS, n = left < 0 ? 0 : left < ROWS ? left : ROWS;
-    return Tile{n > 0 ? base + (long)t * tile_bytes : base, (unsigned)n * row_bytes};
+    return Tile{uniform(n > 0 ? base + (long)t * tile_bytes : base), uniform((unsigned)n * row_bytes)};
   }
   GX_DEVINL void issue(const Tile& x, char* dst, int wave, int i, bool on) const {
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(x.p), 0, x.bytes, 0x00020000);
@@ -620,40 +628,55 @@ GX_DEVINL float unpack_p(unsigned w, int second) {
   return __builtin_bit_cast(float, second ? (w & 0xFFFF0000u) >> 2 : (w & 0xFFFFu) << 14);
 }
 
-// Tiles of 32 rows of a group of heads: a tile's descriptor starts at its first query, a lane's offset follows from
-// the head at which the tile starts.
+// Tiles of 32 rows of a group of heads, one after the other: a tile's descriptor starts at its first query, a lane's offset follows
+// from the head at which the tile starts (always the first one where the group divides 32).  What moves from tile to tile is
+// kept in scalars.
 template <int NW>
 struct RowTiles {
   static constexpr int RPI = 64 / CPR, PER = KV_BI / RPI / NW;
   static_assert(PER >= 1, "tile too small for the workgroup");
-  const char* base;
-  long token_bytes;
+  const char* at;                  // first query of the next tile
+  long step, token_bytes;          // to the first query of the tile after it; of one query
   unsigned head_bytes;
-  unsigned wrap;                   // from head `group` of a query to head 0 of the next one, modulo 2^32
-  unsigned off[PER];
-  int head[PER], group, rows;
-  GX_DEVINL void init(const bf16* p, const HeadStrides& s, int g, int n, int wave, int lane) {
-    base = reinterpret_cast<const char*>(p);
+  int group, h0, dh, left;         // head at which the next tile starts, and by how much that moves; rows from there on
+  unsigned off[PER], off_wrapped[PER];   // modulo 2^32, without the tile's first head; wrapped: past the query's last head
+  int head[PER], row0;
+  GX_DEVINL void init(const bf16* p, const HeadStrides& s, int g, int rows, int t, int wave, int lane) {
     token_bytes = s.t * 2;
-    head_bytes = (unsigned)(s.h * 2);
-    wrap = (unsigned)token_bytes - (unsigned)g * head_bytes;
+    head_bytes = uniform((unsigned)(s.h * 2));
     group = g;
-    rows = n;
+    const unsigned q0 = uniform((unsigned)(t * KV_BI) / (unsigned)g), dq = uniform((unsigned)KV_BI / (unsigned)g);
+    h0 = t * KV_BI - (int)q0 * g;
+    dh = KV_BI - (int)dq * g;
+    step = (long)dq * token_bytes;
+    at = uniform(reinterpret_cast<const char*>(p) + (long)q0 * token_bytes);
+    left = rows - t * KV_BI;
+    row0 = RPI * wave * PER + lane / CPR;
 #pragma unroll
     for (int i = 0; i < PER; i++) {
-      const int r = RPI * (wave * PER + i) + lane / CPR, c = (lane % CPR) ^ swz(r);
+      const int r = row0 + RPI * i, c = (lane % CPR) ^ swz(r);
       const unsigned q = (unsigned)r / (unsigned)g;
-      head[i] = r - q * g;
+      head[i] = r - (int)q * g;
       off[i] = q * (unsigned)token_bytes + head[i] * head_bytes + (unsigned)(c * 16);
+      off_wrapped[i] = off[i] + (unsigned)token_bytes - (unsigned)g * head_bytes;
     }
   }
-  // instruction i of tile t, which starts at head h0 of query q0
-  GX_DEVINL void issue(int t, int q0, int h0, char* dst, int wave, int lane, int i) const {
-    const __amdgpu_buffer_rsrc_t rs =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base + (long)q0 * token_bytes), 0, 0x7FFFFFFFu, 0x00020000);
-    const int r = t * KV_BI + RPI * (wave * PER + i) + lane / CPR;
-    const unsigned at = r < rows ? off[i] + (unsigned)h0 * head_bytes + (head[i] + h0 >= group ? wrap : 0u) : OOB;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_ptr)(dst + (wave * PER + i) * 1024), 16, at, 0, 0, 0);
+  // instruction i of the next tile
+  GX_DEVINL void issue(char* dst, int wave, int i) const {
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, 0x7FFFFFFFu, 0x00020000);
+    unsigned o = (head[i] + h0 >= group ? off_wrapped[i] : off[i]) + (unsigned)h0 * head_bytes;
+    asm volatile("" : "+v"(o));    // selected, not branched around
+    o = row0 + RPI * i < left ? o : OOB;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_ptr)(dst + (wave * PER + i) * 1024), 16, o, 0, 0, 0);
+  }
+  GX_DEVINL void next() {
+    left -= KV_BI;
+    at += step;
+    h0 += dh;
+    if (h0 >= group) {
+      h0 -= group;
+      at += token_bytes;
+    }
   }
 };
 
@@ -708,47 +731,29 @@ __global__ void __launch_bounds__(64 * KV_NW, DH == 64 ? 3 : 2) cross_dkv_kernel
   const float* const aux = (wave == 0 ? a.lrow : a.drow) + (long)kp * a.rows;
   RowTiles<KV_NW> srcq, srcdo;
   constexpr int PER = RowTiles<KV_NW>::PER, NREQ = 2 * PER + 1;
-  srcq.init(static_cast<const bf16*>(a.q) + pair_offset(a.sq, b, kh * a.group), a.sq, a.group, a.rows, wave, lane);
-  srcdo.init(static_cast<const bf16*>(a.d_o) + pair_offset(a.sdo, b, kh * a.group), a.sdo, a.group, a.rows, wave, lane);
-  // where tile t starts: the next tiles to be requested are followed, not divided for
-  struct At { int t, q, h; };
-  const int dq = KV_BI / a.group, dh = KV_BI - dq * a.group;
-  auto at_tile = [&](int t) {
-    const int q = (int)((unsigned)(t * KV_BI) / (unsigned)a.group);
-    return At{t, q, t * KV_BI - q * a.group};
-  };
-  auto next_tile = [&](At& x) __attribute__((always_inline)) {
-    x.t++;
-    x.q += dq;
-    x.h += dh;
-    if (x.h >= a.group) { x.h -= a.group; x.q++; }
-  };
+  srcq.init(static_cast<const bf16*>(a.q) + pair_offset(a.sq, b, kh * a.group), a.sq, a.group, a.rows, t0, wave, lane);
+  srcdo.init(static_cast<const bf16*>(a.d_o) + pair_offset(a.sdo, b, kh * a.group), a.sdo, a.group, a.rows, t0, wave, lane);
   auto q_slot = [&](int slot) { return smem + slot * KV_TILE; };
   auto do_slot = [&](int slot) { return smem + KV_OFF_DO + slot * KV_TILE; };
-  auto load_rows_of = [&](const RowTiles<KV_NW>& src, const At& x, char* dst) {
+  auto load_tile = [&](RowTiles<KV_NW>& src, char* dst) {
 #pragma unroll
-    for (int i = 0; i < PER; i++) src.issue(x.t, x.q, x.h, dst, wave, lane, i);
+    for (int i = 0; i < PER; i++) src.issue(dst, wave, i);
+    src.next();
   };
   auto aux_load = [&](int t, char* dst, bool on) {
     const int i = t * KV_BI + lane;
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(aux), 0, (unsigned)a.rows * 4u, 0x00020000);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_ptr)(on ? dst : smem + KV_OFF_SINK), 4,
-                                             (on && lane < KV_BI && i < a.rows) ? (unsigned)i * 4u : OOB, 0, 0, 0);
+    const unsigned o = on && lane < KV_BI && i < a.rows ? (unsigned)i * 4u : OOB;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_ptr)(on ? dst : smem + KV_OFF_SINK), 4, o, 0, 0, 0);
   };
-  At xq = at_tile(t0), xd = xq;
   const bool lse_or_d = wave < 2, d_too = wave == 1;
-  load_rows_of(srcq, xq, q_slot(0));
-  next_tile(xq);
-  load_rows_of(srcq, xq, q_slot(1));
-  next_tile(xq);
-  load_rows_of(srcdo, xd, do_slot(0));
-  next_tile(xd);
+  load_tile(srcq, q_slot(0));
+  load_tile(srcq, q_slot(1));
+  load_tile(srcdo, do_slot(0));
   aux_load(t0, wave == 0 ? do_slot(0) + KV_BI * ROWB : q_slot(0) + KV_BI * ROWB, lse_or_d);
   aux_load(t0 + 1, q_slot(1) + KV_BI * ROWB, d_too);
-  load_rows_of(srcq, xq, q_slot(2));
-  next_tile(xq);
-  load_rows_of(srcdo, xd, do_slot(1));
-  next_tile(xd);
+  load_tile(srcq, q_slot(2));
+  load_tile(srcdo, do_slot(1));
   aux_load(wave == 0 ? t0 + 1 : t0 + 2, (wave == 0 ? do_slot(1) : q_slot(2)) + KV_BI * ROWB, lse_or_d);
   // all that was requested before this phase has landed, and this wavefront is done with its reads
   auto meet = [&]() __attribute__((always_inline)) {
@@ -761,8 +766,8 @@ __global__ void __launch_bounds__(64 * KV_NW, DH == 64 ? 3 : 2) cross_dkv_kernel
   auto do_of = [&](int d) { return do_slot(ds + d < KV_NDO ? ds + d : ds + d - KV_NDO); };   // tile n + d, d in 0 .. 2
   // request i of phase n: this wavefront's share of Q(n + 3), of dO(n + 2), then D(n + 3) or lse(n + 2)
   auto request = [&](int n, int i) __attribute__((always_inline)) {
-    if (i < PER) srcq.issue(xq.t, xq.q, xq.h, q_of(3), wave, lane, i);
-    else if (i < 2 * PER) srcdo.issue(xd.t, xd.q, xd.h, do_of(2), wave, lane, i - PER);
+    if (i < PER) srcq.issue(q_of(3), wave, i);
+    else if (i < 2 * PER) srcdo.issue(do_of(2), wave, i - PER);
     else aux_load(wave == 0 ? n + 2 : n + 3, (wave == 0 ? do_of(2) : q_of(3)) + KV_BI * ROWB, lse_or_d);
   };
   auto request_all = [&](int n) __attribute__((always_inline)) {
@@ -772,8 +777,8 @@ __global__ void __launch_bounds__(64 * KV_NW, DH == 64 ? 3 : 2) cross_dkv_kernel
   auto advance = [&]() __attribute__((always_inline)) {
     qs = qs == KV_NQ - 1 ? 0 : qs + 1;
     ds = ds == KV_NDO - 1 ? 0 : ds + 1;
-    next_tile(xq);
-    next_tile(xd);
+    srcq.next();
+    srcdo.next();
   };
   struct CFrag { bf16x4 lo, hi; };
   constexpr int NPC = 2 * NDT, VD = 4, KD = 4;       // products with a transposed tile; fragments requested ahead
@@ -998,7 +1003,7 @@ hipError_t fwd(CrossArgs a, hipStream_t s) {
   if (shape == 3) e = mask ? go_fwd<1, 4, 32, true, true>(a, s) : go_fwd<1, 4, 32, true, false>(a, s);
   else if (mask) e = go_fwd<2, 2, 32, true, true>(a, s);
   else if (shape == 1) e = go_fwd<2, 2, 32, true, false>(a, s);
-  else e = go_fwd<4, 1, 64, false, false>(a, s);
+  else e = go_fwd<4, 1, 64, true, false>(a, s);
   return e != hipSuccess || a.splits == 1 ? e : cross_join_fwd(true, a, s);
 }
 
