@@ -604,20 +604,23 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, NQ * SPLIT == 4 ? 2 : 1) cros
 }
 
 // ------------------------------------------------------------------------------- backward: dK, dV
-// A workgroup owns 64 keys as 2 blocks of 32 and goes over the pair's rows (or, with a.splits > 1, a part of them) in tiles of
-// 32; each block belongs to a pair of wavefronts that split the work by output, as in the causal kernel: role V forms S = Q K^T,
-// the probabilities P and dV += P^T dO, role K dP = dO V^T, dS = P (dP - D) and dK += dS^T Q.  P crosses through LDS in 16
+// A workgroup owns 128 keys as 4 blocks of 32 and goes over the pair's rows (or, with a.splits > 1, a part of them) in tiles of
+// 64, two sub-tiles of 32; each block belongs to a pair of wavefronts that split the work by output, as in the causal kernel: role V
+// forms S = Q K^T, the probabilities P and dV += P^T dO, role K dP = dO V^T, dS = P (dP - D) and dK += dS^T Q, a tile behind.
+// A wavefront's stream mixes the first products of its next sub-tile with the vector work of the present one.  One
+// workgroup of 8 wavefronts fills a compute unit; wavefronts w and w + 4 share a SIMD, one of either role.
+// P crosses through LDS in 16
 // bits: 0 <= P < 2, so an fp32 P has two leading zero bits, and the next 16 (7 of the exponent, 9 of the mantissa, rounded) say P to
 // 2^-10 over the whole range: dS is then rounded to bf16 once, not twice.
 // Keys that do not count are columns of their own in S and dP and rows of their own in dK and dV: whatever
 // their lanes compute stays there, and zeros are stored.
-constexpr int KV_PAIRS = 2, KV_NW = 2 * KV_PAIRS, KV_BJ = 32 * KV_PAIRS, KV_BI = 32;
-constexpr int KV_NQ = 5, KV_NDO = 3;                         // Q tiles n-1 .. n+3, dO tiles n .. n+2
-constexpr int KV_TILE = KV_BI * ROWB + 256;                  // rows of Q or dO | their D or lse (64 lanes' worth)
-constexpr int KV_PX = KV_PAIRS * 2 * 1024;                   // P exchange: [pair][half][lane] x 16 B
+constexpr int KV_PAIRS = 4, KV_NW = 2 * KV_PAIRS, KV_BJ = 32 * KV_PAIRS, KV_SUB = 2, KV_BI = 32 * KV_SUB;
+constexpr int KV_NQ = 4, KV_NDO = 3;                         // Q tiles n-1 .. n+2, dO tiles n-1 .. n+1
+constexpr int KV_TILE = KV_BI * ROWB + KV_BI * 4;            // rows of Q or dO | their D or lse
+constexpr int KV_PX = KV_PAIRS * KV_SUB * 2 * 1024;          // P exchange: [pair][sub-tile][half][lane] x 16 B
 constexpr int KV_OFF_DO = KV_NQ * KV_TILE, KV_OFF_PX = KV_OFF_DO + KV_NDO * KV_TILE;
 constexpr int KV_OFF_SINK = KV_OFF_PX + 2 * KV_PX, KV_SMEM = KV_OFF_SINK + 256;
-static_assert(2 * KV_SMEM <= 160 * 1024, "two workgroups per compute unit");
+static_assert(KV_BI == 64 && KV_SMEM <= 160 * 1024, "a lane to a row's D or lse; one workgroup per compute unit");
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 // two probabilities in a word, the first in its low half; and back
 GX_DEVINL unsigned pack_p(float a, float b) {
@@ -680,7 +683,7 @@ struct RowTiles {
   }
 };
 
-__global__ void __launch_bounds__(64 * KV_NW, DH == 64 ? 3 : 2) cross_dkv_kernel(CrossArgs a) {
+__global__ void __launch_bounds__(64 * KV_NW, 2) cross_dkv_kernel(CrossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   constexpr int NS = DH / 16, NDT = DH / 32;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -695,7 +698,7 @@ __global__ void __launch_bounds__(64 * KV_NW, DH == 64 ? 3 : 2) cross_dkv_kernel
   // a block without a key that counts has only zeros to store (none where a later launch joins the splits and does that)
   if (j0 >= len) {
     if (a.splits == 1) {
-      const int key = j0 + (threadIdx.x >> 2);
+      const int key = j0 + (threadIdx.x >> 2);         // 4 lanes to a key
       if (key < a.Sk) {
         bf16* const dk = static_cast<bf16*>(a.dk) + pair_offset(a.sdk, b, kh) + key * a.sdk.t;
         bf16* const dv = static_cast<bf16*>(a.dv) + pair_offset(a.sdv, b, kh) + key * a.sdv.t;
@@ -725,9 +728,8 @@ __global__ void __launch_bounds__(64 * KV_NW, DH == 64 ? 3 : 2) cross_dkv_kernel
   const int tiles = (a.rows + KV_BI - 1) / KV_BI;
   const int t0 = (int)((long)tiles * split / a.splits), nt = (int)((long)tiles * (split + 1) / a.splits);
   // lse and D of a tile's rows go to LDS by the same direct path, 4 B per lane (wavefront 0: lse, wavefront 1: D; the others
-  // send an out-of-range load to a sink, so that every wavefront has the same number of loads in flight).  Rows beyond
-  // the last read as 0 everywhere (Q, dO, lse, D): their P is 1 but their contributions are exactly 0, and whole tiles beyond may
-  // be requested harmlessly.
+  // send an out-of-range load to a sink).  Rows beyond the last read as 0 everywhere (Q, dO, lse, D): their P is 1 but their
+  // contributions are exactly 0, and whole tiles beyond may be requested harmlessly.
   const float* const aux = (wave == 0 ? a.lrow : a.drow) + (long)kp * a.rows;
   RowTiles<KV_NW> srcq, srcdo;
   constexpr int PER = RowTiles<KV_NW>::PER, NREQ = 2 * PER + 1;
@@ -743,47 +745,47 @@ __global__ void __launch_bounds__(64 * KV_NW, DH == 64 ? 3 : 2) cross_dkv_kernel
   auto aux_load = [&](int t, char* dst, bool on) {
     const int i = t * KV_BI + lane;
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(aux), 0, (unsigned)a.rows * 4u, 0x00020000);
-    const unsigned o = on && lane < KV_BI && i < a.rows ? (unsigned)i * 4u : OOB;
+    const unsigned o = on && i < a.rows ? (unsigned)i * 4u : OOB;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_ptr)(on ? dst : smem + KV_OFF_SINK), 4, o, 0, 0, 0);
   };
   const bool lse_or_d = wave < 2, d_too = wave == 1;
   load_tile(srcq, q_slot(0));
-  load_tile(srcq, q_slot(1));
   load_tile(srcdo, do_slot(0));
+  load_tile(srcq, q_slot(1));
   aux_load(t0, wave == 0 ? do_slot(0) + KV_BI * ROWB : q_slot(0) + KV_BI * ROWB, lse_or_d);
   aux_load(t0 + 1, q_slot(1) + KV_BI * ROWB, d_too);
-  load_tile(srcq, q_slot(2));
-  load_tile(srcdo, do_slot(1));
-  aux_load(wave == 0 ? t0 + 1 : t0 + 2, (wave == 0 ? do_slot(1) : q_slot(2)) + KV_BI * ROWB, lse_or_d);
-  // all that was requested before this phase has landed, and this wavefront is done with its reads
+  // all that was requested has landed, and this wavefront is done with its reads
   auto meet = [&]() __attribute__((always_inline)) {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NREQ) : "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
   meet();
 
   int qs = 0, ds = 0;                       // ring positions of tile n
-  auto q_of = [&](int d) { return q_slot(qs + d < KV_NQ ? qs + d : qs + d - KV_NQ); };       // tile n + d, d in 0 .. 4
-  auto do_of = [&](int d) { return do_slot(ds + d < KV_NDO ? ds + d : ds + d - KV_NDO); };   // tile n + d, d in 0 .. 2
-  // request i of phase n: this wavefront's share of Q(n + 3), of dO(n + 2), then D(n + 3) or lse(n + 2)
+  auto q_of = [&](int d) { return q_slot((qs + d) & (KV_NQ - 1)); };                         // tile n + d, d in -1 .. 2
+  auto do_of = [&](int d) {                                                                  // tile n + d, d in -1 .. 1
+    const int x = ds + d;
+    return do_slot(x < 0 ? x + KV_NDO : x < KV_NDO ? x : x - KV_NDO);
+  };
+  // request i of phase n: this wavefront's share of Q(n + 2), of dO(n + 1), then D(n + 2) or lse(n + 1)
   auto request = [&](int n, int i) __attribute__((always_inline)) {
-    if (i < PER) srcq.issue(q_of(3), wave, i);
-    else if (i < 2 * PER) srcdo.issue(do_of(2), wave, i - PER);
-    else aux_load(wave == 0 ? n + 2 : n + 3, (wave == 0 ? do_of(2) : q_of(3)) + KV_BI * ROWB, lse_or_d);
+    if (i < PER) srcq.issue(q_of(2), wave, i);
+    else if (i < 2 * PER) srcdo.issue(do_of(1), wave, i - PER);
+    else aux_load(wave == 0 ? n + 1 : n + 2, (wave == 0 ? do_of(1) : q_of(2)) + KV_BI * ROWB, lse_or_d);
+  };
+  auto advance = [&]() __attribute__((always_inline)) {
+    qs = (qs + 1) & (KV_NQ - 1);
+    ds = ds == KV_NDO - 1 ? 0 : ds + 1;
+    srcq.next();
+    srcdo.next();
   };
   auto request_all = [&](int n) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < NREQ; i++) request(n, i);
   };
-  auto advance = [&]() __attribute__((always_inline)) {
-    qs = qs == KV_NQ - 1 ? 0 : qs + 1;
-    ds = ds == KV_NDO - 1 ? 0 : ds + 1;
-    srcq.next();
-    srcdo.next();
-  };
   struct CFrag { bf16x4 lo, hi; };
   constexpr int NPC = 2 * NDT, VD = 4, KD = 4;       // products with a transposed tile; fragments requested ahead
   static_assert(NPC >= VD && NS >= KD && NREQ <= NS, "slots of a phase");
-  // product p takes head-dim block p % NDT and rows 16 (p / NDT) .. + 15 of the tile
+  // product p takes head-dim block p % NDT and rows 16 (p / NDT) .. + 15 of the sub-tile
   auto c_request = [&](unsigned ct, auto P, CFrag& f) __attribute__((always_inline)) {
     constexpr int p = decltype(P)::value, dt = p % NDT, u = p / NDT;
     f.lo = lds_read_tr_issue<u * 16 * ROWB>(ct + coff[0][dt]);
@@ -794,20 +796,22 @@ __global__ void __launch_bounds__(64 * KV_NW, DH == 64 ? 3 : 2) cross_dkv_kernel
     lds_pin(f.hi);
     return __builtin_shufflevector(f.lo, f.hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  // S or dP of one tile on its own
+  // S or dP of a tile's first 32 rows on their own
   auto first_product = [&](const char* rows, f32x16& out) __attribute__((always_inline)) {
     out = zero16();
     streamed<NS, KD>([&](int s) { return frag_rows(rows, l32, s, g); },
                      [&](int s, bf16x8 f) { out = MFMA(f, kvf[s], out); });
   };
-  // One phase.  cur: S(n) (role V) or dP(n - 1) (role K), worked on in place; nxt: S(n + 1) or dP(n).
-  auto phase = [&](int n, f32x16& cur, f32x16& nxt, auto role_tag) __attribute__((always_inline)) {
+  // 32 rows of a phase.  Role V, tile n: cur holds their S; P and dV from it, and S of the next 32 rows into nxt.  Role K, tile
+  // n - 1: cur holds dP; dS and dK from it, dP of the next 32 rows into nxt.
+  auto half_phase = [&](int n, f32x16& cur, f32x16& nxt, auto role_tag, auto sub_tag) __attribute__((always_inline)) {
     constexpr bool ROLE_V = decltype(role_tag)::value;
-    const char* rows = ROLE_V ? q_of(1) : do_of(0);
-    const char* own = ROLE_V ? do_of(0) : q_of(4);                    // dO(n) and lse(n), or Q(n - 1) and D(n - 1)
-    const unsigned ct = lds_addr(own);
-    const float* stat = reinterpret_cast<const float*>(own + KV_BI * ROWB);
-    char* const pxn = px + ((ROLE_V ? n : n - 1) & 1) * KV_PX;
+    constexpr int SUB = decltype(sub_tag)::value, NEXT = (1 - SUB) * 32 * ROWB;
+    const char* rows = (ROLE_V ? q_of(SUB) : do_of(SUB - 1)) + NEXT;
+    const char* tile = ROLE_V ? do_of(0) : q_of(-1);                  // dO(n) and lse(n), or Q(n - 1) and D(n - 1)
+    const unsigned ct = lds_addr(tile + SUB * 32 * ROWB);
+    const float* stat = reinterpret_cast<const float*>(tile + KV_BI * ROWB) + SUB * 32;
+    char* const pxn = px + ((ROLE_V ? n : n - 1) & 1) * KV_PX + SUB * 2048;
     f32x4 row_value[4];
 #pragma unroll
     for (int q4 = 0; q4 < 4; q4++) row_value[q4] = *reinterpret_cast<const f32x4*>(stat + 8 * q4 + 4 * g);
@@ -859,7 +863,9 @@ __global__ void __launch_bounds__(64 * KV_NW, DH == 64 ? 3 : 2) cross_dkv_kernel
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (x + KD < NS) rf[x % KD] = frag_rows(rows, l32, x + KD, g);
       if constexpr (x >= NS - VD) c_request(ct, std::integral_constant<int, x - (NS - VD)>(), cf[x - (NS - VD)]);
-      if constexpr (x < NREQ) request(n, x);
+      if constexpr (SUB == 0) {             // as early as can be: the phase's end waits for them
+        if constexpr (x < NREQ) request(n, x);
+      }
       unroll<NPIECE>([&](auto K) __attribute__((always_inline)) {
         if constexpr (slot_of(decltype(K)::value) == x) piece(K);
       });
@@ -874,40 +880,38 @@ __global__ void __launch_bounds__(64 * KV_NW, DH == 64 ? 3 : 2) cross_dkv_kernel
     });
     asm volatile("" : "+v"(nxt));           // also where no tile follows
   };
-  // One loop per role (the branch is wavefront-uniform; both pass a barrier after each of the phases t0 .. nt - 1).
+  // One loop per role (the branch is wavefront-uniform; all pass a barrier after each of the phases t0 .. nt - 1).
   f32x16 sa, sb;
   int n = t0;
-  if (nt > t0) {
+  auto phase = [&](auto role_tag) __attribute__((always_inline)) {
+    half_phase(n, sa, sb, role_tag, std::integral_constant<int, 0>());
+    half_phase(n, sb, sa, role_tag, std::integral_constant<int, 1>());
+  };
+  if (jw >= len) {                          // a pair without a key that counts only brings its share of the tiles
+    for (; n < nt; n++) {
+      request_all(n);
+      meet();
+      advance();
+    }
+  } else if (nt > t0) {
     if (role_v) {
       first_product(q_of(0), sa);
-      auto next = [&](f32x16& cur, f32x16& nxt) __attribute__((always_inline)) {
-        phase(n, cur, nxt, std::true_type());
+      for (; n < nt; n++) {
+        phase(std::true_type());
         meet();
         advance();
-        n++;
-      };
-      while (n + 1 < nt) {
-        next(sa, sb);
-        next(sb, sa);
       }
-      if (n < nt) next(sa, sb);
     } else {
       request_all(n);
       first_product(do_of(0), sa);
       meet();
       advance();
-      n++;                                    // phases up to nt
-      auto next = [&](f32x16& cur, f32x16& nxt) __attribute__((always_inline)) {
-        phase(n, cur, nxt, std::false_type());
-        if (n < nt) meet();
+      for (n++; n < nt; n++) {
+        phase(std::false_type());
+        meet();
         advance();
-        n++;
-      };
-      while (n < nt) {
-        next(sa, sb);
-        next(sb, sa);
       }
-      if (n <= nt) next(sa, sb);
+      phase(std::false_type());             // the last tile's dS and dK; the others are done
     }
   }
   WAIT_VM0();   // requests for tiles beyond the last one (zero fill) must not outlive the workgroup's LDS
@@ -972,7 +976,7 @@ CrossSplits splits(const CrossArgs& a) {
   s.dq = parts(pairs_of(a) * cdiv(a.rows, d.bq), cdiv(a.Sk, d.rows), 512, 4);
   s.fwd = s.fwd < least ? least : s.fwd;
   s.dq = s.dq < least ? least : s.dq;
-  s.dkv = parts(pairs_of(a) * cdiv(a.Sk, KV_BJ), cdiv(a.rows, KV_BI), 512, 16);
+  s.dkv = parts(pairs_of(a) * cdiv(a.Sk, KV_BJ), cdiv(a.rows, KV_BI), 256, 8);
   return s;
 }
 int mask_smem(const CrossArgs& a, int splits, int rows) {
