@@ -35,14 +35,13 @@ GX_DEVINL long row_offset(const HeadStrides& s, int group, int r) {
 }
 GX_DEVINL long pair_offset(const HeadStrides& s, int b, int head) { return (long)b * s.b + (long)head * s.h; }
 
-// Into how many parts each launch cuts its keys or rows, and the scratch of a pass (host code, a rule on sizes alone)
-struct CrossSplits { int fwd, dq, dkv; };
-CrossSplits cross_splits_bf16(const CrossArgs& a);
-CrossSplits cross_splits_f32(const CrossArgs& a);
+// Into how many parts a launch cuts its keys (pass 0: forward, 1: dQ) or rows (2: dK / dV); host code, a rule on sizes alone
+int cross_parts_bf16(const CrossArgs& a, int pass);
+int cross_parts_f32(const CrossArgs& a, int pass);
 
 hipError_t cross_fwd_bf16(const CrossArgs& a, hipStream_t s);
 hipError_t cross_fwd_f32(const CrossArgs& a, hipStream_t s);
-// `a.splits` is set by the callee from cross_splits_*; part serves dQ, then dK / dV
+// `a.splits` is set by the callee; part serves dQ, then dK / dV
 hipError_t cross_bwd_bf16(const CrossArgs& a, hipStream_t s);
 hipError_t cross_bwd_f32(const CrossArgs& a, hipStream_t s);
 

@@ -7,6 +7,7 @@
 // once for the group), no block is shorter than another of its sample, and few rows against many keys (decoding) are
 // served by cutting the keys over workgroups too.
 #include "cross.h"
+#include <math.h>
 #include <type_traits>
 
 namespace gx {
@@ -31,7 +32,7 @@ namespace dh64 {
 
 }  // namespace
 
-CrossSplits cross_splits_bf16(const CrossArgs& a) { return a.dh == 128 ? dh128::splits(a) : dh64::splits(a); }
+int cross_parts_bf16(const CrossArgs& a, int pass) { return a.dh == 128 ? dh128::parts(a, pass) : dh64::parts(a, pass); }
 hipError_t cross_fwd_bf16(const CrossArgs& a, hipStream_t s) { return a.dh == 128 ? dh128::fwd(a, s) : dh64::fwd(a, s); }
 hipError_t cross_bwd_bf16(const CrossArgs& a, hipStream_t s) { return a.dh == 128 ? dh128::bwd(a, s) : dh64::bwd(a, s); }
 

@@ -234,9 +234,9 @@ GX_DEVINL void fwd_finish(const CrossArgs& a, const RowBlock& w, char* smem, f32
 // a row block's keys.
 // The step is the one of the causal forward kernel: in step t the products of the step before (O += V P, t - 1) and the scores
 // of the next one (S, t + 1) are issued one by one, behind each its share of the softmax of step t; K(t + 2) and V(t) are
-// requested in its first slots into two buffers each.  LAZY: the reference exponent follows a row's maximum only when that
-// exceeds it by more than 2^8; else it is the running maximum.
-template <int NQ, int SPLIT, int BKV, bool LAZY, bool MASK>
+// requested in its first slots into two buffers each.  The reference exponent follows a row's maximum only when that exceeds it by
+// more than 2^8, so that O is rescaled rarely (following every rise, 128 pairs of 2048 x 2048 took 338 us instead of 301).
+template <int NQ, int SPLIT, int BKV, bool MASK>
 __global__ void __launch_bounds__(64 * NQ * SPLIT, 2) cross_fwd_kernel(CrossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   constexpr int NW = NQ * SPLIT, BQ = 32 * NQ, ROWS = BKV * SPLIT, TILE = ROWS * ROWB, NS = DH / 16;
@@ -347,9 +347,9 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, 2) cross_fwd_kernel(CrossArgs
     float psum = 0.f, alpha = 1.f;
     bool moved = false;
     // the softmax of step t (base-2 exponentials, scale folded into the exponent's multiply-add) in pieces: 0 mask, 1
-    // reference, then EPP scores each, a head-dim block of O to rescale each, 16 keys to round each
+    // reference, then EPP scores each, O to rescale, 16 keys to round each
     constexpr int EPP = 2;
-    constexpr int NE = 16 * NJT / EPP, P_E = 2, P_R = P_E + NE, P_P = P_R + NDT, NPIECE = P_P + NG;
+    constexpr int NE = 16 * NJT / EPP, P_E = 2, P_R = P_E + NE, P_P = P_R + 1, NPIECE = P_P + NG;
     auto piece = [&](auto K) __attribute__((always_inline)) {
       constexpr int k = decltype(K)::value;
       if constexpr (k == 0) {
@@ -361,11 +361,8 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, 2) cross_fwd_kernel(CrossArgs
 #pragma unroll
           for (int v = 0; v < 16; v++) mloc = fmaxf(mloc, sacc[jt][v]);
         mloc = max_across_halves(mloc) * c2;
-        float mnew = fmaxf(m, mloc);
-        if (LAZY) {
-          moved = __builtin_amdgcn_ballot_w64(mloc > m + 8.f) != 0;
-          mnew = moved ? mnew : m;
-        }
+        moved = __builtin_amdgcn_ballot_w64(mloc > m + 8.f) != 0;
+        const float mnew = moved ? fmaxf(m, mloc) : m;
         alpha = __builtin_amdgcn_exp2f(m - mnew);
         m = mnew;
         lsum *= alpha;
@@ -380,12 +377,7 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, 2) cross_fwd_kernel(CrossArgs
         }
         asm volatile("" : "+v"(psum));
       } else if constexpr (k < P_P) {
-        constexpr int dt = k - P_R;
-        if constexpr (!LAZY && !FIRST) {
-#pragma unroll
-          for (int v = 0; v < 16; v++) o[dt][v] *= alpha;
-          asm volatile("" : "+v"(o[dt]));
-        } else if constexpr (LAZY && !FIRST && dt == 0) {
+        if constexpr (!FIRST) {
           if (moved) {
 #pragma unroll
             for (int d = 0; d < NDT; d++)
@@ -400,7 +392,7 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, 2) cross_fwd_kernel(CrossArgs
     };
     // cost of the pieces in issue slots, for spreading them over the matrix instructions
     constexpr auto cost = [](int k) constexpr {
-      return k == 0 ? 4 : k == 1 ? 12 + 8 * NJT : k < P_R ? 6 * EPP : k < P_P ? (LAZY ? 1 : 16) : 4;
+      return k == 0 ? 4 : k == 1 ? 12 + 8 * NJT : k < P_R ? 6 * EPP : 4;
     };
     constexpr auto upto = [cost](int k) constexpr { int c = 0; for (int x = 0; x < k; x++) c += cost(x); return c; };
     constexpr int TOTAL = upto(NPIECE);
@@ -949,65 +941,126 @@ hipError_t set_smem(K kernel, int bytes) {
 }
 long pairs_of(const CrossArgs& a) { return (long)a.B * a.hk; }
 
-// Shapes of the forward and dQ kernels: 0 <4, 1, 64>: 128 rows, 1 <2, 2, 32>: 64 rows and two shares of a step's keys, 3 <1, 4, 32>:
-// 32 rows and four shares.
-struct Shape { int bq, rows, threads; };
-constexpr Shape SHAPES[4] = {{128, 64, 256}, {64, 64, 256}, {64, 128, 512}, {32, 128, 256}};
+// What a launch takes is estimated from its sizes, and the least estimate decides shape and splits.  A workgroup takes `fix` and
+// `step` for each tile, `pair` where two share a compute unit (0: one at a time); keys that nobody else has brought near come
+// at 5.3 TB/s to many workgroups, at 0.63 of that to `busy` of them; parts of a split are written, read and added by a launch of its own.
+// Microseconds and MB, from the runs listed below; only their proportions matter.
+struct Shape { int rows, keys; double fix, step, pair, busy; };       // rows of a block, keys of a step
+double estimate(const Shape& s, long blocks, long steps, int parts, double part_mb, double mb) {
+  const long n = cdiv(blocks * parts, 256), per = cdiv(steps, parts);
+  double t = s.pair > 0 ? (n / 2) * (s.fix + per * s.pair) + (n % 2) * (s.fix + per * s.step) : n * (s.fix + per * s.step);
+  if (mb > 0) {
+    const double us = mb / (5.3 * (1.0 - exp(-(double)(blocks * parts) / s.busy)));
+    if (t < us) t = us;
+  }
+  return parts == 1 ? t : t + 3.5 + 0.04 * parts + parts * part_mb / 4.0;
+}
+// the best number of parts of a launch and its estimate
+struct Choice { int shape, parts; double us; };
+Choice best_parts(int shape, const Shape& s, long blocks, long steps, int least, double part_mb, double mb) {
+  Choice c{shape, least, estimate(s, blocks, steps, least, part_mb, mb)};
+  for (const int p : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+    if (p > steps) break;
+    const double t = p > least ? estimate(s, blocks, steps, p, part_mb, mb) : c.us;
+    if (t < c.us) c = Choice{shape, p, t};
+  }
+  return c;
+}
 
-int fwd_shape(const CrossArgs& a) {
-  if (a.rows <= 32) return 3;
-  return pairs_of(a) * cdiv(a.rows, 128) > 384 ? 0 : 1;
+// Forward: 0 <4, 1, 64>: 128 rows, 1 <2, 2, 32>: 64 rows and two shares of a step's keys, 2 <1, 4, 32>: 32 rows and four shares.
+// us, head dim 128, batch x queries x keys x heads / key heads: best of each shape (with its parts)
+//   1 x 1024 x 1024 x 8 / 8:  12.8 (shape 2), 15.7 (1), 21.4 (0)     2 x 1024 x 1024 x 16 / 16: 24.5 (0), 26.2 (1)
+//   1 x 512 x 512 x 8 / 8:    9.1 (2), 10.9 (1), 14.0 (0)            1 x 2048 x 2048 x 16 / 16: 41.0 (0), 43.6 (1)
+//   1 x 200 x 200 x 64 / 8:   9.2 (1), 10.7 (0), 13.7 (2)            4 x 2048 x 1501 x 16 / 16: 107 (0), 129 (1)
+//   1 x 1024 x 4096 x 8 / 8:  31.9 (2), 34.0 (1, 2 parts)            16 x 1 x 8192 x 40 / 8: 98.6 (1, 4 parts), 104 (2, 2 parts)
+//   1 x 1 x 65536 x 32 / 8:   48.9 (2, 32 parts), 49.6 (1, 32)       8 x 5 x 3000 x 32 / 8: 22.5 (1, 8 parts), 22.6 (2, 4 parts)
+//   16 x 1 x 8192 x 40 / 8 whole (128 workgroups) 173 (1), 140 (2); 8 x 64 x 8192 x 16 / 16 134 (1, 2 parts), 109 (1, 4 parts)
+//   1 x 16 x 4096 x 16 / 4:   12.6 (2, 16 parts), 13.5 (2, 8)        4 x 1 x 512 x 32 / 8: 9.5 (2, whole), 11.8 (2, 4 parts)
+// Head dim 64: 1 x 1024 x 1024 x 12 / 12 11.8 (2), 12.0 (1), 16.3 (0); 4 x 1024 x 1024 x 16 / 16 25.7 (0), 29.0 (1).
+constexpr Shape FWD[3] = {{128, 64, 5.0, DH == 128 ? 1.0 : 0.72, DH == 128 ? 2.1 : 1.15, DH == 128 ? 146 : 290},
+                          {64, 64, 2.5, DH == 128 ? 0.62 : 0.41, DH == 128 ? 1.09 : 0.78, DH == 128 ? 146 : 290},
+                          {32, 128, 3.0, DH == 128 ? 0.85 : 0.5, DH == 128 ? 0.0 : 0.85, DH == 128 ? 100 : 146}};
+// Neither here nor below by whether there is a mask, so that one workspace serves both
+Choice fwd_estimate(const CrossArgs& a) {
+  const int least = cdiv(a.Sk, MASK_KEYS * 3 / 4) > 1 ? cdiv(a.Sk, MASK_KEYS * 3 / 4) : 1;   // mask bits have their room in LDS
+  const double part_mb = pairs_of(a) * a.rows * (DH + 2) * 8e-6, mb = pairs_of(a) * a.Sk * DH * 4e-6;
+  Choice c{};
+  for (int k = 0; k < 3; k++) {
+    const int blocks = cdiv(a.rows, FWD[k].rows);            // of a pair: two or more do not read the keys quite together
+    const Choice x = best_parts(k, FWD[k], pairs_of(a) * blocks, cdiv(a.Sk, FWD[k].keys), least, part_mb,
+                                blocks > 1 ? 1.33 * mb : mb);
+    if (k == 0 || x.us < c.us) c = x;
+  }
+  return c;
 }
-int dq_shape(const CrossArgs& a) { return pairs_of(a) * cdiv(a.rows, 128) > 384 ? 0 : 1; }
-
-// Parts of a launch of `blocks` workgroups, `units` of work (tiles) each, so that about `want` workgroups come out, each with
-// at least `least` units
-int parts(long blocks, long units, long want, long least) {
-  long n = blocks >= want || blocks == 0 ? 1 : want / blocks;
-  if (n > units / least) n = units / least;
-  return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+// dQ: 0 <4, 1, 64>: 128 rows, 1 <2, 2, 32>: 64 rows.  Forward and backward, us, shape 0 / 1: 4 x 2048 x 1501 x 16 / 16 381 / 402, 2 x
+// 4096 x 64 x 16 / 8 60.5 / 68.1, 1 x 2048 x 2048 x 16 / 16 141 / 139, 1 x 4096 x 1024 x 8 / 2 91.4 / 88.9; in parts, shape 1: 1 x 1024 x 1024
+// x 8 / 8 whole 55.2, two 56.5, four 64.8; 4 x 40 x 4096 x 16 / 8 four 73.3, two 78.
+constexpr Shape DQ[2] = {{128, 64, 5.0, DH == 128 ? 1.45 : 0.95, DH == 128 ? 2.6 : 1.5, 0},
+                         {64, 64, 3.5, DH == 128 ? 0.95 : 0.65, DH == 128 ? 1.5 : 0.95, 0}};
+Choice dq_estimate(const CrossArgs& a) {
+  const int least = cdiv(a.Sk, MASK_KEYS * 3 / 4) > 1 ? cdiv(a.Sk, MASK_KEYS * 3 / 4) : 1;
+  const double part_mb = pairs_of(a) * a.rows * DH * 8e-6;
+  Choice c{};
+  for (int k = 0; k < 2; k++) {
+    const Choice x = best_parts(k, DQ[k], pairs_of(a) * cdiv(a.rows, DQ[k].rows), cdiv(a.Sk, DQ[k].keys), least, part_mb, 0);
+    if (k == 0 || x.us < c.us) c = x;
+  }
+  return c;
 }
-// Never by whether there is a mask, so that one workspace serves both
-CrossSplits splits(const CrossArgs& a) {
-  CrossSplits s;
-  const Shape f = SHAPES[fwd_shape(a)], d = SHAPES[dq_shape(a)];
-  const int least = cdiv(a.Sk, MASK_KEYS * 3 / 4);   // the bits of a workgroup's keys have their room in LDS
-  s.fwd = parts(pairs_of(a) * cdiv(a.rows, f.bq), cdiv(a.Sk, f.rows), 512, 2);
-  s.dq = parts(pairs_of(a) * cdiv(a.rows, d.bq), cdiv(a.Sk, d.rows), 512, 4);
-  s.fwd = s.fwd < least ? least : s.fwd;
-  s.dq = s.dq < least ? least : s.dq;
-  s.dkv = parts(pairs_of(a) * cdiv(a.Sk, KV_BJ), cdiv(a.rows, KV_BI), 256, 8);
-  return s;
+// dK / dV, parts of the rows.  Forward and backward, us: 1 x 1024 x 1024 x 8 / 8 two parts 64.8, four 56.9, six 61.5; 2 x 4096 x 64 x
+// 16 / 8 eight 69.4, sixteen 59.8, 24 70.7; head dim 64, 3 x 3000 x 300 x 16 / 16 whole 94.5, three 88.9, six 97.8.
+constexpr Shape DKV = {KV_BI, KV_BJ, 5.0, DH == 128 ? 1.9 : 1.2, 0.0, 0};
+Choice dkv_estimate(const CrossArgs& a) {
+  return best_parts(0, DKV, pairs_of(a) * cdiv(a.Sk, DKV.keys), cdiv(a.rows, DKV.rows), 1, pairs_of(a) * a.Sk * DH * 16e-6, 0);
 }
+// A call asks several times for the same sizes, and the next one mostly too: each host thread keeps its last plan (sizes in, shape
+// and parts out)
+template <Choice (*ESTIMATE)(const CrossArgs&)>
+Choice kept(const CrossArgs& a) {
+  static thread_local long pairs = -1;
+  static thread_local int rows, keys;
+  static thread_local Choice last;
+  if (pairs != pairs_of(a) || rows != a.rows || keys != a.Sk) {
+    last = ESTIMATE(a);
+    pairs = pairs_of(a);
+    rows = a.rows;
+    keys = a.Sk;
+  }
+  return last;
+}
+Choice fwd_choice(const CrossArgs& a) { return kept<fwd_estimate>(a); }
+Choice dq_choice(const CrossArgs& a) { return kept<dq_estimate>(a); }
+Choice dkv_choice(const CrossArgs& a) { return kept<dkv_estimate>(a); }
+int parts(const CrossArgs& a, int pass) { return (pass == 0 ? fwd_choice(a) : pass == 1 ? dq_choice(a) : dkv_choice(a)).parts; }
 int mask_smem(const CrossArgs& a, int splits, int rows) {
   return a.key_mask ? 4 * mask_words(cdiv(cdiv(a.Sk, rows), splits) * rows + rows, rows) : 0;
 }
 
-template <int NQ, int SPLIT, int BKV, bool LAZY, bool MASK>
+template <int NQ, int SPLIT, int BKV, bool MASK>
 hipError_t go_fwd(const CrossArgs& a, hipStream_t s) {
   constexpr int TILES = fwd_smem(NQ, SPLIT, BKV), ROWS = BKV * SPLIT;
   static bool configured = false;
   if (!configured) {
     const hipError_t e =
-        set_smem(cross_fwd_kernel<NQ, SPLIT, BKV, LAZY, MASK>, TILES + (MASK ? 4 * mask_words(MASK_KEYS, ROWS) : 0));
+        set_smem(cross_fwd_kernel<NQ, SPLIT, BKV, MASK>, TILES + (MASK ? 4 * mask_words(MASK_KEYS, ROWS) : 0));
     if (e != hipSuccess) return e;
     configured = true;
   }
   const dim3 grid((unsigned)(pairs_of(a) * cdiv(a.rows, 32 * NQ) * a.splits));
-  hipLaunchKernelGGL((cross_fwd_kernel<NQ, SPLIT, BKV, LAZY, MASK>), grid, dim3(64 * NQ * SPLIT),
+  hipLaunchKernelGGL((cross_fwd_kernel<NQ, SPLIT, BKV, MASK>), grid, dim3(64 * NQ * SPLIT),
                      TILES + mask_smem(a, a.splits, ROWS), s, a);
   return hipGetLastError();
 }
 // With a mask the 128-row shape would spill registers (the untracked LDS reads forbid that): 64 rows then.
 hipError_t fwd(CrossArgs a, hipStream_t s) {
-  a.splits = splits(a).fwd;
+  const Choice c = fwd_choice(a);
+  a.splits = c.parts;
   const bool mask = a.key_mask != nullptr;
-  const int shape = fwd_shape(a);
   hipError_t e;
-  if (shape == 3) e = mask ? go_fwd<1, 4, 32, true, true>(a, s) : go_fwd<1, 4, 32, true, false>(a, s);
-  else if (mask) e = go_fwd<2, 2, 32, true, true>(a, s);
-  else if (shape == 1) e = go_fwd<2, 2, 32, true, false>(a, s);
-  else e = go_fwd<4, 1, 64, true, false>(a, s);
+  if (c.shape == 2) e = mask ? go_fwd<1, 4, 32, true>(a, s) : go_fwd<1, 4, 32, false>(a, s);
+  else if (mask) e = go_fwd<2, 2, 32, true>(a, s);
+  else e = c.shape == 1 ? go_fwd<2, 2, 32, false>(a, s) : go_fwd<4, 1, 64, false>(a, s);
   return e != hipSuccess || a.splits == 1 ? e : cross_join_fwd(true, a, s);
 }
 
@@ -1032,16 +1085,16 @@ hipError_t bwd(CrossArgs a, hipStream_t s) {
     if (e != hipSuccess) return e;
     configured = true;
   }
-  const CrossSplits n = splits(a);
   hipError_t e = hipSuccess;
   if (a.rows > 0) {
-    a.splits = n.dq;
+    const Choice c = dq_choice(a);
+    a.splits = c.parts;
     if (a.key_mask) e = go_dq<2, 2, 32, true>(a, s);
-    else e = dq_shape(a) == 0 ? go_dq<4, 1, 64, false>(a, s) : go_dq<2, 2, 32, false>(a, s);
+    else e = c.shape == 0 ? go_dq<4, 1, 64, false>(a, s) : go_dq<2, 2, 32, false>(a, s);
     if (e == hipSuccess && a.splits > 1) e = cross_join_dq(true, a, s);
   }
   if (e != hipSuccess || a.Sk == 0) return e;
-  a.splits = n.dkv;
+  a.splits = dkv_choice(a).parts;
   hipLaunchKernelGGL(cross_dkv_kernel, dim3((unsigned)(pairs_of(a) * cdiv(a.Sk, KV_BJ) * a.splits)), dim3(64 * KV_NW), KV_SMEM, s, a);
   e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : cross_join_dkv(true, a, s);

@@ -360,15 +360,14 @@ int parts(long blocks, long units, long want, long least) {
 
 }  // namespace
 
-CrossSplits cross_splits_f32(const CrossArgs& a) {
+int cross_parts_f32(const CrossArgs& a, int pass) {
   const long pairs = (long)a.B * a.hk;
-  return CrossSplits{parts(pairs * cdiv(a.rows, 32), cdiv(a.Sk, 32), 512, 8), parts(pairs * cdiv(a.rows, 32), cdiv(a.Sk, 32), 512, 8),
-                     parts(pairs * cdiv(a.Sk, 32), cdiv(a.rows, 32), 256, 8)};
+  return pass < 2 ? parts(pairs * cdiv(a.rows, 32), cdiv(a.Sk, 32), 512, 8) : parts(pairs * cdiv(a.Sk, 32), cdiv(a.rows, 32), 256, 8);
 }
 
 hipError_t cross_fwd_f32(const CrossArgs& args, hipStream_t s) {
   CrossArgs a = args;
-  a.splits = cross_splits_f32(a).fwd;
+  a.splits = cross_parts_f32(a, 0);
   GX_CROSS_F32(cross_fwd_f32_kernel, cdiv(a.rows, 32));
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : cross_join_fwd(false, a, s);
@@ -376,16 +375,15 @@ hipError_t cross_fwd_f32(const CrossArgs& args, hipStream_t s) {
 
 hipError_t cross_bwd_f32(const CrossArgs& args, hipStream_t s) {
   CrossArgs a = args;
-  const CrossSplits n = cross_splits_f32(a);
   hipError_t e = hipSuccess;
   if (a.rows > 0) {
-    a.splits = n.dq;
+    a.splits = cross_parts_f32(a, 1);
     GX_CROSS_F32(cross_dq_f32_kernel, cdiv(a.rows, 32));
     e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) e = cross_join_dq(false, a, s);
   }
   if (e != hipSuccess || a.Sk == 0) return e;
-  a.splits = n.dkv;
+  a.splits = cross_parts_f32(a, 2);
   GX_CROSS_F32(cross_dkv_f32_kernel, cdiv(a.Sk, 32));
   e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : cross_join_dkv(false, a, s);
