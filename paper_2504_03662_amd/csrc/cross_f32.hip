@@ -2,11 +2,15 @@
 //
 // As in the causal fp32 kernels a workgroup owns 32 rows (forward, dQ) or 32 keys (dK / dV) of a (sample, key head) pair and
 // its 4 wavefronts take every 4th 32-wide tile of the other side; scores are taken transposed to the owner, so that an accumulator
-// register is, as it stands, an operand of the next product (register v of a lane in half g holds tile row 8 (v / 4) + 4 g + v % 4)
-// and operands come straight from global memory.  The parts' results are merged through LDS in wavefront order.  Head dimensions
-// up to 128 (multiples of 4) are padded with zeros to 32, 64 or 128.
+// register is, as it stands, an operand of the next product (register v of a lane in half g holds tile row 8 (v / 4) + 4 g + v % 4).
+// Operands come from global memory, requested while the tile before is worked on; where a tile's rows are the second operand of
+// one product and the first of another (dQ, dK / dV) a wavefront puts what it holds of them into LDS and reads columns.  The parts'
+// results are merged through LDS in wavefront order.  Head dimensions up to 128 (multiples of 4) are padded with zeros to 32, 64 or 128.
 // Keys that do not count have bits of a 32-bit word per tile: their scores are left out by selection, and what is read of them
 // is replaced by zeros before it becomes an operand.
+// Bound by the matrix pipe where there are many tiles (2048 x 2048, 16 heads of 128: forward 384 us, 90 TFLOP/s of the 145 that a
+// library product of fp32 reaches; a lone wavefront per SIMD does not overlap its exponentials), by latency where there are few:
+// 3 x 257 x 333, 8 / 4 heads of 64: 16 us, 21 us (dQ) and 33 us (dK / dV in three parts; 40 whole).
 #include "cross.h"
 
 namespace gx {
@@ -44,35 +48,40 @@ GX_DEVINL f32x16 row_product(const f32x4 (&a)[DHP / 8], const f32x4 (&b)[DHP / 8
     for (int e = 0; e < 4; e++) s = mfma(a[c][e], b[c][e], s);
   return s;
 }
-// acc[dt][d][col] += sum over the tile's 32 rows of x[row][d] * w[row][col]; row_at(v) gives the address of the row of register v,
-// which counts if its bit does (else zero stands for it)
-template <int DHP, class RowAt>
-GX_DEVINL void col_product(f32x16 (&acc)[DHP / 32], const f32x16& w, RowAt row_at, unsigned bits, int dh, int g, int l32) {
-  constexpr int CH = DHP >= 64 ? 2 : 1;                      // column blocks in registers at a time
-  const float* rows[16];
+// A tile's rows as the other operand of a product over them: a wavefront puts the rows that its lanes hold into LDS (zeros for
+// rows that do not count) and reads columns.  A row's 16 spare bytes put rows that are written together into different banks.
+template <int DHP>
+constexpr int STRIDE = DHP + 4;
+template <int DHP>
+GX_DEVINL void put_rows(float* tile, const f32x4 (&x)[DHP / 8], bool on, int g, int l32) {
+  __builtin_amdgcn_wave_barrier();
 #pragma unroll
-  for (int v = 0; v < 16; v++) rows[v] = row_at(v);
+  for (int c = 0; c < DHP / 8; c++) {
+    f32x4 y = x[c];
 #pragma unroll
-  for (int d0 = 0; d0 < DHP / 32; d0 += CH) {
-    float x[CH][16];
+    for (int e = 0; e < 4; e++) y[e] = on ? y[e] : 0.f;
+    *reinterpret_cast<f32x4*>(tile + l32 * STRIDE<DHP> + 8 * c + 4 * g) = y;
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+// acc[dt][d][col] += sum over the tile's rows of x[row][d] * w[row][col]
+template <int DHP>
+GX_DEVINL void col_product(f32x16 (&acc)[DHP / 32], const f32x16& w, const float* tile, int g, int l32) {
+  constexpr int AHEAD = DHP <= 32 ? 4 : 2;                   // rows read ahead of the products
+  float x[AHEAD][DHP / 32];
+  const float* const mine = tile + 4 * g * STRIDE<DHP> + l32;
+  auto read = [&](int v) __attribute__((always_inline)) {
 #pragma unroll
-    for (int c = 0; c < CH; c++) {
-      const int dd = 32 * (d0 + c) + l32, d = dd < dh ? dd : dh - 1;    // columns beyond dh are never stored
+    for (int dt = 0; dt < DHP / 32; dt++) x[v % AHEAD][dt] = mine[acc_row(v, 0) * STRIDE<DHP> + 32 * dt];
+  };
 #pragma unroll
-      for (int v = 0; v < 16; v++) x[c][v] = rows[v][d];
-    }
-    if (bits != ALL) {
+  for (int v = 0; v < AHEAD; v++) read(v);
 #pragma unroll
-      for (int v = 0; v < 16; v++)
-        if (!bit_of(bits, v, g)) {
+  for (int v = 0; v < 16; v++) {
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int c = 0; c < CH; c++) x[c][v] = 0.f;
-        }
-    }
-#pragma unroll
-    for (int v = 0; v < 16; v++)
-#pragma unroll
-      for (int c = 0; c < CH; c++) acc[d0 + c] = mfma(x[c][v], w[v], acc[d0 + c]);
+    for (int dt = 0; dt < DHP / 32; dt++) acc[dt] = mfma(x[v % AHEAD][dt], w[v], acc[dt]);
+    if (v + AHEAD < 16) read(v + AHEAD);
   }
 }
 // Adds the parts' accumulators in the order of the wavefronts; the sum is complete in wavefront 0.
@@ -119,12 +128,12 @@ struct Where {
     len = keys_of(a, b);
   }
 };
-// bits of the 32 keys from key j0 on; the same in every lane
-GX_DEVINL unsigned key_bits(const CrossArgs& a, int b, int j0, int len, int l32) {
-  const int j = j0 + l32;
-  bool on = j < len;
-  if (a.key_mask && on) on = a.key_mask[(long)b * a.Sk + j] != 0;
-  return (unsigned)__builtin_amdgcn_ballot_w64(on);
+// the mask's byte of this lane's key of the 32 from key j0 on, read a tile early, and the bits of the 32, the same in every lane
+GX_DEVINL unsigned key_byte(const CrossArgs& a, int b, int j0, int l32) {
+  return a.key_mask ? a.key_mask[(long)b * a.Sk + min(j0 + l32, a.Sk - 1)] : 1u;
+}
+GX_DEVINL unsigned key_bits(unsigned byte, int j0, int len, int l32) {
+  return (unsigned)__builtin_amdgcn_ballot_w64(byte != 0 && j0 + l32 < len);
 }
 GX_DEVINL const float* f32_of(const void* p) { return static_cast<const float*>(p); }
 
@@ -149,12 +158,33 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_fwd_f32_k
   const float* const vb = f32_of(a.v) + pair_offset(a.sv, w.b, w.kh);
   const int nt = (w.len + 31) / 32;
   const int t0 = (int)((long)nt * w.split / a.splits), t1 = (int)((long)nt * (w.split + 1) / a.splits);
+  f32x4 kf[DHP / 8];
+  auto load_k = [&](int t) __attribute__((always_inline)) {
+    load_rows<DHP>(kb + (long)min(32 * t + l32, w.len - 1) * a.sk.t, a.dh, g, kf);
+  };
+  unsigned byte = 0;
+  if (t0 + part < t1) {
+    byte = key_byte(a, w.b, 32 * (t0 + part), l32);
+    load_k(t0 + part);
+  }
   for (int t = t0 + part; t < t1; t += PARTS) {
     const int j0 = 32 * t;
-    const unsigned bits = key_bits(a, w.b, j0, w.len, l32);
-    f32x4 kf[DHP / 8];
-    load_rows<DHP>(kb + (long)min(j0 + l32, w.len - 1) * a.sk.t, a.dh, g, kf);
+    const unsigned bits = key_bits(byte, j0, w.len, l32);
+    float vf[DHP / 32][16];                                      // columns of the tile's rows, on their way while the scores are taken
+#pragma unroll
+    for (int v = 0; v < 16; v++) {
+      const float* const row = vb + (long)min(j0 + acc_row(v, g), w.len - 1) * a.sv.t;
+#pragma unroll
+      for (int dt = 0; dt < DHP / 32; dt++) vf[dt][v] = row[min(32 * dt + l32, a.dh - 1)];    // columns beyond dh are never stored
+    }
+    __builtin_amdgcn_sched_barrier(0);
     f32x16 s = row_product<DHP>(kf, qf);                         // S^T[j][i]
+    __builtin_amdgcn_sched_barrier(0);
+    if (t + PARTS < t1) {                                        // and these while the output is
+      byte = key_byte(a, w.b, 32 * (t + PARTS), l32);
+      load_k(t + PARTS);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     float mx = -INFINITY;
     const float mold = m;
 #pragma unroll
@@ -175,7 +205,18 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_fwd_f32_k
     for (int dt = 0; dt < DHP / 32; dt++)
 #pragma unroll
       for (int v = 0; v < 16; v++) o[dt][v] *= alpha;
-    col_product<DHP>(o, s, [&](int v) { return vb + (long)min(j0 + acc_row(v, g), w.len - 1) * a.sv.t; }, bits, a.dh, g, l32);
+    if (bits != ALL) {
+#pragma unroll
+      for (int v = 0; v < 16; v++)
+        if (!bit_of(bits, v, g)) {
+#pragma unroll
+          for (int dt = 0; dt < DHP / 32; dt++) vf[dt][v] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < 16; v++)
+#pragma unroll
+      for (int dt = 0; dt < DHP / 32; dt++) o[dt] = mfma(vf[dt][v], s[v], o[dt]);
   }
   // merge the parts' (m, l, O); a part without a key has m = -inf, l = 0, O = 0 and adds nothing
   if (part > 0) {
@@ -218,7 +259,8 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_fwd_f32_k
 // D = rowsum(dO * O), dS = P (dP - D), dQ = scale dS K; leaves D and lse (+inf for a row without a key) in row order
 template <int DHP>
 __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dq_f32_kernel(CrossArgs a) {
-  __shared__ float lds[(PARTS - 1) * (DHP / 2) * 64];
+  constexpr int TILE = 32 * STRIDE<DHP>;
+  __shared__ alignas(16) float lds[PARTS * TILE];
   const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5, l32 = lane & 31;
   const Where w(a, (a.rows + 31) / 32);
@@ -250,23 +292,33 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dq_f32_ke
   const float* const vb = f32_of(a.v) + pair_offset(a.sv, w.b, w.kh);
   const int nt = (w.len + 31) / 32;
   const int t0 = (int)((long)nt * w.split / a.splits), t1 = (int)((long)nt * (w.split + 1) / a.splits);
+  float* const tile = lds + part * TILE;
+  f32x4 kf[DHP / 8], vf[DHP / 8];
+  auto row_of = [&](int t) __attribute__((always_inline)) { return (long)min(32 * t + l32, w.len - 1); };
+  unsigned byte = 0;
+  if (t0 + part < t1) {
+    byte = key_byte(a, w.b, 32 * (t0 + part), l32);
+    load_rows<DHP>(kb + row_of(t0 + part) * a.sk.t, a.dh, g, kf);
+    load_rows<DHP>(vb + row_of(t0 + part) * a.sv.t, a.dh, g, vf);
+  }
   for (int t = t0 + part; t < t1; t += PARTS) {
-    const int j0 = 32 * t;
-    const unsigned bits = key_bits(a, w.b, j0, w.len, l32);
-    const long jr = min(j0 + l32, w.len - 1);
-    f32x16 s, dp;
-    {
-      f32x4 kf[DHP / 8];
-      load_rows<DHP>(kb + jr * a.sk.t, a.dh, g, kf);
-      s = row_product<DHP>(kf, qf);                              // S^T[j][i]
-      if (DHP > 64) __builtin_amdgcn_sched_barrier(0);           // one operand in registers at a time
-      load_rows<DHP>(vb + jr * a.sv.t, a.dh, g, kf);
-      dp = row_product<DHP>(kf, dof);                            // dP^T[j][i]
+    const unsigned bits = key_bits(byte, 32 * t, w.len, l32);
+    const bool more = t + PARTS < t1;
+    f32x16 s = row_product<DHP>(kf, qf);                         // S^T[j][i]
+    __builtin_amdgcn_sched_barrier(0);
+    put_rows<DHP>(tile, kf, (bits >> l32) & 1u, g, l32);
+    if (more) {                                                  // on their way during the rest of this tile
+      byte = key_byte(a, w.b, 32 * (t + PARTS), l32);
+      load_rows<DHP>(kb + row_of(t + PARTS) * a.sk.t, a.dh, g, kf);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    const f32x16 dp = row_product<DHP>(vf, dof);                 // dP^T[j][i]
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) load_rows<DHP>(vb + row_of(t + PARTS) * a.sv.t, a.dh, g, vf);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int v = 0; v < 16; v++) s[v] = bit_of(bits, v, g) ? expf(s[v] * a.scale - lse) * (dp[v] - dd) : 0.f;
-    if (DHP > 64) __builtin_amdgcn_sched_barrier(0);
-    col_product<DHP>(dq, s, [&](int v) { return kb + (long)min(j0 + acc_row(v, g), w.len - 1) * a.sk.t; }, bits, a.dh, g, l32);
+    col_product<DHP>(dq, s, tile, g, l32);
   }
   merge_parts(dq, lds, part, lane);
   if (part != 0 || r >= a.rows) return;
@@ -278,14 +330,15 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dq_f32_ke
 // dV_j = sum_i P_ij dO_i, dK_j = scale sum_i dS_ij Q_i over the pair's rows.  A lane owns a key; what the lanes of keys that do not
 // count compute stays in their columns, and zeros are stored for them.
 template <int DHP>
-__global__ void __launch_bounds__(64 * PARTS, 1) cross_dkv_f32_kernel(CrossArgs a) {
-  __shared__ float lds[(PARTS - 1) * (DHP / 2) * 64];
+__global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dkv_f32_kernel(CrossArgs a) {
+  constexpr int TILE = 32 * STRIDE<DHP>;
+  __shared__ alignas(16) float lds[PARTS * TILE + PARTS * 64];
   const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5, l32 = lane & 31;
   const Where w(a, (a.Sk + 31) / 32);
   const int j0 = 32 * w.tile, j = j0 + l32, head0 = w.kh * a.group;
   const long jc = min(j, a.Sk - 1);
-  const unsigned bits = key_bits(a, w.b, j0, w.len, l32);
+  const unsigned bits = key_bits(key_byte(a, w.b, j0, l32), j0, w.len, l32);
   const bool on = (bits >> l32) & 1u;
   f32x16 dk[DHP / 32], dv[DHP / 32];
 #pragma unroll
@@ -300,30 +353,48 @@ __global__ void __launch_bounds__(64 * PARTS, 1) cross_dkv_f32_kernel(CrossArgs 
     const float* const drow = a.drow + (long)w.pair * a.rows;
     const int nt = (a.rows + 31) / 32;
     const int t0 = (int)((long)nt * w.split / a.splits), t1 = (int)((long)nt * (w.split + 1) / a.splits);
+    float* const tile = lds + part * TILE;
+    float* const values = lds + PARTS * TILE + part * 64;        // lse of the tile's rows, then D
+    f32x4 qf[DHP / 8], dof[DHP / 8];
+    auto row_of = [&](int t) __attribute__((always_inline)) { return min(32 * t + l32, a.rows - 1); };
+    float value = 0.f;                                           // lane l: lse of row l, lane 32 + l: D
+    if (t0 + part < t1) {
+      const int i = row_of(t0 + part);
+      value = (g ? drow : lrow)[i];
+      load_rows<DHP>(qb + row_offset(a.sq, a.group, i), a.dh, g, qf);
+      load_rows<DHP>(dob + row_offset(a.sdo, a.group, i), a.dh, g, dof);
+    }
     for (int t = t0 + part; t < t1; t += PARTS) {
-      const int i0 = 32 * t, left = a.rows - i0, ir = min(i0 + l32, a.rows - 1);
-      const unsigned rbits = left >= 32 ? ALL : (1u << left) - 1u;
-      f32x16 p, ds;
-      {
-        f32x4 xf[DHP / 8];
-        load_rows<DHP>(qb + row_offset(a.sq, a.group, ir), a.dh, g, xf);
-        p = row_product<DHP>(xf, kf);                            // S[i][j]
-        if (DHP > 64) __builtin_amdgcn_sched_barrier(0);         // one operand in registers at a time
-        load_rows<DHP>(dob + row_offset(a.sdo, a.group, ir), a.dh, g, xf);
-        ds = row_product<DHP>(xf, vf);                           // dP[i][j]
-      }
+      const int left = a.rows - 32 * t;
+      const bool more = t + PARTS < t1, counts = l32 < left;
+      values[lane] = value;
+      f32x16 p = row_product<DHP>(qf, kf);                       // S[i][j]
+      __builtin_amdgcn_sched_barrier(0);
+      f32x16 ds = row_product<DHP>(dof, vf);                     // dP[i][j]
+      __builtin_amdgcn_sched_barrier(0);
+      put_rows<DHP>(tile, dof, counts, g, l32);
 #pragma unroll
-      for (int v = 0; v < 16; v++) {
-        const int i = min(i0 + acc_row(v, g), a.rows - 1);
-        p[v] = bit_of(rbits, v, g) ? expf(p[v] * a.scale - lrow[i]) : 0.f;
-        ds[v] = bit_of(rbits, v, g) ? p[v] * (ds[v] - drow[i]) : 0.f;
+      for (int q = 0; q < 4; q++) {
+        const f32x4 lse = *reinterpret_cast<const f32x4*>(values + 8 * q + 4 * g);
+        const f32x4 dd = *reinterpret_cast<const f32x4*>(values + 32 + 8 * q + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const int v = 4 * q + e, i = acc_row(v, g);
+          p[v] = i < left ? expf(p[v] * a.scale - lse[e]) : 0.f;
+          ds[v] = i < left ? p[v] * (ds[v] - dd[e]) : 0.f;
+        }
       }
-      if (DHP >= 64) __builtin_amdgcn_sched_barrier(0);
-      col_product<DHP>(dv, p, [&](int v) { return dob + row_offset(a.sdo, a.group, min(i0 + acc_row(v, g), a.rows - 1)); }, rbits,
-                       a.dh, g, l32);
-      if (DHP > 64) __builtin_amdgcn_sched_barrier(0);
-      col_product<DHP>(dk, ds, [&](int v) { return qb + row_offset(a.sq, a.group, min(i0 + acc_row(v, g), a.rows - 1)); }, rbits,
-                       a.dh, g, l32);
+      col_product<DHP>(dv, p, tile, g, l32);
+      __builtin_amdgcn_sched_barrier(0);
+      put_rows<DHP>(tile, qf, counts, g, l32);
+      if (more) {                                                // the next tile's are on their way during the rest of this one
+        const int next = row_of(t + PARTS);
+        value = (g ? drow : lrow)[next];
+        load_rows<DHP>(dob + row_offset(a.sdo, a.group, next), a.dh, g, dof);
+        load_rows<DHP>(qb + row_offset(a.sq, a.group, next), a.dh, g, qf);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      col_product<DHP>(dk, ds, tile, g, l32);
     }
   }
   merge_parts(dk, lds, part, lane);
@@ -344,10 +415,23 @@ __global__ void __launch_bounds__(64 * PARTS, 1) cross_dkv_f32_kernel(CrossArgs 
   store_column<DHP>(dv, static_cast<float*>(a.dv) + pair_offset(a.sdv, w.b, w.kh) + (long)j * a.sdv.t, 1.0f, a.dh, g);
 }
 
-int parts(long blocks, long units, long want, long least) {
-  long n = blocks >= want || blocks == 0 ? 1 : want / blocks;
-  if (n > units / least) n = units / least;
-  return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+// Parts of a launch, by an estimate in microseconds: a workgroup takes 4 and `alone` for each 32 x 32 tile of a wavefront's
+// share, `pair` where two share a compute unit (0: one at a time); a launch of its own joins parts, which are written and read.
+struct Tile { double alone, pair; };
+int best_parts(const Tile& c, long blocks, long units, double part_mb) {
+  int best = 1;
+  double least = 0.0;
+  for (const int p : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+    if (p > 1 && units < 2 * p) break;
+    const long n = cdiv(blocks * p, 256), per = cdiv(cdiv(units, p), PARTS);
+    double t = c.pair > 0 ? (n / 2) * (4.0 + per * c.pair) + (n % 2) * (4.0 + per * c.alone) : n * (4.0 + per * c.alone);
+    if (p > 1) t += 3.5 + 0.04 * p + p * part_mb / 4.0;
+    if (p == 1 || t < least) {
+      least = t;
+      best = p;
+    }
+  }
+  return best;
 }
 
 #define GX_CROSS_F32(KERNEL, TILES)                                                                       \
@@ -362,7 +446,12 @@ int parts(long blocks, long units, long want, long least) {
 
 int cross_parts_f32(const CrossArgs& a, int pass) {
   const long pairs = (long)a.B * a.hk;
-  return pass < 2 ? parts(pairs * cdiv(a.rows, 32), cdiv(a.Sk, 32), 512, 8) : parts(pairs * cdiv(a.Sk, 32), cdiv(a.rows, 32), 256, 8);
+  constexpr Tile COST[3][3] = {{{2.3, 3.3}, {3.0, 4.5}, {3.6, 5.5}},           // forward, dQ, dK / dV at head dims up to 32
+                               {{4.5, 6.5}, {6.0, 9.0}, {7.2, 11.0}},          // 64
+                               {{5.7, 0.0}, {7.5, 0.0}, {11.0, 0.0}}};         // 128
+  const Tile& c = COST[a.dh <= 32 ? 0 : a.dh <= 64 ? 1 : 2][pass];
+  return pass == 2 ? best_parts(c, pairs * cdiv(a.Sk, 32), cdiv(a.rows, 32), pairs * a.Sk * a.dh * 16e-6)
+                   : best_parts(c, pairs * cdiv(a.rows, 32), cdiv(a.Sk, 32), pairs * a.rows * a.dh * 8e-6);
 }
 
 hipError_t cross_fwd_f32(const CrossArgs& args, hipStream_t s) {
