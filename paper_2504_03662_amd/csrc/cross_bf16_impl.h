@@ -503,13 +503,16 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, NQ * SPLIT == 4 ? 2 : 1) cros
     }
   };
   load(0);
-  float d4[4] = {0.f, 0.f, 0.f, 0.f};
+  // D on the matrix pipe, in dP's own order of summation: a row with one key has o = v to the bit, and its dS is exactly zero
+  float dd = 0.f;
+  {
+    f32x16 all = zero16();
 #pragma unroll
-  for (int x = 0; x < DH / 16; x++)
+    for (int x = 0; x < DH / 16; x++) all = MFMA(of[x], dof[x], all);
 #pragma unroll
-    for (int e = 0; e < 8; e++) d4[e & 3] = __builtin_fmaf((float)of[x][e], (float)dof[x][e], d4[e & 3]);
-  float dd = (d4[0] + d4[1]) + (d4[2] + d4[3]);
-  dd += __shfl_xor(dd, 32, 64);
+    for (int v = 0; v < 16; v++) dd = 8 * (v >> 2) + 4 * g + (v & 3) == l32 ? all[v] : dd;      // the diagonal, in one of a column's lanes
+    dd += __shfl_xor(dd, 32, 64);
+  }
   if (w.split == 0 && part == 0 && g == 0 && r < a.rows) {
     a.drow[(long)w.pair * a.rows + r] = dd;
     a.lrow[(long)w.pair * a.rows + r] = lse2;

@@ -268,14 +268,14 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dq_f32_ke
   f32x4 qf[DHP / 8], dof[DHP / 8];
   load_rows<DHP>(f32_of(a.q) + pair_offset(a.sq, w.b, head0) + row_offset(a.sq, a.group, rc), a.dh, g, qf);
   load_rows<DHP>(f32_of(a.d_o) + pair_offset(a.sdo, w.b, head0) + row_offset(a.sdo, a.group, rc), a.dh, g, dof);
+  // D in dP's own order of summation: a row with one key has o = v to the bit, and its dS is exactly zero
   float dd = 0.f;
   {
     f32x4 of[DHP / 8];
     load_rows<DHP>(f32_of(a.o) + pair_offset(a.so, w.b, head0) + row_offset(a.so, a.group, rc), a.dh, g, of);
+    const f32x16 all = row_product<DHP>(of, dof);
 #pragma unroll
-    for (int c = 0; c < DHP / 8; c++)
-#pragma unroll
-      for (int e = 0; e < 4; e++) dd = fmaf(dof[c][e], of[c][e], dd);
+    for (int v = 0; v < 16; v++) dd = acc_row(v, g) == l32 ? all[v] : dd;       // the diagonal, in one of a column's lanes
   }
   dd += __shfl_xor(dd, 32, 64);
   const int i = rc / a.group, h = head0 + (rc - i * a.group);
