@@ -28,6 +28,42 @@ GX_DEVINL int keys_of(const CrossArgs& a, int b) {
   const int n = a.key_lens ? a.key_lens[b] : a.Sk;
   return __builtin_amdgcn_readfirstlane(n < 0 ? 0 : n > a.Sk ? a.Sk : n);
 }
+// The sample that takes its turn `rank`-th when the longest go first, so that a launch of several rounds ends with short ones
+// (4 samples of 1501 .. 938 keys, 2048 queries of 16 heads of 128: forward 99 and dQ 137 us, in the samples' order 106 and 151).  Every
+// wavefront sorts the lengths for itself, a lane to a sample.
+GX_DEVINL int sample_by_length(const CrossArgs& a, int rank) {
+  const int lane = threadIdx.x & 63;
+  const int n = lane < a.B ? a.key_lens[lane] : 0;
+  int before = 0;
+  for (int m = 0; m < a.B; m++) {
+    const int other = __builtin_amdgcn_readlane(n, m);
+    before += other > n || (other == n && m < lane) ? 1 : 0;
+  }
+  return __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < a.B && before == rank));
+}
+// Pair, row block and split of a workgroup of a launch over `blocks` row blocks of every pair.  Pairs go round the chip, so that a pair's
+// workgroups share an L2 where the pairs (key heads, with lengths) are a multiple of 8.
+struct Share { int b, kh, pair, block, split; };
+GX_DEVINL Share share_of(const CrossArgs& a, int blk, int blocks) {
+  Share x;
+  if (a.key_lens && a.B <= 64) {
+    x.kh = blk % a.hk;
+    int rest = blk / a.hk;
+    x.block = rest % blocks;
+    rest /= blocks;
+    x.split = rest % a.splits;
+    x.b = a.B == 1 ? 0 : __builtin_amdgcn_readfirstlane(sample_by_length(a, rest / a.splits));
+    x.pair = x.b * a.hk + x.kh;
+  } else {
+    const int npair = a.B * a.hk, rest = blk / npair;
+    x.pair = blk % npair;
+    x.block = rest % blocks;
+    x.split = rest / blocks;
+    x.kh = x.pair % a.hk;
+    x.b = x.pair / a.hk;
+  }
+  return x;
+}
 // element offset of row r of a pair's group of heads
 GX_DEVINL long row_offset(const HeadStrides& s, int group, int r) {
   const int i = (int)((unsigned)r / (unsigned)group);

@@ -101,13 +101,12 @@ struct RowBlock {
   template <int BQ, int ROWS>
   GX_DEVINL static RowBlock of(const CrossArgs& a, int blk) {
     RowBlock w;
-    const int npair = a.B * a.hk, nb = (a.rows + BQ - 1) / BQ;
-    w.pair = blk % npair;                        // pairs go round the chip: a pair's blocks share an L2 where npair is a multiple of 8
-    const int rest = blk / npair;
-    w.i0 = (rest % nb) * BQ;
-    w.split = rest / nb;
-    w.kh = w.pair % a.hk;
-    w.b = w.pair / a.hk;
+    const Share x = share_of(a, blk, (a.rows + BQ - 1) / BQ);
+    w.b = x.b;
+    w.kh = x.kh;
+    w.pair = x.pair;
+    w.i0 = x.block * BQ;
+    w.split = x.split;
     const int n = keys_of(a, w.b), nt = (n + ROWS - 1) / ROWS;
     const int t0 = (int)((long)nt * w.split / a.splits), t1 = (int)((long)nt * (w.split + 1) / a.splits);
     w.key0 = t0 * ROWS;

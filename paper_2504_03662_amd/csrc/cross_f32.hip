@@ -119,12 +119,12 @@ GX_DEVINL void store_column(const f32x16 (&acc)[DHP / 32], float* dst, float sca
 struct Where {
   int b, kh, pair, tile, split, len;
   GX_DEVINL Where(const CrossArgs& a, int tiles) {
-    const int npair = a.B * a.hk, rest = blockIdx.x / npair;
-    pair = blockIdx.x % npair;
-    tile = rest % tiles;
-    split = rest / tiles;
-    kh = pair % a.hk;
-    b = pair / a.hk;
+    const Share x = share_of(a, blockIdx.x, tiles);
+    b = x.b;
+    kh = x.kh;
+    pair = x.pair;
+    tile = x.block;
+    split = x.split;
     len = keys_of(a, b);
   }
 };
