@@ -235,6 +235,11 @@ GX_DEVINL void fwd_finish(const CrossArgs& a, const RowBlock& w, char* smem, f32
 // of the next one (S, t + 1) are issued one by one, behind each its share of the softmax of step t; K(t + 2) and V(t) are
 // requested in its first slots into two buffers each.  The reference exponent follows a row's maximum only when that exceeds it by
 // more than 2^8, so that O is rescaled rarely (following every rise, 128 pairs of 2048 x 2048 took 338 us instead of 301).
+// Arithmetic: base-2 exponentials of fp32 scores, sums of them in fp32 before P is rounded to bf16 for the product with V (an
+// error of the size that V's own type has), O in fp32 until it is stored.
+// Bound by the issue of matrix and vector instructions where there are rows: a product takes 31 ns of a SIMD with its share of the
+// softmax, 15 alone (2 x 4096 x 4096, 32 / 8 heads of 128: 500 us, 1.1 PFLOP/s, a library product 1.53); by memory where there are
+// few (one query of 40 heads, 16 x 8192 keys of 8 heads: 105 us, 5.1 TB/s).
 template <int NQ, int SPLIT, int BKV, bool MASK>
 __global__ void __launch_bounds__(64 * NQ * SPLIT, 2) cross_fwd_kernel(CrossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -453,7 +458,10 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, 2) cross_fwd_kernel(CrossArgs
 }
 
 // ------------------------------------------------------------------------------- backward: dQ
-// Rows as in the forward kernel.  Also forms D = rowsum(dO * O) and leaves D and lse * log2(e) in row order for the other
+// Rows as in the forward kernel.  dS = P (dP - D) is rounded to bf16 once, as an operand.  D is taken from o as it was stored: the
+// rounding of o, 2^-8 of |dO| |o| at most, stays in the dS of rows with few keys, and no further pass over the keys is needed.
+// 2 x 4096 x 4096, 32 / 8 heads of 128: 750 us, 1.1 PFLOP/s; a product takes 30 ns of a SIMD.
+// Also forms D = rowsum(dO * O) and leaves D and lse * log2(e) in row order for the other
 // kernel (the first split does); a row without a key gets +inf there, so that its probabilities are 0.
 template <int NQ, int SPLIT, int BKV, bool MASK>
 __global__ void __launch_bounds__(64 * NQ * SPLIT, NQ * SPLIT == 4 ? 2 : 1) cross_dq_kernel(CrossArgs a) {
@@ -509,7 +517,7 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, NQ * SPLIT == 4 ? 2 : 1) cros
 #pragma unroll
     for (int x = 0; x < DH / 16; x++) all = MFMA(of[x], dof[x], all);
 #pragma unroll
-    for (int v = 0; v < 16; v++) dd = 8 * (v >> 2) + 4 * g + (v & 3) == l32 ? all[v] : dd;      // the diagonal, in one of a column's lanes
+    for (int v = 0; v < 16; v++) dd = 8 * (v >> 2) + 4 * g + (v & 3) == l32 ? all[v] : dd;      // the diagonal, in one half
     dd += __shfl_xor(dd, 32, 64);
   }
   if (w.split == 0 && part == 0 && g == 0 && r < a.rows) {
@@ -603,9 +611,10 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, NQ * SPLIT == 4 ? 2 : 1) cros
 // forms S = Q K^T, the probabilities P and dV += P^T dO, role K dP = dO V^T, dS = P (dP - D) and dK += dS^T Q, a tile behind.
 // A wavefront's stream mixes the first products of its next sub-tile with the vector work of the present one.  One
 // workgroup of 8 wavefronts fills a compute unit; wavefronts w and w + 4 share a SIMD, one of either role.
-// P crosses through LDS in 16
-// bits: 0 <= P < 2, so an fp32 P has two leading zero bits, and the next 16 (7 of the exponent, 9 of the mantissa, rounded) say P to
-// 2^-10 over the whole range: dS is then rounded to bf16 once, not twice.
+// 2 x 4096 x 4096, 32 / 8 heads of 128: 1080 us, 1.0 PFLOP/s; 4 x 2048 x 1501 .. 938, 16 heads: 219 us, of which the last of three
+// rounds fills 112 of 256 compute units.
+// P crosses through LDS in 16 bits: 0 <= P < 2, so an fp32 P has two leading zero bits, and the next 16 (7 of the exponent, 9 of
+// the mantissa, rounded) say P to 2^-10 over the whole range: dS is then rounded to bf16 once, not twice.
 // Keys that do not count are columns of their own in S and dP and rows of their own in dK and dV: whatever
 // their lanes compute stays there, and zeros are stored.
 constexpr int KV_PAIRS = 4, KV_NW = 2 * KV_PAIRS, KV_BJ = 32 * KV_PAIRS, KV_SUB = 2, KV_BI = 32 * KV_SUB;
@@ -1076,7 +1085,8 @@ hipError_t go_dq(const CrossArgs& a, hipStream_t s) {
     configured = true;
   }
   const dim3 grid((unsigned)(pairs_of(a) * cdiv(a.rows, 32 * NQ) * a.splits));
-  hipLaunchKernelGGL((cross_dq_kernel<NQ, SPLIT, BKV, MASK>), grid, dim3(64 * NQ * SPLIT), TILES + mask_smem(a, a.splits, ROWS), s, a);
+  hipLaunchKernelGGL((cross_dq_kernel<NQ, SPLIT, BKV, MASK>), grid, dim3(64 * NQ * SPLIT),
+                     TILES + mask_smem(a, a.splits, ROWS), s, a);
   return hipGetLastError();
 }
 // dQ with D, then dK / dV

@@ -6,6 +6,10 @@
 // and every piece adds up its runs of equal rows: a run that lies inside a piece is stored, one that crosses the piece's ends leaves
 // a partial sum, and the partial sums of a run are added in order afterwards.  No floating-point atomics; the order of every
 // sum depends on sizes and ids alone.
+// Both directions are bound by memory (a large copy moves 5.0 TB/s on these chips, read and written): 8192 tokens of 2048 columns
+// (bf16) look up in 15.5 us (4.3 TB/s) and, with 32768 rows of which most are cleared, get their gradient in 72 us (268 MB of
+// fp32 gradient alone take 54); 16385 tokens of 4096, half of them of this shard, a quarter padding, 64013 rows: 33 to 41 and 217 us
+// (1.05 GB of gradient take 210).  Few tokens cost the launches: 257 tokens, 1001 rows of 256 (fp32) 2.5 and 15 us.
 #include "../../include/gx.h"
 #include "gx_kernels.h"
 
@@ -246,7 +250,8 @@ GX_DEVINL void put_row(float* dst, const float (&s)[V], float scale, bool accumu
 }
 
 // The first workgroups: `lpr` lanes own a piece of the sorted tokens and 16 bytes of every row each.  The others clear the
-// rows to which no token points, so that the one's reads and the other's writes share the memory's time.
+// rows to which no token points, so that the one's reads and the other's writes share the memory's time (8192 tokens of 2048
+// columns, 32768 rows: 43 to 55 us).
 template <typename T>
 __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a, int lpr_log, int col_blocks) {
   constexpr int V = Lanes<T>::N;
@@ -311,7 +316,8 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a, int lpr_log, 
 }
 
 // One workgroup per piece and 256 columns: if a run begins in the piece and goes on behind it, adds the run's partial sums.  Each
-// wavefront takes a consecutive quarter of them, and the quarters are added in order.
+// wavefront takes a consecutive quarter of them, and the quarters are added in order.  The most frequent token of a text has hundreds
+// of pieces: 7 us at 8192 tokens.
 __global__ void __launch_bounds__(256) embed_join_kernel(SumArgs a) {
   __shared__ f32x4 red[3][64];
   const int p = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.y * 64 + lane;
