@@ -312,8 +312,8 @@ gx_status gx_params_merge(const gx_layer_cfg* cfg, const gx_params* shard, const
  * no gradient.
  *   ids [tokens] : int32 or int64 (id_bytes 4 or 8), aligned to itself       table [rows, hidden], y, dy [tokens, hidden] : dtype
  *   dtable [rows, hidden] fp32, written whole (zeros where no token points) or, with GX_ACCUM_WGRAD, added to.
- * Products and sums are fp32, y is rounded once.  A row's tokens are added in ascending order within fixed pieces of the
- * sorted tokens, pieces in order: the same bits for the same sizes and ids.
+ * Products and sums are fp32, y is rounded once.  A row's tokens are added in ascending order within pieces that follow from
+ * the sizes and ids alone, pieces in order: the same bits for the same sizes and ids.
  * tokens may be 0.  hidden must be a multiple of 8 (bf16) or 4 (fp32), at most 65536; rows and tokens at most 2^24.
  * gx_embed_bwd needs gx_embed_workspace_bytes(cfg) bytes of scratch (0 for an invalid cfg), which grow with the
  * tokens and with hidden.  Errors: GX_ERR_NULL, GX_ERR_SHAPE, GX_ERR_DIVIS, GX_ERR_DTYPE (dtype, id_bytes),

@@ -9,7 +9,7 @@
 // Both directions are bound by memory (a large copy moves 5.0 TB/s on these chips, read and written): 8192 tokens of 2048 columns
 // (bf16) look up in 15.5 us (4.3 TB/s) and, with 32768 rows of which most are cleared, get their gradient in 72 us (268 MB of
 // fp32 gradient alone take 54); 16385 tokens of 4096, half of them of this shard, a quarter padding, 64013 rows: 33 to 41 and 217 us
-// (1.05 GB of gradient take 210).  Few tokens cost the launches: 257 tokens, 1001 rows of 256 (fp32) 2.5 and 15 us.
+// (1.05 GB of gradient take 210).  Few tokens cost the launches: 257 tokens, 1001 rows of 256 (fp32) 2.5 and 3.7 us.
 #include "../../include/gx.h"
 #include "gx_kernels.h"
 
@@ -344,6 +344,125 @@ __global__ void __launch_bounds__(256) embed_join_kernel(SumArgs a) {
   put_row<4>(a.dtable + (size_t)key * a.hidden + (size_t)c * 4, v, a.scale, a.accumulate);
 }
 
+// ------------------------------------------------------------------------------- backward: few tokens
+// One launch: every workgroup owns `span` consecutive rows of the table, 64 lanes' columns of them, and looks at all ids.  A wavefront
+// takes every 4th row: it lists the row's tokens in order (ballots over the ids that its lanes hold) and adds them up, or clears the row; rows
+// with more than HOT tokens come after that, a quarter of the tokens to a wavefront, and the quarters are added in order.
+// us, this / by sorted tokens: 257 tokens, 1001 rows of 256 (fp32) 3.7 / 14.5; 48 tokens, 97749 x 576 (bf16) 33.9 / 42.9; 512 tokens, 300000
+// x 64 22.4 / 27.5; 512 tokens, 32000 x 4096 108.3 / 107.4 (a copy's rate for the table's gradient); 512 tokens all alike, 500 x 8192
+// (fp32) 23.3 / 17.0, 1001 x 256 11.0 / 13.5.  More tokens would make rows that all of them share a long sum, and ids a long list.
+constexpr int FEW_TOKENS = 512, FEW_CHUNKS = FEW_TOKENS / 64, FEW_ROWS = 32, HOT = 16;
+template <typename I>
+struct FewArgs {
+  Ids<I> ids;
+  long pad_row;                    // relative to the shard, -1: none
+  const void* dy;
+  float* dtable;
+  int tokens, hidden, rows, span, accumulate;
+  float scale;
+};
+// adds chunk c of the tokens list[from .. to), AT_ONCE of them requested together
+template <typename T, int AT_ONCE>
+GX_DEVINL void sum_listed(float (&s)[Lanes<T>::N], const T* dy, const unsigned short* list, int from, int to, int hidden, int c) {
+  constexpr int V = Lanes<T>::N;
+  typedef typename Lanes<T>::type Raw;
+#pragma unroll
+  for (int e = 0; e < V; e++) s[e] = 0.f;
+  for (int i = from; i < to; i += AT_ONCE) {
+    Raw x[AT_ONCE];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; u++)
+      x[u] = *reinterpret_cast<const Raw*>(dy + (size_t)list[min(i + u, to - 1)] * hidden + (size_t)c * V);
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; u++)
+      if (i + u < to)
+#pragma unroll
+        for (int e = 0; e < V; e++) s[e] += to_f32(x[u][e]);
+  }
+}
+template <typename T, typename I>
+__global__ void __launch_bounds__(256) embed_few_kernel(FewArgs<I> a) {
+  constexpr int V = Lanes<T>::N;
+  __shared__ int row_of[FEW_TOKENS];
+  __shared__ unsigned short lists[4][FEW_TOKENS];
+  __shared__ int counts[FEW_ROWS];
+  __shared__ float red[3][V][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long first = (long)blockIdx.x * a.span;
+  const int rows = (int)min((long)a.span, a.rows - first), chunks = a.hidden / V, c = blockIdx.y * 64 + lane;
+  bool some = false;
+#pragma unroll
+  for (int k = 0; k < FEW_TOKENS / 256; k++) {
+    const int t = threadIdx.x + 256 * k;
+    long r = -1;
+    if (t < a.tokens) {
+      r = a.ids.row(t);
+      if (r == a.pad_row) r = -1;
+    }
+    const bool own = r >= first && r < first + rows;
+    row_of[t] = own ? (int)(r - first) : -1;
+    some |= own;
+  }
+  float* const table = a.dtable + first * a.hidden;
+  if (!__syncthreads_or(some)) {
+    if (a.accumulate) return;
+    if (gridDim.y == 1) {
+      for (int i = threadIdx.x; i < rows * (a.hidden / 4); i += 256) reinterpret_cast<f32x4*>(table)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      return;
+    }
+    constexpr int W = 64 * V / 4;                                // 16 bytes of fp32 at a time
+    const int at = blockIdx.y * W + threadIdx.x % W;
+    if (at < a.hidden / 4)
+      for (int r = threadIdx.x / W; r < rows; r += 256 / W)
+        reinterpret_cast<f32x4*>(table + (size_t)r * a.hidden)[at] = f32x4{0.f, 0.f, 0.f, 0.f};
+    return;
+  }
+  int mine[FEW_CHUNKS];
+#pragma unroll
+  for (int k = 0; k < FEW_CHUNKS; k++) mine[k] = row_of[64 * k + lane];
+  unsigned short* const list = lists[wave];
+  auto list_tokens = [&](int r) __attribute__((always_inline)) {
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < FEW_CHUNKS; k++) {
+      const bool it = mine[k] == r;
+      const unsigned long long m = __builtin_amdgcn_ballot_w64(it);
+      if (it) list[n + __popcll(m & ((1ull << lane) - 1))] = (unsigned short)(64 * k + lane);
+      n += __popcll(m);
+    }
+    __builtin_amdgcn_wave_barrier();
+    return n;
+  };
+  const T* const dy = static_cast<const T*>(a.dy);
+  float s[V];
+  for (int r = wave; r < rows; r += 4) {
+    const int n = list_tokens(r);
+    if (lane == 0) counts[r] = n;
+    if (n > HOT || (n == 0 && a.accumulate)) continue;
+    if (c >= chunks) continue;
+    sum_listed<T, 4>(s, dy, list, 0, n, a.hidden, c);               // of no token: zeros
+    put_row<V>(table + (size_t)r * a.hidden + (size_t)c * V, s, a.scale, a.accumulate);
+  }
+  __syncthreads();
+  for (int r = 0; r < rows; r++) {
+    if (counts[r] <= HOT) continue;                              // the same for all
+    const int n = list_tokens(r), per = (n + 3) / 4, from = min(wave * per, n), to = min(from + per, n);
+    sum_listed<T, 16>(s, dy, list, from, to, a.hidden, min(c, chunks - 1));
+    if (wave > 0)
+#pragma unroll
+      for (int e = 0; e < V; e++) red[wave - 1][e][lane] = s[e];
+    __syncthreads();
+    if (wave == 0 && c < chunks) {
+#pragma unroll
+      for (int w = 0; w < 3; w++)
+#pragma unroll
+        for (int e = 0; e < V; e++) s[e] += red[w][e][lane];
+      put_row<V>(table + (size_t)r * a.hidden + (size_t)c * V, s, a.scale, a.accumulate);
+    }
+    __syncthreads();
+  }
+}
+
 // ------------------------------------------------------------------------------- host
 int lanes_log(int chunks) {
   int l = 3;
@@ -439,13 +558,29 @@ gx_status gx_embed_bwd(const gx_embed_cfg* cfg, const void* ids, const void* dy,
   if (!device_is_gfx950()) return GX_ERR_ARCH;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const bool accumulate = cfg->flags & GX_ACCUM_WGRAD, bf = cfg->dtype == GX_BF16;
+  const long pad_row = cfg->pad_id < 0 ? -1 : (long)(cfg->pad_id - cfg->first_row);
+  if (cfg->tokens <= FEW_TOKENS) {
+    // about 2048 workgroups, or more of 32 rows
+    const int cols = cdiv(cfg->hidden, bf ? 512 : 256);
+    const long even = (long)cfg->rows * cols / 2048;
+    const int span = even < 1 ? 1 : even > FEW_ROWS ? FEW_ROWS : (int)even;
+    auto go = [&](auto type, auto id) {
+      typedef decltype(type) T;
+      typedef decltype(id) I;
+      const FewArgs<I> a{ids_of<I>(*cfg, ids), pad_row, dy, dtable, cfg->tokens, cfg->hidden, cfg->rows, span, accumulate, cfg->scale};
+      hipLaunchKernelGGL((embed_few_kernel<T, I>), dim3(cdiv(cfg->rows, span), cols), dim3(256), 0, s, a);
+    };
+    if (cfg->id_bytes == 8) bf ? go(bf16(), 0l) : go(0.f, 0l);
+    else bf ? go(bf16(), 0) : go(0.f, 0);
+    return launched();
+  }
   const Plan p = plan_of(*cfg);
   char* ws = static_cast<char*>(workspace);
   auto u32 = [&](size_t at) { return reinterpret_cast<unsigned*>(ws + at); };
   auto sort = [&](auto id) {
     typedef decltype(id) I;
-    const SortArgs<I> a{ids_of<I>(*cfg, ids), cfg->pad_id < 0 ? -1 : (long)(cfg->pad_id - cfg->first_row), cfg->tokens, p.span,
-                        p.span_log, u32(p.list_key), u32(p.list_tok), u32(p.key), u32(p.tok), u32(p.start)};
+    const SortArgs<I> a{ids_of<I>(*cfg, ids), pad_row, cfg->tokens, p.span, p.span_log,
+                        u32(p.list_key), u32(p.list_tok), u32(p.key), u32(p.tok), u32(p.start)};
     hipLaunchKernelGGL(embed_sort_kernel<I>, dim3(cdiv(cfg->rows, p.span)), dim3(SORT_THREADS), 0, s, a);
   };
   cfg->id_bytes == 8 ? sort(0l) : sort(0);
