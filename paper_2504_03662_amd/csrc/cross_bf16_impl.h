@@ -98,6 +98,7 @@ constexpr float NO_KEY = -3.0e38f;
 // What a workgroup of the forward or dQ kernel works on
 struct RowBlock {
   int b, kh, pair, split, i0, key0, len;         // len: keys from key0 on
+  bool one;                                      // the sample has one step of keys at most, and the last split gets it
   template <int BQ, int ROWS>
   GX_DEVINL static RowBlock of(const CrossArgs& a, int blk) {
     RowBlock w;
@@ -109,6 +110,7 @@ struct RowBlock {
     w.split = x.split;
     const int n = keys_of(a, w.b), nt = (n + ROWS - 1) / ROWS;
     const int t0 = (int)((long)nt * w.split / a.splits), t1 = (int)((long)nt * (w.split + 1) / a.splits);
+    w.one = nt <= 1;
     w.key0 = t0 * ROWS;
     w.len = (t1 * ROWS < n ? t1 * ROWS : n) - w.key0;
     if (w.len < 0) w.len = 0;
@@ -459,7 +461,9 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, 2) cross_fwd_kernel(CrossArgs
 
 // ------------------------------------------------------------------------------- backward: dQ
 // Rows as in the forward kernel.  dS = P (dP - D) is rounded to bf16 once, as an operand.  D is taken from o as it was stored: the
-// rounding of o, 2^-8 of |dO| |o| at most, stays in the dS of rows with few keys, and no further pass over the keys is needed.
+// rounding of o, 2^-8 of |dO| |o| at most, stays in dS, beside dS's own rounding the smaller the more keys share a row, and no further
+// pass over the keys is needed.  Where one step holds all the keys D is made exact first: a row's dS add up to what it lacks
+// (two keys: dQ and dK off by 0.0024 of their norm, 0.0039 without; 8 x 2000 x 30, 16 / 4 heads of 64: 2 us of 59).
 // 2 x 4096 x 4096, 32 / 8 heads of 128: 750 us, 1.1 PFLOP/s; a product takes 30 ns of a SIMD.
 // Also forms D = rowsum(dO * O) and leaves D and lse * log2(e) in row order for the other
 // kernel (the first split does); a row without a key gets +inf there, so that its probabilities are 0.
@@ -520,12 +524,45 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, NQ * SPLIT == 4 ? 2 : 1) cros
     for (int v = 0; v < 16; v++) dd = 8 * (v >> 2) + 4 * g + (v & 3) == l32 ? all[v] : dd;      // the diagonal, in one half
     dd += __shfl_xor(dd, 32, 64);
   }
-  if (w.split == 0 && part == 0 && g == 0 && r < a.rows) {
-    a.drow[(long)w.pair * a.rows + r] = dd;
-    a.lrow[(long)w.pair * a.rows + r] = lse2;
-  }
+  auto leave = [&]() __attribute__((always_inline)) {
+    if (part == 0 && g == 0 && r < a.rows) {
+      a.drow[(long)w.pair * a.rows + r] = dd;
+      a.lrow[(long)w.pair * a.rows + r] = lse2;
+    }
+  };
+  if (w.split == (w.one ? a.splits - 1 : 0) && !(w.one && nt == 1)) leave();
   WAIT_VM0();
   __syncthreads();
+  if (w.one && nt == 1) {                               // all of a row's keys are here: what the first dS add up to goes to D
+    const char* kp = smem + part * BKV * ROWB;
+    const unsigned long long on = bits.template of<BKV>(part * BKV) >> (4 * g);
+    float rest = 0.f;
+#pragma unroll 1
+    for (int jt = 0; jt < NJT; jt++) {
+      f32x16 sc = zero16(), dp = zero16();
+#pragma unroll
+      for (int x = 0; x < DH / 16; x++) {
+        sc = MFMA(frag_rows(kp, 32 * jt + l32, x, g), qf[x], sc);
+        dp = MFMA(frag_rows(kp + ROWS * ROWB, 32 * jt + l32, x, g), dof[x], dp);
+      }
+#pragma unroll
+      for (int v = 0; v < 16; v++) {
+        const float ds = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[v], c2, -lse2)) * (dp[v] - dd);
+        rest += (on >> (32 * jt + 8 * (v >> 2) + (v & 3))) & 1u ? ds : 0.f;
+      }
+    }
+    rest += __shfl_xor(rest, 32, 64);
+    if (SPLIT > 1) {
+      float* const shares = reinterpret_cast<float*>(smem + STAGE);     // the second stage: no tile follows
+      if (g == 0) shares[(part * NQ + qs) * 32 + l32] = rest;
+      __syncthreads();
+      rest = 0.f;
+#pragma unroll
+      for (int pp = 0; pp < SPLIT; pp++) rest += shares[(pp * NQ + qs) * 32 + l32];
+    }
+    dd += rest;
+    leave();
+  }
   for (int t = 0; t < nt; t++) {
     if (t + 1 < nt) load(t + 1);
     const int j0 = t * ROWS + part * BKV;
@@ -954,9 +991,10 @@ long pairs_of(const CrossArgs& a) { return (long)a.B * a.hk; }
 
 // What a launch takes is estimated from its sizes, and the least estimate decides shape and splits.  A workgroup takes `fix` and
 // `step` for each tile, `pair` where two share a compute unit (0: one at a time); keys that nobody else has brought near come
-// at 5.3 TB/s to many workgroups, at 0.63 of that to `busy` of them; parts of a split are written, read and added by a launch of its own.
+// at 5.3 TB/s to many workgroups, at 0.63 of that to `busy` of them; parts of a split are written, read and added by a launch of
+// its own, which costs a small forward pass `join` of 5.5 rather than 3.5 (one query of 16 heads of 64, 1000 keys, whole 8.7, in parts 11.5).
 // Microseconds and MB, from the runs listed below; only their proportions matter.
-struct Shape { int rows, keys; double fix, step, pair, busy; };       // rows of a block, keys of a step
+struct Shape { int rows, keys; double fix, step, pair, busy, join; };       // rows of a block, keys of a step
 double estimate(const Shape& s, long blocks, long steps, int parts, double part_mb, double mb) {
   const long n = cdiv(blocks * parts, 256), per = cdiv(steps, parts);
   double t = s.pair > 0 ? (n / 2) * (s.fix + per * s.pair) + (n % 2) * (s.fix + per * s.step) : n * (s.fix + per * s.step);
@@ -964,7 +1002,7 @@ double estimate(const Shape& s, long blocks, long steps, int parts, double part_
     const double us = mb / (5.3 * (1.0 - exp(-(double)(blocks * parts) / s.busy)));
     if (t < us) t = us;
   }
-  return parts == 1 ? t : t + 3.5 + 0.04 * parts + parts * part_mb / 4.0;
+  return parts == 1 ? t : t + s.join + 0.04 * parts + parts * part_mb / 4.0;
 }
 // the best number of parts of a launch and its estimate
 struct Choice { int shape, parts; double us; };
@@ -988,9 +1026,9 @@ Choice best_parts(int shape, const Shape& s, long blocks, long steps, int least,
 //   16 x 1 x 8192 x 40 / 8 whole (128 workgroups) 173 (1), 140 (2); 8 x 64 x 8192 x 16 / 16 134 (1, 2 parts), 109 (1, 4 parts)
 //   1 x 16 x 4096 x 16 / 4:   12.6 (2, 16 parts), 13.5 (2, 8)        4 x 1 x 512 x 32 / 8: 9.5 (2, whole), 11.8 (2, 4 parts)
 // Head dim 64: 1 x 1024 x 1024 x 12 / 12 11.8 (2), 12.0 (1), 16.3 (0); 4 x 1024 x 1024 x 16 / 16 25.7 (0), 29.0 (1).
-constexpr Shape FWD[3] = {{128, 64, 5.0, DH == 128 ? 1.0 : 0.72, DH == 128 ? 2.1 : 1.15, DH == 128 ? 146 : 290},
-                          {64, 64, 2.5, DH == 128 ? 0.62 : 0.41, DH == 128 ? 1.09 : 0.78, DH == 128 ? 146 : 290},
-                          {32, 128, 3.0, DH == 128 ? 0.85 : 0.5, DH == 128 ? 0.0 : 0.85, DH == 128 ? 100 : 146}};
+constexpr Shape FWD[3] = {{128, 64, 5.0, DH == 128 ? 1.0 : 0.72, DH == 128 ? 2.1 : 1.15, DH == 128 ? 146 : 290, 5.5},
+                          {64, 64, 2.5, DH == 128 ? 0.62 : 0.41, DH == 128 ? 1.09 : 0.78, DH == 128 ? 146 : 290, 5.5},
+                          {32, 128, 3.0, DH == 128 ? 0.85 : 0.5, DH == 128 ? 0.0 : 0.85, DH == 128 ? 100 : 146, 5.5}};
 // Neither here nor below by whether there is a mask, so that one workspace serves both
 Choice fwd_estimate(const CrossArgs& a) {
   const int least = cdiv(a.Sk, MASK_KEYS * 3 / 4) > 1 ? cdiv(a.Sk, MASK_KEYS * 3 / 4) : 1;   // mask bits have their room in LDS
@@ -1007,8 +1045,8 @@ Choice fwd_estimate(const CrossArgs& a) {
 // dQ: 0 <4, 1, 64>: 128 rows, 1 <2, 2, 32>: 64 rows.  Forward and backward, us, shape 0 / 1: 4 x 2048 x 1501 x 16 / 16 381 / 402, 2 x
 // 4096 x 64 x 16 / 8 60.5 / 68.1, 1 x 2048 x 2048 x 16 / 16 141 / 139, 1 x 4096 x 1024 x 8 / 2 91.4 / 88.9; in parts, shape 1: 1 x 1024 x 1024
 // x 8 / 8 whole 55.2, two 56.5, four 64.8; 4 x 40 x 4096 x 16 / 8 four 73.3, two 78.
-constexpr Shape DQ[2] = {{128, 64, 5.0, DH == 128 ? 1.45 : 0.95, DH == 128 ? 2.6 : 1.5, 0},
-                         {64, 64, 3.5, DH == 128 ? 0.95 : 0.65, DH == 128 ? 1.5 : 0.95, 0}};
+constexpr Shape DQ[2] = {{128, 64, 5.0, DH == 128 ? 1.45 : 0.95, DH == 128 ? 2.6 : 1.5, 0, 3.5},
+                         {64, 64, 3.5, DH == 128 ? 0.95 : 0.65, DH == 128 ? 1.5 : 0.95, 0, 3.5}};
 Choice dq_estimate(const CrossArgs& a) {
   const int least = cdiv(a.Sk, MASK_KEYS * 3 / 4) > 1 ? cdiv(a.Sk, MASK_KEYS * 3 / 4) : 1;
   const double part_mb = pairs_of(a) * a.rows * DH * 8e-6;
@@ -1021,7 +1059,7 @@ Choice dq_estimate(const CrossArgs& a) {
 }
 // dK / dV, parts of the rows.  Forward and backward, us: 1 x 1024 x 1024 x 8 / 8 two parts 64.8, four 56.9, six 61.5; 2 x 4096 x 64 x
 // 16 / 8 eight 69.4, sixteen 59.8, 24 70.7; head dim 64, 3 x 3000 x 300 x 16 / 16 whole 94.5, three 88.9, six 97.8.
-constexpr Shape DKV = {KV_BI, KV_BJ, 5.0, DH == 128 ? 1.9 : 1.2, 0.0, 0};
+constexpr Shape DKV = {KV_BI, KV_BJ, 5.0, DH == 128 ? 1.9 : 1.2, 0.0, 0, 3.5};
 Choice dkv_estimate(const CrossArgs& a) {
   return best_parts(0, DKV, pairs_of(a) * cdiv(a.Sk, DKV.keys), cdiv(a.rows, DKV.rows), 1, pairs_of(a) * a.Sk * DH * 16e-6, 0);
 }
