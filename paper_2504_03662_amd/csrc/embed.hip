@@ -6,7 +6,7 @@
 // and every piece adds up its runs of equal rows: a run that lies inside a piece is stored, one that crosses the piece's ends leaves
 // a partial sum, and the partial sums of a run are added in order afterwards.  No floating-point atomics; the order of every
 // sum depends on sizes and ids alone.
-// Both directions are bound by memory (a large copy moves 5.0 TB/s on these chips, read and written): 8192 tokens of 2048 columns
+// Both directions are bound by memory (a large copy moves 5.7 TB/s on these chips, read and written): 8192 tokens of 2048 columns
 // (bf16) look up in 15.5 us (4.3 TB/s) and, with 32768 rows of which most are cleared, get their gradient in 72 us (268 MB of
 // fp32 gradient alone take 54); 16385 tokens of 4096, half of them of this shard, a quarter padding, 64013 rows: 33 to 41 and 217 us
 // (1.05 GB of gradient take 210).  Few tokens cost the launches: 257 tokens, 1001 rows of 256 (fp32) 2.5 and 3.7 us.
