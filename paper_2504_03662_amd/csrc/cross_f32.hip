@@ -1,14 +1,14 @@
 // fp32 cross attention on v_mfma_f32_32x32x2_f32: every product and sum is a full fp32 one, in a fixed order.
 //
 // As in the causal fp32 kernels a workgroup owns 32 rows (forward, dQ) or 32 keys (dK / dV) of a (sample, key head) pair and
-// its 4 wavefronts take every 4th 32-wide tile of the other side; scores are taken transposed to the owner, so that an accumulator
-// register is, as it stands, an operand of the next product (register v of a lane in half g holds tile row 8 (v / 4) + 4 g + v % 4).
+// its 4 wavefronts take every 4th 32-wide tile of the other side, or every wavefront owns 32 and takes all the tiles.  Scores
+// are taken transposed to the owner, so that an accumulator register is, as it stands, an operand of the next product (register v of a lane in half g holds tile row 8 (v / 4) + 4 g + v % 4).
 // Operands come from global memory, requested while the tile before is worked on; where a tile's rows are the second operand of
 // one product and the first of another (dQ, dK / dV) a wavefront puts what it holds of them into LDS and reads columns.  The parts'
 // results are merged through LDS in wavefront order.  Head dimensions up to 128 (multiples of 4) are padded with zeros to 32, 64 or 128.
 // Keys that do not count have bits of a 32-bit word per tile: their scores are left out by selection, and what is read of them
 // is replaced by zeros before it becomes an operand.
-// Bound by the matrix pipe where there are many tiles (2048 x 2048, 16 heads of 128: forward 384 us, 90 TFLOP/s of the 145 that a
+// Bound by the matrix pipe where there are many tiles (2048 x 2048, 16 heads of 128: forward 365 us, 94 TFLOP/s of the 145 that a
 // library product of fp32 reaches; a lone wavefront per SIMD does not overlap its exponentials), by latency where there are few:
 // 3 x 257 x 333, 8 / 4 heads of 64: 16 us, 21 us (dQ) and 33 us (dK / dV in three parts; 40 whole).
 #include "cross.h"
@@ -140,14 +140,16 @@ GX_DEVINL const float* f32_of(const void* p) { return static_cast<const float*>(
 // what exponents are taken relative to while a row has seen no key, or only scores of -inf
 GX_DEVINL float finite_ref(float m) { return m == -INFINITY ? 0.f : m; }
 
-template <int DHP>
+// EACH: every wavefront has 32 rows of its own and goes over all of the keys
+template <int DHP, bool EACH>
 __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_fwd_f32_kernel(CrossArgs a) {
   constexpr int VALS = DHP / 2 + 2;
-  __shared__ float lds[(PARTS - 1) * VALS * 64];
+  __shared__ float lds[EACH ? 1 : (PARTS - 1) * VALS * 64];
   const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5, l32 = lane & 31;
-  const Where w(a, (a.rows + 31) / 32);
-  const int r = 32 * w.tile + l32, rc = r < a.rows ? r : a.rows - 1;
+  constexpr int ROWS = EACH ? 32 * PARTS : 32, STEP = EACH ? 1 : PARTS;
+  const Where w(a, (a.rows + ROWS - 1) / ROWS);
+  const int first = EACH ? 0 : part, r = ROWS * w.tile + (EACH ? 32 * part : 0) + l32, rc = r < a.rows ? r : a.rows - 1;
   f32x4 qf[DHP / 8];
   load_rows<DHP>(f32_of(a.q) + pair_offset(a.sq, w.b, w.kh * a.group) + row_offset(a.sq, a.group, rc), a.dh, g, qf);
   f32x16 o[DHP / 32];
@@ -163,11 +165,11 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_fwd_f32_k
     load_rows<DHP>(kb + (long)min(32 * t + l32, w.len - 1) * a.sk.t, a.dh, g, kf);
   };
   unsigned byte = 0;
-  if (t0 + part < t1) {
-    byte = key_byte(a, w.b, 32 * (t0 + part), l32);
-    load_k(t0 + part);
+  if (t0 + first < t1) {
+    byte = key_byte(a, w.b, 32 * (t0 + first), l32);
+    load_k(t0 + first);
   }
-  for (int t = t0 + part; t < t1; t += PARTS) {
+  for (int t = t0 + first; t < t1; t += STEP) {
     const int j0 = 32 * t;
     const unsigned bits = key_bits(byte, j0, w.len, l32);
     float vf[DHP / 32][16];                                      // columns of the tile's rows, on their way while the scores are taken
@@ -180,9 +182,9 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_fwd_f32_k
     __builtin_amdgcn_sched_barrier(0);
     f32x16 s = row_product<DHP>(kf, qf);                         // S^T[j][i]
     __builtin_amdgcn_sched_barrier(0);
-    if (t + PARTS < t1) {                                        // and these while the output is
-      byte = key_byte(a, w.b, 32 * (t + PARTS), l32);
-      load_k(t + PARTS);
+    if (t + STEP < t1) {                                        // and these while the output is
+      byte = key_byte(a, w.b, 32 * (t + STEP), l32);
+      load_k(t + STEP);
     }
     __builtin_amdgcn_sched_barrier(0);
     float mx = -INFINITY;
@@ -218,27 +220,29 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_fwd_f32_k
 #pragma unroll
       for (int dt = 0; dt < DHP / 32; dt++) o[dt] = mfma(vf[dt][v], s[v], o[dt]);
   }
-  // merge the parts' (m, l, O); a part without a key has m = -inf, l = 0, O = 0 and adds nothing
-  if (part > 0) {
-    float* p = lds + (part - 1) * VALS * 64 + lane;
-    p[0] = m;
-    p[64] = l;
+  if constexpr (!EACH) {
+    // merge the parts' (m, l, O); a part without a key has m = -inf, l = 0, O = 0 and adds nothing
+    if (part > 0) {
+      float* p = lds + (part - 1) * VALS * 64 + lane;
+      p[0] = m;
+      p[64] = l;
 #pragma unroll
-    for (int dt = 0; dt < DHP / 32; dt++)
+      for (int dt = 0; dt < DHP / 32; dt++)
 #pragma unroll
-      for (int v = 0; v < 16; v++) p[(2 + 16 * dt + v) * 64] = o[dt][v];
-  }
-  __syncthreads();
-  if (part > 0) return;
-  for (int pp = 0; pp < PARTS - 1; pp++) {
-    const float* p = lds + pp * VALS * 64 + lane;
-    const float mm = fmaxf(m, p[0]), ref = finite_ref(mm), a0 = expf(m - ref), a1 = expf(p[0] - ref);
-    l = l * a0 + p[64] * a1;
-    m = mm;
+        for (int v = 0; v < 16; v++) p[(2 + 16 * dt + v) * 64] = o[dt][v];
+    }
+    __syncthreads();
+    if (part > 0) return;
+    for (int pp = 0; pp < PARTS - 1; pp++) {
+      const float* p = lds + pp * VALS * 64 + lane;
+      const float mm = fmaxf(m, p[0]), ref = finite_ref(mm), a0 = expf(m - ref), a1 = expf(p[0] - ref);
+      l = l * a0 + p[64] * a1;
+      m = mm;
 #pragma unroll
-    for (int dt = 0; dt < DHP / 32; dt++)
+      for (int dt = 0; dt < DHP / 32; dt++)
 #pragma unroll
-      for (int v = 0; v < 16; v++) o[dt][v] = o[dt][v] * a0 + p[(2 + 16 * dt + v) * 64] * a1;
+        for (int v = 0; v < 16; v++) o[dt][v] = o[dt][v] * a0 + p[(2 + 16 * dt + v) * 64] * a1;
+    }
   }
   l += __shfl_xor(l, 32, 64);
   if (r >= a.rows) return;
@@ -257,14 +261,16 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_fwd_f32_k
 }
 
 // D = rowsum(dO * O), dS = P (dP - D), dQ = scale dS K; leaves D and lse (+inf for a row without a key) in row order
-template <int DHP>
+template <int DHP, bool EACH>
 __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dq_f32_kernel(CrossArgs a) {
   constexpr int TILE = 32 * STRIDE<DHP>;
   __shared__ alignas(16) float lds[PARTS * TILE];
   const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5, l32 = lane & 31;
-  const Where w(a, (a.rows + 31) / 32);
-  const int r = 32 * w.tile + l32, rc = r < a.rows ? r : a.rows - 1, head0 = w.kh * a.group;
+  constexpr int ROWS = EACH ? 32 * PARTS : 32, STEP = EACH ? 1 : PARTS;
+  const Where w(a, (a.rows + ROWS - 1) / ROWS);
+  const int first = EACH ? 0 : part, r = ROWS * w.tile + (EACH ? 32 * part : 0) + l32, rc = r < a.rows ? r : a.rows - 1;
+  const int head0 = w.kh * a.group;
   f32x4 qf[DHP / 8], dof[DHP / 8];
   load_rows<DHP>(f32_of(a.q) + pair_offset(a.sq, w.b, head0) + row_offset(a.sq, a.group, rc), a.dh, g, qf);
   load_rows<DHP>(f32_of(a.d_o) + pair_offset(a.sdo, w.b, head0) + row_offset(a.sdo, a.group, rc), a.dh, g, dof);
@@ -281,7 +287,7 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dq_f32_ke
   const int i = rc / a.group, h = head0 + (rc - i * a.group);
   float lse = a.lse[((long)w.b * a.hk * a.group + h) * a.Sq + i];
   if (lse == -INFINITY) lse = INFINITY;
-  if (w.split == 0 && part == 0 && g == 0 && r < a.rows) {
+  if (w.split == 0 && first == 0 && g == 0 && r < a.rows) {
     a.drow[(long)w.pair * a.rows + r] = dd;
     a.lrow[(long)w.pair * a.rows + r] = lse;
   }
@@ -296,32 +302,32 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dq_f32_ke
   f32x4 kf[DHP / 8], vf[DHP / 8];
   auto row_of = [&](int t) __attribute__((always_inline)) { return (long)min(32 * t + l32, w.len - 1); };
   unsigned byte = 0;
-  if (t0 + part < t1) {
-    byte = key_byte(a, w.b, 32 * (t0 + part), l32);
-    load_rows<DHP>(kb + row_of(t0 + part) * a.sk.t, a.dh, g, kf);
-    load_rows<DHP>(vb + row_of(t0 + part) * a.sv.t, a.dh, g, vf);
+  if (t0 + first < t1) {
+    byte = key_byte(a, w.b, 32 * (t0 + first), l32);
+    load_rows<DHP>(kb + row_of(t0 + first) * a.sk.t, a.dh, g, kf);
+    load_rows<DHP>(vb + row_of(t0 + first) * a.sv.t, a.dh, g, vf);
   }
-  for (int t = t0 + part; t < t1; t += PARTS) {
+  for (int t = t0 + first; t < t1; t += STEP) {
     const unsigned bits = key_bits(byte, 32 * t, w.len, l32);
-    const bool more = t + PARTS < t1;
+    const bool more = t + STEP < t1;
     f32x16 s = row_product<DHP>(kf, qf);                         // S^T[j][i]
     __builtin_amdgcn_sched_barrier(0);
     put_rows<DHP>(tile, kf, (bits >> l32) & 1u, g, l32);
     if (more) {                                                  // on their way during the rest of this tile
-      byte = key_byte(a, w.b, 32 * (t + PARTS), l32);
-      load_rows<DHP>(kb + row_of(t + PARTS) * a.sk.t, a.dh, g, kf);
+      byte = key_byte(a, w.b, 32 * (t + STEP), l32);
+      load_rows<DHP>(kb + row_of(t + STEP) * a.sk.t, a.dh, g, kf);
     }
     __builtin_amdgcn_sched_barrier(0);
     const f32x16 dp = row_product<DHP>(vf, dof);                 // dP^T[j][i]
     __builtin_amdgcn_sched_barrier(0);
-    if (more) load_rows<DHP>(vb + row_of(t + PARTS) * a.sv.t, a.dh, g, vf);
+    if (more) load_rows<DHP>(vb + row_of(t + STEP) * a.sv.t, a.dh, g, vf);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int v = 0; v < 16; v++) s[v] = bit_of(bits, v, g) ? expf(s[v] * a.scale - lse) * (dp[v] - dd) : 0.f;
     col_product<DHP>(dq, s, tile, g, l32);
   }
-  merge_parts(dq, lds, part, lane);
-  if (part != 0 || r >= a.rows) return;
+  if constexpr (!EACH) merge_parts(dq, lds, part, lane);
+  if (first != 0 || r >= a.rows) return;
   if (a.splits > 1) store_column<DHP>(dq, a.part + (((long)w.split * a.B * a.hk + w.pair) * a.rows + r) * a.dh, 1.0f, a.dh, g);
   else store_column<DHP>(dq, static_cast<float*>(a.dq) + pair_offset(a.sdq, w.b, head0) + row_offset(a.sdq, a.group, r), a.scale,
                          a.dh, g);
@@ -329,21 +335,22 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dq_f32_ke
 
 // dV_j = sum_i P_ij dO_i, dK_j = scale sum_i dS_ij Q_i over the pair's rows.  A lane owns a key; what the lanes of keys that do not
 // count compute stays in their columns, and zeros are stored for them.
-template <int DHP>
+template <int DHP, bool EACH>
 __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dkv_f32_kernel(CrossArgs a) {
   constexpr int TILE = 32 * STRIDE<DHP>;
   __shared__ alignas(16) float lds[PARTS * TILE + PARTS * 64];
   const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5, l32 = lane & 31;
-  const Where w(a, (a.Sk + 31) / 32);
-  const int j0 = 32 * w.tile, j = j0 + l32, head0 = w.kh * a.group;
+  constexpr int KEYS = EACH ? 32 * PARTS : 32, STEP = EACH ? 1 : PARTS;
+  const Where w(a, (a.Sk + KEYS - 1) / KEYS);
+  const int first = EACH ? 0 : part, j0 = KEYS * w.tile + (EACH ? 32 * part : 0), j = j0 + l32, head0 = w.kh * a.group;
   const long jc = min(j, a.Sk - 1);
   const unsigned bits = key_bits(key_byte(a, w.b, j0, l32), j0, w.len, l32);
   const bool on = (bits >> l32) & 1u;
   f32x16 dk[DHP / 32], dv[DHP / 32];
 #pragma unroll
   for (int dt = 0; dt < DHP / 32; dt++) dk[dt] = dv[dt] = zero16();
-  if (bits) {                                                    // the same for the whole workgroup
+  if (bits) {
     f32x4 kf[DHP / 8], vf[DHP / 8];
     load_rows<DHP>(f32_of(a.k) + pair_offset(a.sk, w.b, w.kh) + jc * a.sk.t, a.dh, g, kf);
     load_rows<DHP>(f32_of(a.v) + pair_offset(a.sv, w.b, w.kh) + jc * a.sv.t, a.dh, g, vf);
@@ -358,15 +365,15 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dkv_f32_k
     f32x4 qf[DHP / 8], dof[DHP / 8];
     auto row_of = [&](int t) __attribute__((always_inline)) { return min(32 * t + l32, a.rows - 1); };
     float value = 0.f;                                           // lane l: lse of row l, lane 32 + l: D
-    if (t0 + part < t1) {
-      const int i = row_of(t0 + part);
+    if (t0 + first < t1) {
+      const int i = row_of(t0 + first);
       value = (g ? drow : lrow)[i];
       load_rows<DHP>(qb + row_offset(a.sq, a.group, i), a.dh, g, qf);
       load_rows<DHP>(dob + row_offset(a.sdo, a.group, i), a.dh, g, dof);
     }
-    for (int t = t0 + part; t < t1; t += PARTS) {
+    for (int t = t0 + first; t < t1; t += STEP) {
       const int left = a.rows - 32 * t;
-      const bool more = t + PARTS < t1, counts = l32 < left;
+      const bool more = t + STEP < t1, counts = l32 < left;
       values[lane] = value;
       f32x16 p = row_product<DHP>(qf, kf);                       // S[i][j]
       __builtin_amdgcn_sched_barrier(0);
@@ -388,7 +395,7 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dkv_f32_k
       __builtin_amdgcn_sched_barrier(0);
       put_rows<DHP>(tile, qf, counts, g, l32);
       if (more) {                                                // the next tile's are on their way during the rest of this one
-        const int next = row_of(t + PARTS);
+        const int next = row_of(t + STEP);
         value = (g ? drow : lrow)[next];
         load_rows<DHP>(dob + row_offset(a.sdo, a.group, next), a.dh, g, dof);
         load_rows<DHP>(qb + row_offset(a.sq, a.group, next), a.dh, g, qf);
@@ -397,9 +404,11 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dkv_f32_k
       col_product<DHP>(dk, ds, tile, g, l32);
     }
   }
-  merge_parts(dk, lds, part, lane);
-  merge_parts(dv, lds, part, lane);
-  if (part != 0 || j >= a.Sk) return;
+  if constexpr (!EACH) {
+    merge_parts(dk, lds, part, lane);
+    merge_parts(dv, lds, part, lane);
+  }
+  if (first != 0 || j >= a.Sk) return;
   if (a.splits > 1) {
     if (!on) return;                                             // the launch that joins the splits stores zeros
     float* dst = a.part + (((long)w.split * a.B * a.hk + w.pair) * a.Sk + j) * 2 * a.dh;
@@ -415,49 +424,59 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dkv_f32_k
   store_column<DHP>(dv, static_cast<float*>(a.dv) + pair_offset(a.sdv, w.b, w.kh) + (long)j * a.sdv.t, 1.0f, a.dh, g);
 }
 
-// Parts of a launch, by an estimate in microseconds: a workgroup takes 4 and `alone` for each 32 x 32 tile of a wavefront's
-// share, `pair` where two share a compute unit (0: one at a time); a launch of its own joins parts, which are written and read.
+// How a launch is cut, by an estimate in microseconds: a workgroup takes 4 and `alone` for each 32 x 32 tile of a wavefront's share,
+// `pair` where two share a compute unit (0: one at a time); a launch of its own joins parts, which are written and read.  A workgroup
+// works on 32 rows (dK / dV: keys) together, or on 32 for each wavefront, which few keys (rows) or many rows (keys) need.
+// us, forward + backward, head dim 128, each / together: 3 x 6231 x 7, 8 / 1 heads 283 / 672; 2048 x 2048, 16 / 4 heads 1558 / 1603;
+// one query, 8192 keys of 8 heads 113 / 213.
 struct Tile { double alone, pair; };
-int best_parts(const Tile& c, long blocks, long units, double part_mb) {
-  int best = 1;
-  double least = 0.0;
+struct Cut { int parts; bool each; double us; };
+Cut best_cut(const Tile& c, long blocks, long units, int share, double part_mb) {
+  Cut best{0, share == 1, 0.0};
   for (const int p : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
     if (p > 1 && units < 2 * p) break;
-    const long n = cdiv(blocks * p, 256), per = cdiv(cdiv(units, p), PARTS);
+    const long n = cdiv(blocks * p, 256), per = cdiv(cdiv(units, p), share);
     double t = c.pair > 0 ? (n / 2) * (4.0 + per * c.pair) + (n % 2) * (4.0 + per * c.alone) : n * (4.0 + per * c.alone);
     if (p > 1) t += 3.5 + 0.04 * p + p * part_mb / 4.0;
-    if (p == 1 || t < least) {
-      least = t;
-      best = p;
+    if (p == 1 || t < best.us) {
+      best.parts = p;
+      best.us = t;
     }
   }
   return best;
 }
+// pass 0: forward, 1: dQ, 2: dK / dV
+Cut cut_of(const CrossArgs& a, int pass) {
+  constexpr Tile COST[3][3] = {{{2.3, 3.3}, {3.0, 4.5}, {3.6, 5.5}},           // forward, dQ, dK / dV at head dims up to 32
+                               {{4.5, 6.5}, {6.0, 9.0}, {7.2, 11.0}},          // 64
+                               {{5.7, 0.0}, {7.5, 0.0}, {11.0, 0.0}}};         // 128
+  const long pairs = (long)a.B * a.hk;
+  const Tile& c = COST[a.dh <= 32 ? 0 : a.dh <= 64 ? 1 : 2][pass];
+  const int own = pass == 2 ? a.Sk : a.rows, units = cdiv(pass == 2 ? a.rows : a.Sk, 32);
+  const double mb = pairs * own * a.dh * (pass == 2 ? 16e-6 : 8e-6);
+  const Cut together = best_cut(c, pairs * cdiv(own, 32), units, PARTS, mb);
+  const Cut each = best_cut(c, pairs * cdiv(own, 32 * PARTS), units, 1, mb);
+  return each.us < together.us ? each : together;
+}
 
-#define GX_CROSS_F32(KERNEL, TILES)                                                                       \
-  do {                                                                                                    \
-    const dim3 grid((unsigned)((long)a.B * a.hk * (TILES) * a.splits)), block(64 * PARTS);                \
-    if (a.dh <= 32) hipLaunchKernelGGL(KERNEL<32>, grid, block, 0, s, a);                                 \
-    else if (a.dh <= 64) hipLaunchKernelGGL(KERNEL<64>, grid, block, 0, s, a);                            \
-    else hipLaunchKernelGGL(KERNEL<128>, grid, block, 0, s, a);                                           \
+#define GX_CROSS_F32(KERNEL, TILES, EACH)                                                  \
+  do {                                                                                     \
+    const dim3 grid((unsigned)((long)a.B * a.hk * (TILES) * a.splits)), block(64 * PARTS); \
+    if (a.dh <= 32) hipLaunchKernelGGL((KERNEL<32, EACH>), grid, block, 0, s, a);          \
+    else if (a.dh <= 64) hipLaunchKernelGGL((KERNEL<64, EACH>), grid, block, 0, s, a);     \
+    else hipLaunchKernelGGL((KERNEL<128, EACH>), grid, block, 0, s, a);                    \
   } while (0)
 
 }  // namespace
 
-int cross_parts_f32(const CrossArgs& a, int pass) {
-  const long pairs = (long)a.B * a.hk;
-  constexpr Tile COST[3][3] = {{{2.3, 3.3}, {3.0, 4.5}, {3.6, 5.5}},           // forward, dQ, dK / dV at head dims up to 32
-                               {{4.5, 6.5}, {6.0, 9.0}, {7.2, 11.0}},          // 64
-                               {{5.7, 0.0}, {7.5, 0.0}, {11.0, 0.0}}};         // 128
-  const Tile& c = COST[a.dh <= 32 ? 0 : a.dh <= 64 ? 1 : 2][pass];
-  return pass == 2 ? best_parts(c, pairs * cdiv(a.Sk, 32), cdiv(a.rows, 32), pairs * a.Sk * a.dh * 16e-6)
-                   : best_parts(c, pairs * cdiv(a.rows, 32), cdiv(a.Sk, 32), pairs * a.rows * a.dh * 8e-6);
-}
+int cross_parts_f32(const CrossArgs& a, int pass) { return cut_of(a, pass).parts; }
 
 hipError_t cross_fwd_f32(const CrossArgs& args, hipStream_t s) {
   CrossArgs a = args;
-  a.splits = cross_parts_f32(a, 0);
-  GX_CROSS_F32(cross_fwd_f32_kernel, cdiv(a.rows, 32));
+  const Cut c = cut_of(a, 0);
+  a.splits = c.parts;
+  if (c.each) GX_CROSS_F32(cross_fwd_f32_kernel, cdiv(a.rows, 32 * PARTS), true);
+  else GX_CROSS_F32(cross_fwd_f32_kernel, cdiv(a.rows, 32), false);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : cross_join_fwd(false, a, s);
 }
@@ -466,14 +485,18 @@ hipError_t cross_bwd_f32(const CrossArgs& args, hipStream_t s) {
   CrossArgs a = args;
   hipError_t e = hipSuccess;
   if (a.rows > 0) {
-    a.splits = cross_parts_f32(a, 1);
-    GX_CROSS_F32(cross_dq_f32_kernel, cdiv(a.rows, 32));
+    const Cut c = cut_of(a, 1);
+    a.splits = c.parts;
+    if (c.each) GX_CROSS_F32(cross_dq_f32_kernel, cdiv(a.rows, 32 * PARTS), true);
+    else GX_CROSS_F32(cross_dq_f32_kernel, cdiv(a.rows, 32), false);
     e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) e = cross_join_dq(false, a, s);
   }
   if (e != hipSuccess || a.Sk == 0) return e;
-  a.splits = cross_parts_f32(a, 2);
-  GX_CROSS_F32(cross_dkv_f32_kernel, cdiv(a.Sk, 32));
+  const Cut c = cut_of(a, 2);
+  a.splits = c.parts;
+  if (c.each) GX_CROSS_F32(cross_dkv_f32_kernel, cdiv(a.Sk, 32 * PARTS), true);
+  else GX_CROSS_F32(cross_dkv_f32_kernel, cdiv(a.Sk, 32), false);
   e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : cross_join_dkv(false, a, s);
 }
