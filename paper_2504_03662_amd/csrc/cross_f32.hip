@@ -2,7 +2,8 @@
 //
 // As in the causal fp32 kernels a workgroup owns 32 rows (forward, dQ) or 32 keys (dK / dV) of a (sample, key head) pair and
 // its 4 wavefronts take every 4th 32-wide tile of the other side, or every wavefront owns 32 and takes all the tiles.  Scores
-// are taken transposed to the owner, so that an accumulator register is, as it stands, an operand of the next product (register v of a lane in half g holds tile row 8 (v / 4) + 4 g + v % 4).
+// are taken transposed to the owner, so that an accumulator register is, as it stands, an operand of the next product (register
+// v of a lane in half g holds tile row 8 (v / 4) + 4 g + v % 4).
 // Operands come from global memory, requested while the tile before is worked on; where a tile's rows are the second operand of
 // one product and the first of another (dQ, dK / dV) a wavefront puts what it holds of them into LDS and reads columns.  The parts'
 // results are merged through LDS in wavefront order.  Head dimensions up to 128 (multiples of 4) are padded with zeros to 32, 64 or 128.
