@@ -346,8 +346,8 @@ typedef struct {
  * with GX_ROPE_PAIRS, (2 i, 2 i + 1) become (a cos - b sin, b cos + a sin) with cos[p, i], sin[p, i] from two fp32
  * tables [max_pos, rot_dim / 2].  rot_dim 0: norm only.
  *   queries [batch, q_len, q_heads, head_dim], keys [batch, k_len, k_heads, head_dim] (k_len or k_heads 0, or q_len or q_heads
- *   0: that side is left out and its pointers may be NULL); positions int32 [batch, len] (aligned to
- *   themselves), NULL for p = s.  A position
+ *   0: that side is left out and its pointers may be NULL; its gain's gradient, where it is asked for, is zeros); positions
+ *   int32 [batch, len] (aligned to themselves), NULL for p = s.  A position
  *   outside [0, max_pos) gives a token of NaN.  gain [head_dim] in dtype, NULL for ones.
  * gx_heads_norm_fwd writes q_out and k_out; they may be the inputs themselves (same data and strides).
  * gx_heads_norm_bwd takes the inputs q, k again and the gradients dq_out, dk_out of the outputs; writes dq, dk (may be

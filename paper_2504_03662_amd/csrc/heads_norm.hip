@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(256) heads_norm_kernel(NormArgs a) {
   else work_on<T, PAIRS, BACK>(a, a.side[1], blk - a.side[0].blocks, red);
 }
 
-// Sum of a side's partial rows, in order: 8 lanes of 4 columns, 32 runs of rows
+// Sum of a side's partial rows (there may be none), in order: 8 lanes of 4 columns, 32 runs of rows
 struct GainArgs {
   struct { const float* part; float* out; int blocks; } side[2];
   int dh, accumulate;
@@ -435,7 +435,13 @@ gx_status run(const gx_heads_norm_cfg* c, const gx_heads_norm_in* in, const gx_h
     s.blocks = l.blocks[k];
     s.per_token = l.per_token[k];
     s.units = l.units[k];
-    if (s.blocks == 0) continue;
+    if (s.blocks == 0) {                             // no token or no head: the gain's gradient is a sum of nothing
+      if (!backward || !dgain[k]) continue;
+      if (misaligned(dgain[k])) return GX_ERR_ALIGN;
+      gains.side[k] = {nullptr, dgain[k], 0};
+      any_gain = true;
+      continue;
+    }
     bad = check_heads(&x, c->batch, s.len, s.heads, c->head_dim, e, false);
     if (bad == GX_OK) bad = check_heads(out[k], c->batch, s.len, s.heads, c->head_dim, e, true);
     if (bad == GX_OK && backward) bad = check_heads(dy[k], c->batch, s.len, s.heads, c->head_dim, e, false);
@@ -457,13 +463,13 @@ gx_status run(const gx_heads_norm_cfg* c, const gx_heads_norm_in* in, const gx_h
   }
   if (!device_is_gfx950()) return GX_ERR_ARCH;
   const int blocks = a.side[0].blocks + a.side[1].blocks;
-  if (blocks == 0) return GX_OK;
+  if (blocks == 0 && !any_gain) return GX_OK;
   const bool bf = c->dtype == GX_BF16, pairs = c->flags & GX_ROPE_PAIRS;
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, st, a); };
-  if (backward) {
+  if (backward && blocks > 0) {
     if (bf) pairs ? go(heads_norm_kernel<bf16, true, true>) : go(heads_norm_kernel<bf16, false, true>);
     else pairs ? go(heads_norm_kernel<float, true, true>) : go(heads_norm_kernel<float, false, true>);
-  } else {
+  } else if (blocks > 0) {
     if (bf) pairs ? go(heads_norm_kernel<bf16, true, false>) : go(heads_norm_kernel<bf16, false, false>);
     else pairs ? go(heads_norm_kernel<float, true, false>) : go(heads_norm_kernel<float, false, false>);
   }
