@@ -347,8 +347,9 @@ typedef struct {
  * tables [max_pos, rot_dim / 2].  rot_dim 0: norm only.
  *   queries [batch, q_len, q_heads, head_dim], keys [batch, k_len, k_heads, head_dim] (k_len or k_heads 0, or q_len or q_heads
  *   0: that side is left out and its pointers may be NULL; its gain's gradient, where it is asked for, is zeros); positions
- *   int32 [batch, len] (aligned to themselves), NULL for p = s.  A position
- *   outside [0, max_pos) gives a token of NaN.  gain [head_dim] in dtype, NULL for ones.
+ *   int32 [batch, len] (aligned to themselves), NULL for p = s.  Where rot_dim > 0 a
+ *   position outside [0, max_pos) makes all columns of a token's heads NaN, turned or not, in outputs and input gradients, and so
+ *   the gain's gradient.  gain [head_dim] in dtype, NULL for ones.
  * gx_heads_norm_fwd writes q_out and k_out; they may be the inputs themselves (same data and strides).
  * gx_heads_norm_bwd takes the inputs q, k again and the gradients dq_out, dk_out of the outputs; writes dq, dk (may be
  * dq_out, dk_out themselves) and, where a gain is given, the gain's gradient fp32 [head_dim] (NULL to skip;

@@ -102,20 +102,15 @@ struct Place {
   }
 };
 
+// Whether a token can be turned: the tables have its position
+GX_DEVINL bool has_position(const NormArgs& a, int pos) { return a.rot == 0 || (pos >= 0 && pos < a.max_pos); }
+
 // The angles of a lane's columns at a token.  PAIRS: four for each chunk; else the same eight for both.
 struct Angles {
   f32x4 c[2], s[2];
   template <bool PAIRS>
   GX_DEVINL void load(const NormArgs& a, const Place& p, int pos) {
-    if (!p.turned) return;
-    const bool there = pos >= 0 && pos < a.max_pos;
-    if (!there) {
-#pragma unroll
-      for (int h = 0; h < 2; h++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) c[h][e] = s[h][e] = __builtin_nanf("");
-      return;
-    }
+    if (!p.turned || !has_position(a, pos)) return;       // (a token without its position is NaN whatever the angles are)
     const float* cr = a.cos + (size_t)pos * (a.rot / 2);
     const float* sr = a.sin + (size_t)pos * (a.rot / 2);
 #pragma unroll
@@ -193,7 +188,8 @@ struct Cursor {
 };
 
 // A unit's loads are issued before the unit before it is worked on; its angles with them, for which the position has
-// been read one unit earlier still.
+// been read one unit earlier still.  A unit is of one token, so that it takes one scalar comparison to make all of a token's
+// columns NaN whose position is not in the tables: its heads' factor r is.
 template <typename T, bool PAIRS, bool BACK>
 GX_DEVINL void work_on(const NormArgs& a, const Side& s, int blk, float (&red)[4][256]) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -219,7 +215,9 @@ GX_DEVINL void work_on(const NormArgs& a, const Side& s, int blk, float (&red)[4
     if (BACK) dr.load(s.dy.p + c.at(s.dy, h), p);
     an.load<PAIRS>(a, p, pos);
   };
-  fetch(now, pos_of(now), x, d, ang);
+  const int pos_first = __builtin_amdgcn_readfirstlane(pos_of(now));
+  bool there = has_position(a, pos_first);
+  fetch(now, pos_first, x, d, ang);
   if (s.gain) {
     RawPair<T> g;
     g.load(static_cast<const char*>(s.gain), p);
@@ -233,8 +231,11 @@ GX_DEVINL void work_on(const NormArgs& a, const Side& s, int blk, float (&red)[4
     RawPair<T> xn = x, dn = d;
     Angles an = ang;
     const Cursor then = ahead;
+    bool there_then = there;
     if (u + 1 < u1) {
-      fetch(ahead, pos, xn, dn, an);
+      const int pos_then = __builtin_amdgcn_readfirstlane(pos);
+      there_then = has_position(a, pos_then);
+      fetch(ahead, pos_then, xn, dn, an);
       if (u + 2 < u1) ahead.next(s);
       pos = pos_of(ahead);
     }
@@ -246,7 +247,8 @@ GX_DEVINL void work_on(const NormArgs& a, const Side& s, int blk, float (&red)[4
     float q = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; e++) q = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], q));
-    const float r = rsqrtf(fmaf(head_sum(q, lph), inv, a.eps));
+    float r = rsqrtf(fmaf(head_sum(q, lph), inv, a.eps));
+    if (!there) r = __builtin_nanf("");
     char* const out = s.out.p + now.at(s.out, h);
     if (!BACK) {
 #pragma unroll
@@ -286,6 +288,7 @@ GX_DEVINL void work_on(const NormArgs& a, const Side& s, int blk, float (&red)[4
     d = dn;
     ang = an;
     now = then;
+    there = there_then;
   }
   if (BACK && s.part) {
 #pragma unroll

@@ -100,7 +100,8 @@ class DeviceEmbedding(_Operator):
 
 class DeviceHeadNorm(_Operator):
     """RMS norm of every query and key head with a gain per column, then the rotation of the first `rot_dim` columns by the
-    token's position; columns (i, i + rot_dim / 2) turn together, or with `pairs` (2 i, 2 i + 1)."""
+    token's position; columns (i, i + rot_dim / 2) turn together, or with `pairs` (2 i, 2 i + 1).  A token whose position the
+    tables of angles do not have becomes NaN."""
 
     def __init__(self, head_dim, rot_dim=0, dtype="bf16", eps=1e-6, pairs=False, device="cuda:0"):
         super().__init__(dtype, device)
