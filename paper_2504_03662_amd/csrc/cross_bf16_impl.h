@@ -466,7 +466,8 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, 2) cross_fwd_kernel(CrossArgs
 // (two keys: dQ and dK off by 0.0024 of their norm, 0.0039 without; 8 x 2000 x 30, 16 / 4 heads of 64: 2 us of 59).
 // 2 x 4096 x 4096, 32 / 8 heads of 128: 750 us, 1.1 PFLOP/s; a product takes 30 ns of a SIMD.
 // Also forms D = rowsum(dO * O) and leaves D and lse * log2(e) in row order for the other
-// kernel (the first split does); a row without a key gets +inf there, so that its probabilities are 0.
+// kernel (the first split does); a row without a key, or with scores of -inf only, gets +inf there, so that its probabilities
+// are 0, and zeros for its dQ (with such scores the sum holds 0 times a key's infinity).
 template <int NQ, int SPLIT, int BKV, bool MASK>
 __global__ void __launch_bounds__(64 * NQ * SPLIT, NQ * SPLIT == 4 ? 2 : 1) cross_dq_kernel(CrossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -620,6 +621,10 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, NQ * SPLIT == 4 ? 2 : 1) cros
     }
   }
   if (r >= a.rows) return;
+  if (lse == -INFINITY) {
+#pragma unroll
+    for (int dt = 0; dt < DH / 32; dt++) dq[dt] = zero16();
+  }
   if (a.splits > 1) {
     float* row = a.part + (((long)w.split * a.B * a.hk + w.pair) * a.rows + r) * DH;
 #pragma unroll

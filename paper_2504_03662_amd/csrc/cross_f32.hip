@@ -261,7 +261,8 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_fwd_f32_k
   }
 }
 
-// D = rowsum(dO * O), dS = P (dP - D), dQ = scale dS K; leaves D and lse (+inf for a row without a key) in row order
+// D = rowsum(dO * O), dS = P (dP - D), dQ = scale dS K; leaves D and lse in row order (+inf for a row without a key or with scores of
+// -inf only, whose dQ is zeros)
 template <int DHP, bool EACH>
 __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dq_f32_kernel(CrossArgs a) {
   constexpr int TILE = 32 * STRIDE<DHP>;
@@ -287,7 +288,8 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dq_f32_ke
   dd += __shfl_xor(dd, 32, 64);
   const int i = rc / a.group, h = head0 + (rc - i * a.group);
   float lse = a.lse[((long)w.b * a.hk * a.group + h) * a.Sq + i];
-  if (lse == -INFINITY) lse = INFINITY;
+  const bool none = lse == -INFINITY;
+  if (none) lse = INFINITY;
   if (w.split == 0 && first == 0 && g == 0 && r < a.rows) {
     a.drow[(long)w.pair * a.rows + r] = dd;
     a.lrow[(long)w.pair * a.rows + r] = lse;
@@ -329,6 +331,10 @@ __global__ void __launch_bounds__(64 * PARTS, DHP <= 64 ? 2 : 1) cross_dq_f32_ke
   }
   if constexpr (!EACH) merge_parts(dq, lds, part, lane);
   if (first != 0 || r >= a.rows) return;
+  if (none) {                                                    // its sum may hold 0 times a key's infinity
+#pragma unroll
+    for (int dt = 0; dt < DHP / 32; dt++) dq[dt] = zero16();
+  }
   if (a.splits > 1) store_column<DHP>(dq, a.part + (((long)w.split * a.B * a.hk + w.pair) * a.rows + r) * a.dh, 1.0f, a.dh, g);
   else store_column<DHP>(dq, static_cast<float*>(a.dq) + pair_offset(a.sdq, w.b, head0) + row_offset(a.sdq, a.group, r), a.scale,
                          a.dh, g);
