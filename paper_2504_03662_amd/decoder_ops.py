@@ -3,8 +3,8 @@ gradient, norms of queries and keys with the position rotation, and cross attent
 supplies device memory and the stream, shapes and types are checked here, and the library does all the compute.
 
 Every call works on the current stream and returns without waiting.  An object holds sizes and scratch memory only, one piece of
-scratch per stream, so that calls on different streams do not meet; tensors of another stream are the caller's to order, as
-everywhere in torch.  Outputs are new tensors unless `out`s are given."""
+scratch per stream, so that calls on different streams do not meet, and none that a captured graph uses; tensors of another stream
+are the caller's to order, as everywhere in torch.  Outputs are new tensors unless `out`s are given."""
 from __future__ import annotations
 
 import torch
@@ -30,9 +30,14 @@ class _Operator:
         self._scratch = {}
 
     def _workspace(self, nbytes, stream):
-        w = self._scratch.get(stream)
+        # A captured call has memory of its own, from the graph's pool: the graph keeps the address for as long as it lives, while
+        # the memory that eager calls share is replaced when one needs more.
+        capturing = torch.cuda.is_current_stream_capturing()
+        w = None if capturing else self._scratch.get(stream)
         if w is None or w.numel() < nbytes:
-            w = self._scratch[stream] = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+            w = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+            if not capturing:
+                self._scratch[stream] = w
         return w
 
     def _check(self, name, t, shape, dtype, contiguous=True):
