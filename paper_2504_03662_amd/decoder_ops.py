@@ -3,9 +3,12 @@ gradient, norms of queries and keys with the position rotation, and cross attent
 supplies device memory and the stream, shapes and types are checked here, and the library does all the compute.
 
 Every call works on the current stream and returns without waiting.  An object holds sizes and scratch memory only, one piece of
-scratch per stream, so that calls on different streams do not meet, and none that a captured graph uses; tensors of another stream
-are the caller's to order, as everywhere in torch.  Outputs are new tensors unless `out`s are given."""
+scratch per stream and host thread, so that calls on different streams or of different threads (whose launches on one stream may
+mix) do not meet, and none that a captured graph uses; tensors of another stream or thread are the caller's to order, as everywhere
+in torch.  Outputs are new tensors unless `out`s are given."""
 from __future__ import annotations
+
+import threading
 
 import torch
 
@@ -27,17 +30,19 @@ class _Operator:
         self.gtype, self.tdtype = _TYPES[dtype]
         self.device = torch.device(device)
         self.index = -1 if self.device.type == "cpu" else self.device.index or 0
+        # by host thread and stream (what a thread that has ended leaves is found by the next of its number)
         self._scratch = {}
 
     def _workspace(self, nbytes, stream):
         # A captured call has memory of its own, from the graph's pool: the graph keeps the address for as long as it lives, while
         # the memory that eager calls share is replaced when one needs more.
         capturing = torch.cuda.is_current_stream_capturing()
-        w = None if capturing else self._scratch.get(stream)
+        key = threading.get_ident(), stream
+        w = None if capturing else self._scratch.get(key)
         if w is None or w.numel() < nbytes:
             w = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
             if not capturing:
-                self._scratch[stream] = w
+                self._scratch[key] = w
         return w
 
     def _check(self, name, t, shape, dtype, contiguous=True):

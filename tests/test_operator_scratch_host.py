@@ -1,4 +1,6 @@
 """Who shares scratch memory of an operator: calls of one host thread on one stream, and nobody else."""
+import copy
+import pickle
 import threading
 
 import pytest
@@ -43,3 +45,33 @@ def test_a_captured_call_has_memory_of_its_own(make, capturing):
     of_graph = fresh._workspace(1000, 7)
     capturing[0] = False
     assert fresh._workspace(1000, 7).data_ptr() != of_graph.data_ptr()
+
+
+@pytest.mark.parametrize("make", OPERATORS)
+def test_host_threads_do_not_share(make, capturing):
+    """Two threads' launches on one stream (every thread's default stream is the same) may come in any order, also one between two of
+    another's call"""
+    op = make()
+    mine, theirs = op._workspace(1000, 7), []
+    meet = threading.Barrier(3)
+
+    def other():
+        w = op._workspace(1000, 7)
+        meet.wait(10)                                              # both have theirs while the other lives
+        theirs.append((w, op._workspace(600, 7)))
+    threads = [threading.Thread(target=other) for _ in range(2)]
+    for t in threads:
+        t.start()
+    meet.wait(10)
+    for t in threads:
+        t.join(10)
+    assert len({w.data_ptr() for w in (mine, theirs[0][0], theirs[1][0])}) == 3
+    assert all(w is again for w, again in theirs) and op._workspace(1000, 7) is mine
+
+
+@pytest.mark.parametrize("make", OPERATORS)
+def test_operators_can_be_copied(make, capturing):
+    op = make()
+    w = op._workspace(1000, 7)
+    for twin in (copy.deepcopy(op), pickle.loads(pickle.dumps(op))):
+        assert twin._workspace(1000, 7).data_ptr() != w.data_ptr()
