@@ -23,13 +23,15 @@ def _need(ok, what):
 
 
 class _Operator:
-    """Type, device and scratch of an operator."""
+    """Type, device (which has to be the current one in calls) and scratch of an operator."""
 
     def __init__(self, dtype, device):
         gx.lib()                                   # fail loudly if the library is not built
         self.gtype, self.tdtype = _TYPES[dtype]
         self.device = torch.device(device)
-        self.index = -1 if self.device.type == "cpu" else self.device.index or 0
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.index = -1 if self.device.type == "cpu" else self.device.index
         # by host thread and stream (what a thread that has ended leaves is found by the next of its number)
         self._scratch = {}
 
@@ -65,6 +67,9 @@ class _Operator:
         return torch.empty(shape, dtype=dtype, device=self.device)
 
     def _stream(self):
+        # launches go to the current GPU, whatever stream they are given
+        if torch._C._cuda_getDevice() != self.index:
+            raise ValueError(f"{self.device} is not the current GPU")
         # the handle itself: a torch.cuda.Stream around it takes 2.8 us to make, a third of a small call
         return torch._C._cuda_getCurrentRawStream(self.index)
 
