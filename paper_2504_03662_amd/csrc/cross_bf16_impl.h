@@ -790,7 +790,7 @@ __global__ void __launch_bounds__(64 * KV_NW, 2) cross_dkv_kernel(CrossArgs a) {
   auto aux_load = [&](int t, char* dst, bool on) {
     const int i = t * KV_BI + lane;
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(aux), 0, (unsigned)a.rows * 4u, 0x00020000);
-    const unsigned o = on && i < a.rows ? (unsigned)i * 4u : OOB;
+    const unsigned o = on && i < a.rows ? (unsigned)i * 4u : 0xFFFFFFFCu;     // rows < 2^30: beyond all of them (OOB is 2^29 rows)
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_ptr)(on ? dst : smem + KV_OFF_SINK), 4, o, 0, 0, 0);
   };
   const bool lse_or_d = wave < 2, d_too = wave == 1;
