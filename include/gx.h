@@ -385,7 +385,8 @@ gx_status gx_heads_norm_bwd(const gx_heads_norm_cfg* cfg, const gx_heads_norm_in
  * What does not count is never read into a sum: infinities and NaN there change nothing.  A query for which no key
  * counts has O = 0, lse = -inf and no gradient, and so has one whose scores that count are all -inf (dQ = 0, and where dO and V are
  * finite nothing of it in dK and dV); keys that do not
- * count have dK = dV = 0.  gx_cross_bwd takes the forward pass's inputs, o and lse and writes dQ, dK, dV (all required).
+ * count have dK = dV = 0.  gx_cross_bwd takes the forward pass's inputs, o and lse and writes dQ, dK, dV (all required); it forms
+ * the probabilities from lse, whose own rounding puts them off by about 2^-23 |lse| of themselves.
  * Element types: bf16 with fp32 scores, softmax and sums (probabilities and their gradients are rounded to bf16 as operands of
  * the second products; head_dim 64 or 128) or fp32 throughout (head_dim a multiple of 4 up to 128).  scale > 0.
  * k and v keep at least head_dim elements between tokens.  q_len or k_len may be 0.

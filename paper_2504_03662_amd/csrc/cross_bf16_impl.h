@@ -239,8 +239,8 @@ GX_DEVINL void fwd_finish(const CrossArgs& a, const RowBlock& w, char* smem, f32
 // more than 2^8, so that O is rescaled rarely (following every rise, 128 pairs of 2048 x 2048 took 338 us instead of 301).
 // Arithmetic: base-2 exponentials of fp32 scores, sums of them in fp32 before P is rounded to bf16 for the product with V (an
 // error of the size that V's own type has), O in fp32 until it is stored.
-// Bound by the issue of matrix and vector instructions where there are rows: a product takes 31 ns of a SIMD with its share of the
-// softmax, 15 alone (2 x 4096 x 4096, 32 / 8 heads of 128: 500 us, 1.1 PFLOP/s, a library product 1.53); by memory where there are
+// Bound by the issue of matrix and vector instructions where there are rows: a product takes 32 ns of a SIMD with its share of the
+// softmax, 15 alone (2 x 4096 x 4096, 32 / 8 heads of 128: 521 us, 1.06 PFLOP/s, a library product 1.53); by memory where there are
 // few (one query of 40 heads, 16 x 8192 keys of 8 heads: 105 us, 5.1 TB/s).
 template <int NQ, int SPLIT, int BKV, bool MASK>
 __global__ void __launch_bounds__(64 * NQ * SPLIT, 2) cross_fwd_kernel(CrossArgs a) {
@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, 2) cross_fwd_kernel(CrossArgs
 // rounding of o, 2^-8 of |dO| |o| at most, stays in dS, beside dS's own rounding the smaller the more keys share a row, and no further
 // pass over the keys is needed.  Where one step holds all the keys D is made exact first: a row's dS add up to what it lacks
 // (two keys: dQ and dK off by 0.0024 of their norm, 0.0039 without; 8 x 2000 x 30, 16 / 4 heads of 64: 2 us of 59).
-// 2 x 4096 x 4096, 32 / 8 heads of 128: 750 us, 1.1 PFLOP/s; a product takes 30 ns of a SIMD.
+// 2 x 4096 x 4096, 32 / 8 heads of 128: 735 us, 1.12 PFLOP/s; a product takes 30 ns of a SIMD.
 // Also forms D = rowsum(dO * O) and leaves D and lse * log2(e) in row order for the other
 // kernel (the first split does); a row without a key, or with scores of -inf only, gets +inf there, so that its probabilities
 // are 0, and zeros for its dQ (with such scores the sum holds 0 times a key's infinity).
@@ -653,10 +653,12 @@ __global__ void __launch_bounds__(64 * NQ * SPLIT, NQ * SPLIT == 4 ? 2 : 1) cros
 // forms S = Q K^T, the probabilities P and dV += P^T dO, role K dP = dO V^T, dS = P (dP - D) and dK += dS^T Q, a tile behind.
 // A wavefront's stream mixes the first products of its next sub-tile with the vector work of the present one.  One
 // workgroup of 8 wavefronts fills a compute unit; wavefronts w and w + 4 share a SIMD, one of either role.
-// 2 x 4096 x 4096, 32 / 8 heads of 128: 1080 us, 1.0 PFLOP/s; 4 x 2048 x 1501 .. 938, 16 heads: 219 us, of which the last of three
-// rounds fills 112 of 256 compute units.
+// 2 x 4096 x 4096, 32 / 8 heads of 128: 1100 us, 1.0 PFLOP/s; 4 x 2048 x 1501 .. 938, 16 heads: 240 us, of which the last of three
+// rounds fills 128 of 256 compute units.
 // P crosses through LDS in 16 bits: 0 <= P < 2, so an fp32 P has two leading zero bits, and the next 16 (7 of the exponent, 9 of
-// the mantissa, rounded) say P to 2^-10 over the whole range: dS is then rounded to bf16 once, not twice.
+// the mantissa, rounded) say P to 2^-10 over the whole range: dS is then rounded to bf16 once, not twice.  (P is 1 at most but for the
+// rounding of lse: 2 takes an lse of millions, which puts P off by its own size, and then reads as nearly 0.  A NaN reads as a number,
+// but its row's o and so D are NaN.)
 // Keys that do not count are columns of their own in S and dP and rows of their own in dK and dV: whatever
 // their lanes compute stays there, and zeros are stored.
 constexpr int KV_PAIRS = 4, KV_NW = 2 * KV_PAIRS, KV_BJ = 32 * KV_PAIRS, KV_SUB = 2, KV_BI = 32 * KV_SUB;

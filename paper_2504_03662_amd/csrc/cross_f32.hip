@@ -11,7 +11,7 @@
 // is replaced by zeros before it becomes an operand.
 // Bound by the matrix pipe where there are many tiles (2048 x 2048, 16 heads of 128: forward 365 us, 94 TFLOP/s of the 145 that a
 // library product of fp32 reaches; a lone wavefront per SIMD does not overlap its exponentials), by latency where there are few:
-// 3 x 257 x 333, 8 / 4 heads of 64: 16 us, 21 us (dQ) and 33 us (dK / dV in three parts; 40 whole).
+// 3 x 257 x 333, 8 / 4 heads of 64: 17 us, 24 us (dQ) and 29 us (dK / dV in three parts, 4.5 to join them; whole 40).
 #include "cross.h"
 
 namespace gx {

@@ -7,9 +7,9 @@
 // a partial sum, and the partial sums of a run are added in order afterwards.  No floating-point atomics; the order of every
 // sum depends on sizes and ids alone.
 // Both directions are bound by memory (a large copy moves 5.7 TB/s on these chips, read and written): 8192 tokens of 2048 columns
-// (bf16) look up in 15.5 us (4.3 TB/s) and, with 32768 rows of which most are cleared, get their gradient in 72 us (268 MB of
-// fp32 gradient alone take 54); 16385 tokens of 4096, half of them of this shard, a quarter padding, 64013 rows: 33 to 41 and 217 us
-// (1.05 GB of gradient take 210).  Few tokens cost the launches: 257 tokens, 1001 rows of 256 (fp32) 2.5 and 3.7 us.
+// (bf16) look up in 15 us (4.4 TB/s) and, with 32768 rows of which most are cleared, get their gradient in 69 us (268 MB of
+// fp32 gradient alone take 47); 16385 tokens of 4096, half of them of this shard, a quarter padding, 64013 rows: 34 to 41 and 217 us
+// (1.05 GB of gradient take 185).  Few tokens cost the launches: 257 tokens, 1001 rows of 256 (fp32) 2.5 and 4.7 us.
 #include "../../include/gx.h"
 #include "gx_kernels.h"
 
@@ -348,9 +348,9 @@ __global__ void __launch_bounds__(256) embed_join_kernel(SumArgs a) {
 // One launch: every workgroup owns `span` consecutive rows of the table, 64 lanes' columns of them, and looks at all ids.  A wavefront
 // takes every 4th row: it lists the row's tokens in order (ballots over the ids that its lanes hold) and adds them up, or clears the row; rows
 // with more than HOT tokens come after that, a quarter of the tokens to a wavefront, and the quarters are added in order.
-// us, this / by sorted tokens: 257 tokens, 1001 rows of 256 (fp32) 3.7 / 14.5; 48 tokens, 97749 x 576 (bf16) 33.9 / 42.9; 512 tokens, 300000
-// x 64 22.4 / 27.5; 512 tokens, 32000 x 4096 108.3 / 107.4 (a copy's rate for the table's gradient); 512 tokens all alike, 500 x 8192
-// (fp32) 23.3 / 17.0, 1001 x 256 11.0 / 13.5.  More tokens would make rows that all of them share a long sum, and ids a long list.
+// us of the kernels, this / by sorted tokens: 257 tokens, 1001 rows of 256 (fp32) 4.7 / 15.3; 48 tokens, 97749 x 576 (bf16) 33.7 / 46.8;
+// 512 tokens, 300000 x 64 21.6 / 30.4; 512 tokens, 32000 x 4096 109.8 / 109.8 (a copy's rate for the table's gradient); 512 tokens all
+// alike, 500 x 8192 (fp32) 23.3 / 17.5, 1001 x 256 11.3 / 13.8.  More tokens would make rows that all of them share a long sum, and ids a long list.
 constexpr int FEW_TOKENS = 512, FEW_CHUNKS = FEW_TOKENS / 64, FEW_ROWS = 32, HOT = 16;
 template <typename I>
 struct FewArgs {

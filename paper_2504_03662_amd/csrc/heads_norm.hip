@@ -9,7 +9,7 @@
 // gradient is a sum in registers, added up over lanes, wavefronts and blocks in a fixed order at the end.
 // A unit of work is 64 / LPH heads of a token; a wavefront takes a run of units, and queries and keys get workgroups in proportion.
 // 4096 tokens of 40 heads of 128 (bf16): forward 17 to 19 us (84 MB: 4.5 to 4.9 of the 5.7 TB/s that a copy moves), backward
-// 30 (126 MB, 4.2 TB/s) and 4 for the gains; 3003 tokens of 32 heads of 64 (fp32): 14 (3.6 TB/s), 19 (4.0) and 3 to 4; one token of
+// 32 (126 MB, 4.0 TB/s) and 4 for the gains; 3003 tokens of 32 heads of 64 (fp32): 14 (3.5 TB/s), 19 (3.8) and 4; one token of
 // 64 samples 4, all of it latency (position, angles, heads).
 #include "../../include/gx.h"
 #include "gx_kernels.h"
