@@ -411,6 +411,111 @@ gx_status gx_cross_bwd(const gx_cross_cfg* cfg, const gx_cross_in* in, const gx_
                        const gx_heads* dq, const gx_heads* dk, const gx_heads* dv, void* workspace, void* hip_stream);
 
 /* ------------------------------------------------------------------------------------------
+ * What a decoder learns from: losses of logits, each with the gradient of the logits from the same call.  The calls only
+ * enqueue kernels on `hip_stream`; results are bitwise reproducible.
+ *
+ *     a = scale * logits[t, :],   lse = log sum exp a,   p = exp(a - lse),   logp = a[id] - lse  for row t's token id
+ *
+ *   logits [rows, vocab], `stride` elements between rows (at least vocab); dlogits the same with grad_stride, NULL for the losses
+ *   alone.  dlogits may be the logits themselves (same address and stride) and must not overlap them otherwise.  Rows and columns may
+ *   begin at any element; where rows of dlogits lie as those of the logits relative to 16 bytes, stores are wide.
+ *   ids [rows] : int32 or int64 (id_bytes 4 or 8).  A row whose id is ignore_id does not count.
+ *   A row counts with weights[t] (fp32, NULL for ones): losses and gradients are multiplied by it, so weights of mask / (number
+ *   of tokens) make sums means.  A row that does not count, or has weight 0, has loss 0, logp 0 and a gradient of zeros, whatever
+ *   its logits and other inputs hold: they are not read.  An id of no row of the vocabulary makes the row's results NaN.
+ *   Vocabulary shards: a rank holds columns [first_id, first_id + vocab) of whole_vocab (0: vocab, the whole of it).  lse is then the
+ *   shard's; a token of another shard has logp = -lse.  The whole vocabulary's are lse = log sum exp of the ranks' lse and
+ *   logp = sum over the ranks of (logp + lse) - lse of the whole.  Only gx_logp_* take shards.
+ * Logits of -inf are columns of probability 0.  A row of nothing else has lse = -inf and NaN for the rest, as has a row with NaN
+ * or +inf.  Sums are fp32 over a thread's elements, then fp64; losses are rounded once; gradients are fp32, rounded once.
+ * rows 0 .. 2^21, vocab 1 .. 2^19, scale 2^-20 .. 2^20; dlogits of gx_logp_bwd and gx_preference_loss in less than 2^24 pieces of
+ * 8192 (bf16) or 4096 (fp32) columns.  Pointers are aligned to their elements.  Errors: GX_ERR_NULL, GX_ERR_SHAPE, GX_ERR_DTYPE
+ * (dtype, id_bytes, top_dtype), GX_ERR_ALIGN, GX_ERR_FLAGS, GX_ERR_ARCH, GX_ERR_LAUNCH. */
+typedef struct {
+  int32_t rows, vocab;
+  int32_t dtype;              /* gx_dtype of logits and dlogits */
+  int32_t id_bytes;           /* 4 or 8 */
+  int32_t flags;              /* 0 */
+  float scale;                /* 1 / temperature */
+  int64_t stride, grad_stride;
+  int64_t first_id, whole_vocab, ignore_id;
+} gx_logits_cfg;
+
+/* Log probabilities, and the gradient that dlogp [rows] (the gradient by them) makes of the logits:
+ *     dlogits = dlogp * scale * (1 at the id - exp(a - lse))
+ * logp, lse fp32 [rows] (lse NULL to skip; 0 in rows that do not count).  gx_logp_bwd takes lse of the whole vocabulary; its own
+ * rounding puts p off by about 2^-24 |lse| of itself.  A row with dlogp 0 has a gradient of zeros, whatever its logits hold. */
+gx_status gx_logp_fwd(const gx_logits_cfg* cfg, const void* logits, const void* ids, float* logp, float* lse, void* hip_stream);
+gx_status gx_logp_bwd(const gx_logits_cfg* cfg, const void* logits, const void* ids, const float* lse, const float* dlogp, void* dlogits,
+                      void* hip_stream);
+
+/* Cross entropy: loss[t] = -w logp, dlogits = w * scale * (p - 1 at the id).  logp may be NULL. */
+gx_status gx_token_loss(const gx_logits_cfg* cfg, const void* logits, const void* ids, const float* weights, float* loss, float* logp,
+                        void* dlogits, void* hip_stream);
+
+/* Clipped policy loss with a KL term, of tokens that were drawn with log probability old_logp, with d = ref_logp - logp:
+ *     r = exp(logp - old_logp)
+ *     loss[t] = w * (-min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A) + kl * (exp(d) - d - 1)),   A = advantages[t]
+ * The first term has a gradient where r A is the smaller of the two or they are alike; A = 0 has none, whatever r.
+ * ref_logp may be NULL where kl is 0 (it is not read then); logp, the policy's own, may be NULL.
+ * 0 <= clip_low <= 1, clip_high >= 0, kl >= 0. */
+typedef struct {
+  float clip_low, clip_high, kl;
+  int32_t flags;              /* 0 */
+} gx_policy_cfg;
+typedef struct {
+  const float *old_logp, *advantages, *ref_logp, *weights;   /* [rows] */
+} gx_policy_in;
+gx_status gx_policy_loss(const gx_logits_cfg* cfg, const gx_policy_cfg* policy, const gx_policy_in* in, const void* logits,
+                         const void* ids, float* loss, float* logp, void* dlogits, void* hip_stream);
+
+/* Preference loss of pairs of sequences.  Sequence j is rows starts[j] .. starts[j + 1] - 1 (int32, ascending, 2 pairs + 1 of them,
+ * cut to 0 .. rows; sequences may be empty); pair i is sequence 2 i, the chosen one, against 2 i + 1.
+ *     reward[j] = beta * sum over its rows of w (logp - ref_logp),     x = reward[2 i] - reward[2 i + 1] - margin
+ *     loss[i] = pair weight * (-(1 - smoothing) log sigmoid(x) - smoothing log sigmoid(-x))
+ * ref_logp (NULL: zeros) fp32 [rows]; pair_weights (NULL: ones) fp32 [pairs]; rewards fp32 [2 pairs], may be NULL.  Rows that do not
+ * count, with weight 0 or of no sequence have a gradient of zeros; so has a pair of weight 0, and a loss of 0.
+ * gx_pairs_loss is the part after the log probabilities (which may come from shards): dlogp fp32 [rows] (NULL to skip) is the
+ * gradient by logp, for gx_logp_bwd.  gx_preference_loss takes the logits; its log probabilities are fp64.
+ * rows is that of the logits; at most 2^20 pairs.  Workspace: gx_preference_workspace_bytes(cfg), 0 for an invalid cfg. */
+typedef struct {
+  int32_t pairs, rows;
+  float beta, margin, smoothing;   /* smoothing 0 .. 1 */
+  int32_t flags;                   /* 0 */
+} gx_pairs_cfg;
+typedef struct {
+  const int32_t* starts;
+  const float *ref_logp, *weights, *pair_weights;
+} gx_pairs_in;
+gx_status gx_pairs_loss(const gx_pairs_cfg* pairs, const gx_pairs_in* in, const float* logp, float* loss, float* rewards, float* dlogp,
+                        void* hip_stream);
+size_t gx_preference_workspace_bytes(const gx_logits_cfg* cfg);
+gx_status gx_preference_loss(const gx_logits_cfg* cfg, const gx_pairs_cfg* pairs, const gx_pairs_in* in, const void* logits,
+                             const void* ids, float* loss, float* rewards, void* dlogits, void* workspace, void* hip_stream);
+
+/* Distillation from a teacher's top logits: row t's entries are columns top_ids[t, i] with the teacher's logits
+ * top_logits[t, i], i < top <= 1024 (ids of id_bytes; logits fp32 or bf16: top_dtype).  Entries whose id is no column do not count
+ * (-1 pads).  With q the teacher's probabilities and p the student's at those columns,
+ *     loss[t] = w * (sum of q log(q / p) + r log(r / s))
+ *   top_lse NULL: q = softmax of scale * top_logits over the row's entries, r = 0
+ *   top_lse fp32 [rows], the teacher's own log sum exp of scale times its logits: q = exp(scale * top_logits - top_lse), and the columns
+ *   without an entry are one more outcome, of r = max(0, 1 - sum of q) for the teacher and s, their p's sum, for the student.  (No such
+ *   outcome where there is no such column, or all of them are -inf.)
+ *     dlogits = w * scale * ((sum of q + r) p - q at the entries' columns - r exp(a - lse of the others) elsewhere)
+ * A term with q = 0 is 0.  An id that comes twice is two entries of one column.  A row without an entry has loss 0 and a gradient of
+ * zeros.  ids and ignore_id of the configuration are not used: rows are left out by weights of 0. */
+typedef struct {
+  int32_t top, top_dtype;
+  int32_t flags;              /* 0 */
+} gx_distill_cfg;
+typedef struct {
+  const void *top_ids, *top_logits;
+  const float *top_lse, *weights;
+} gx_distill_in;
+gx_status gx_distill_loss(const gx_logits_cfg* cfg, const gx_distill_cfg* distill, const gx_distill_in* in, const void* logits,
+                          float* loss, void* dlogits, void* hip_stream);
+
+/* ------------------------------------------------------------------------------------------
  * Layer-wise strategy plan (host only, no GPU involved).  The paper's strategy selector, in its
  * discovery phase (section 3, "Dynamic Strategy Selector"; section 2, "Layer-Specific Parallelism
  * Optimization"), prunes the candidate strategies with a decision tree and then runs a dynamic

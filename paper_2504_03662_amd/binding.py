@@ -33,7 +33,8 @@ EXPORTS = ("gx_layer_validate", "gx_layer_saved_bytes", "gx_layer_workspace_byte
            "gx_adamw_step", "gx_params_slice", "gx_params_merge", "gx_plan_search", "gx_strategy_cost", "gx_layer_bwd_static", "gx_peak_mfma", "gx_peak_copy",
            "gx_stage_partition", "gx_stage_moves", "gx_embed_workspace_bytes", "gx_embed_fwd", "gx_embed_bwd",
            "gx_heads_norm_workspace_bytes", "gx_heads_norm_fwd", "gx_heads_norm_bwd",
-           "gx_cross_workspace_bytes", "gx_cross_fwd", "gx_cross_bwd")
+           "gx_cross_workspace_bytes", "gx_cross_fwd", "gx_cross_bwd", "gx_logp_fwd", "gx_logp_bwd", "gx_token_loss",
+           "gx_policy_loss", "gx_pairs_loss", "gx_preference_workspace_bytes", "gx_preference_loss", "gx_distill_loss")
 GX_KC_LN_FWD, GX_KC_LN_BWD, GX_KC_ATTN_FWD, GX_KC_ATTN_BWD, GX_KC_COLSUM, GX_KC_GEMM = 1, 2, 3, 4, 5, 100
 
 
@@ -84,8 +85,8 @@ class StrategyCosts(ctypes.Structure):
                                                "flops_ffn")]
 
 
-# Records of the operators around a block, packed as C lays them out ("0q": padded to 8 bytes); they are made anew for every call,
-# which a ctypes.Structure takes several times as long for.
+# Records of the operators around a block and of the losses, packed as C lays them out ("0q": padded to 8 bytes); they are
+# made anew for every call, which a ctypes.Structure takes several times as long for.
 def _record(fmt):
     return struct.Struct("@" + fmt + "0q").pack
 
@@ -93,6 +94,11 @@ def _record(fmt):
 EmbedCfg = _record("6i2qf")         # tokens, hidden, rows, dtype, id_bytes, flags, first_row, pad_id, scale
 HeadsNormCfg = _record("10if")      # batch, q_len, k_len, q_heads, k_heads, head_dim, rot_dim, max_pos, dtype, flags, eps
 CrossCfg = _record("8if")           # batch, q_len, k_len, q_heads, k_heads, head_dim, dtype, flags, scale
+LogitsCfg = _record("5if5q")        # rows, vocab, dtype, id_bytes, flags, scale, stride, grad_stride, first_id, whole_vocab, ignore_id
+PolicyCfg = _record("3fi")          # clip_low, clip_high, kl, flags
+PairsCfg = _record("2i3fi")         # pairs, rows, beta, margin, smoothing, flags
+DistillCfg = _record("3i")          # top, top_dtype, flags
+_Pointers = _record("4P")
 _Heads = _record("P3q")             # data, strides of batch, token, head
 _HeadsNormIn = _record("P3qP3q6P")
 _CrossIn = _record("P3qP3qP3q2P")
@@ -163,10 +169,11 @@ def lib():
         L.gx_strategy_cost.argtypes = [ctypes.POINTER(StrategyQuery), ctypes.POINTER(StrategyCosts)]
         L.gx_strategy_cost.restype = ctypes.c_int
         for name, n in (("embed_fwd", 5), ("embed_bwd", 6), ("heads_norm_fwd", 5), ("heads_norm_bwd", 10), ("cross_fwd", 6),
-                        ("cross_bwd", 10)):
+                        ("cross_bwd", 10), ("logp_fwd", 6), ("logp_bwd", 7), ("token_loss", 8), ("policy_loss", 9), ("pairs_loss", 7),
+                        ("preference_loss", 10), ("distill_loss", 7)):
             f = getattr(L, "gx_" + name)
             f.argtypes, f.restype = [P] * n, ctypes.c_int
-        for name, more in (("embed", []), ("heads_norm", []), ("cross", [ctypes.c_int])):
+        for name, more in (("embed", []), ("heads_norm", []), ("cross", [ctypes.c_int]), ("preference", [])):
             f = getattr(L, f"gx_{name}_workspace_bytes")
             f.argtypes, f.restype = [P] + more, ctypes.c_size_t
         _lib = L
@@ -462,3 +469,53 @@ def cross_fwd(cfg, inputs, o, lse, workspace, stream=0, check=True):
 def cross_bwd(cfg, inputs, o, lse, d_o, dq, dk, dv, workspace, stream=0, check=True):
     return _checked(lib().gx_cross_bwd(cfg, inputs, heads(o), _addr(lse), heads(d_o), heads(dq), heads(dk), heads(dv),
                                        _addr(workspace), stream), "gx_cross_bwd", check)
+
+
+def logp_fwd(cfg, logits, ids, logp, lse, stream=0, check=True):
+    return _checked(lib().gx_logp_fwd(cfg, _addr(logits), _addr(ids), _addr(logp), _addr(lse), stream), "gx_logp_fwd", check)
+
+
+def logp_bwd(cfg, logits, ids, lse, dlogp, dlogits, stream=0, check=True):
+    return _checked(lib().gx_logp_bwd(cfg, _addr(logits), _addr(ids), _addr(lse), _addr(dlogp), _addr(dlogits), stream), "gx_logp_bwd",
+                    check)
+
+
+def token_loss(cfg, logits, ids, weights, loss, logp, dlogits, stream=0, check=True):
+    return _checked(lib().gx_token_loss(cfg, _addr(logits), _addr(ids), _addr(weights), _addr(loss), _addr(logp), _addr(dlogits), stream),
+                    "gx_token_loss", check)
+
+
+def policy_in(old_logp, advantages, ref_logp=None, weights=None):
+    return _Pointers(_addr(old_logp), _addr(advantages), _addr(ref_logp), _addr(weights))
+
+
+def policy_loss(cfg, policy, inputs, logits, ids, loss, logp, dlogits, stream=0, check=True):
+    return _checked(lib().gx_policy_loss(cfg, policy, inputs, _addr(logits), _addr(ids), _addr(loss), _addr(logp), _addr(dlogits), stream),
+                    "gx_policy_loss", check)
+
+
+def pairs_in(starts, ref_logp=None, weights=None, pair_weights=None):
+    return _Pointers(_addr(starts), _addr(ref_logp), _addr(weights), _addr(pair_weights))
+
+
+def pairs_loss(pairs, inputs, logp, loss, rewards, dlogp, stream=0, check=True):
+    return _checked(lib().gx_pairs_loss(pairs, inputs, _addr(logp), _addr(loss), _addr(rewards), _addr(dlogp), stream), "gx_pairs_loss",
+                    check)
+
+
+def preference_workspace_bytes(cfg):
+    return lib().gx_preference_workspace_bytes(cfg)
+
+
+def preference_loss(cfg, pairs, inputs, logits, ids, loss, rewards, dlogits, workspace, stream=0, check=True):
+    return _checked(lib().gx_preference_loss(cfg, pairs, inputs, _addr(logits), _addr(ids), _addr(loss), _addr(rewards), _addr(dlogits),
+                                             _addr(workspace), stream), "gx_preference_loss", check)
+
+
+def distill_in(top_ids, top_logits, top_lse=None, weights=None):
+    return _Pointers(_addr(top_ids), _addr(top_logits), _addr(top_lse), _addr(weights))
+
+
+def distill_loss(cfg, distill, inputs, logits, loss, dlogits, stream=0, check=True):
+    return _checked(lib().gx_distill_loss(cfg, distill, inputs, _addr(logits), _addr(loss), _addr(dlogits), stream), "gx_distill_loss",
+                    check)

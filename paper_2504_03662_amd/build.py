@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgx.so")
 SOURCES = ("gx_api.hip", "gemm_bf16.hip", "gemm_f32.hip", "attn_bf16.hip", "attn_f32.hip", "rowwise.hip",
            "neighbours.hip", "plan.hip", "dropout.hip", "peaks.hip", "embed.hip", "heads_norm.hip",
-           "cross.hip", "cross_bf16.hip", "cross_f32.hip")
+           "cross.hip", "cross_bf16.hip", "cross_f32.hip", "losses.hip")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
