@@ -503,7 +503,8 @@ gx_status gx_preference_loss(const gx_logits_cfg* cfg, const gx_pairs_cfg* pairs
  *   outcome where there is no such column, or all of them are -inf.)
  *     dlogits = w * scale * ((sum of q + r) p - q at the entries' columns - r exp(a - lse of the others) elsewhere)
  * A term with q = 0 is 0.  An id that comes twice is two entries of one column.  A row without an entry has loss 0 and a gradient of
- * zeros.  ids and ignore_id of the configuration are not used: rows are left out by weights of 0. */
+ * zeros.  ignore_id is not used: rows are left out by weights of 0.  Workspace: gx_distill_workspace_bytes, 0 for an invalid
+ * configuration. */
 typedef struct {
   int32_t top, top_dtype;
   int32_t flags;              /* 0 */
@@ -512,8 +513,9 @@ typedef struct {
   const void *top_ids, *top_logits;
   const float *top_lse, *weights;
 } gx_distill_in;
+size_t gx_distill_workspace_bytes(const gx_logits_cfg* cfg, const gx_distill_cfg* distill);
 gx_status gx_distill_loss(const gx_logits_cfg* cfg, const gx_distill_cfg* distill, const gx_distill_in* in, const void* logits,
-                          float* loss, void* dlogits, void* hip_stream);
+                          float* loss, void* dlogits, void* workspace, void* hip_stream);
 
 /* ------------------------------------------------------------------------------------------
  * Layer-wise strategy plan (host only, no GPU involved).  The paper's strategy selector, in its

@@ -34,7 +34,8 @@ EXPORTS = ("gx_layer_validate", "gx_layer_saved_bytes", "gx_layer_workspace_byte
            "gx_stage_partition", "gx_stage_moves", "gx_embed_workspace_bytes", "gx_embed_fwd", "gx_embed_bwd",
            "gx_heads_norm_workspace_bytes", "gx_heads_norm_fwd", "gx_heads_norm_bwd",
            "gx_cross_workspace_bytes", "gx_cross_fwd", "gx_cross_bwd", "gx_logp_fwd", "gx_logp_bwd", "gx_token_loss",
-           "gx_policy_loss", "gx_pairs_loss", "gx_preference_workspace_bytes", "gx_preference_loss", "gx_distill_loss")
+           "gx_policy_loss", "gx_pairs_loss", "gx_preference_workspace_bytes", "gx_preference_loss",
+           "gx_distill_workspace_bytes", "gx_distill_loss")
 GX_KC_LN_FWD, GX_KC_LN_BWD, GX_KC_ATTN_FWD, GX_KC_ATTN_BWD, GX_KC_COLSUM, GX_KC_GEMM = 1, 2, 3, 4, 5, 100
 
 
@@ -170,10 +171,10 @@ def lib():
         L.gx_strategy_cost.restype = ctypes.c_int
         for name, n in (("embed_fwd", 5), ("embed_bwd", 6), ("heads_norm_fwd", 5), ("heads_norm_bwd", 10), ("cross_fwd", 6),
                         ("cross_bwd", 10), ("logp_fwd", 6), ("logp_bwd", 7), ("token_loss", 8), ("policy_loss", 9), ("pairs_loss", 7),
-                        ("preference_loss", 10), ("distill_loss", 7)):
+                        ("preference_loss", 10), ("distill_loss", 8)):
             f = getattr(L, "gx_" + name)
             f.argtypes, f.restype = [P] * n, ctypes.c_int
-        for name, more in (("embed", []), ("heads_norm", []), ("cross", [ctypes.c_int]), ("preference", [])):
+        for name, more in (("embed", []), ("heads_norm", []), ("cross", [ctypes.c_int]), ("preference", []), ("distill", [P])):
             f = getattr(L, f"gx_{name}_workspace_bytes")
             f.argtypes, f.restype = [P] + more, ctypes.c_size_t
         _lib = L
@@ -516,6 +517,10 @@ def distill_in(top_ids, top_logits, top_lse=None, weights=None):
     return _Pointers(_addr(top_ids), _addr(top_logits), _addr(top_lse), _addr(weights))
 
 
-def distill_loss(cfg, distill, inputs, logits, loss, dlogits, stream=0, check=True):
-    return _checked(lib().gx_distill_loss(cfg, distill, inputs, _addr(logits), _addr(loss), _addr(dlogits), stream), "gx_distill_loss",
-                    check)
+def distill_workspace_bytes(cfg, distill):
+    return lib().gx_distill_workspace_bytes(cfg, distill)
+
+
+def distill_loss(cfg, distill, inputs, logits, loss, dlogits, workspace, stream=0, check=True):
+    return _checked(lib().gx_distill_loss(cfg, distill, inputs, _addr(logits), _addr(loss), _addr(dlogits), _addr(workspace), stream),
+                    "gx_distill_loss", check)

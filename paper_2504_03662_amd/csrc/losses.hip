@@ -10,6 +10,7 @@
 // are small differences of log sums, and a sequence's reward adds up over thousands of tokens.
 #include "../../include/gx.h"
 #include "gx_kernels.h"
+#include <type_traits>
 
 namespace {
 
@@ -19,22 +20,28 @@ constexpr int MAX_ROWS = 1 << 21, MAX_VOCAB = 1 << 19, MAX_TOP = 1024, MAX_PAIRS
 constexpr long MAX_GRID = (1 << 24) - 1;                       // workgroups of 256: a launch has less than 2^32 threads
 constexpr float NO_LOGIT = -INFINITY, MIN_SCALE = 1.f / (1 << 20);
 
+template <int N> using Int = std::integral_constant<int, N>;
+template <bool B> using Flag = std::bool_constant<B>;
+
 template <typename T> struct Lanes;                            // elements of 16 bytes
 template <> struct Lanes<float> { static constexpr int N = 4; typedef f32x4 type; };
 template <> struct Lanes<bf16> { static constexpr int N = 8; typedef bf16x8 type; };
 
-// A row cut at the borders of 16 bytes: `head` elements before the first, `body` chunks, `tail` elements behind the last.  The
-// elements at the ends (fewer than two chunks) go one to a thread.
+// A row cut at the borders of 16 bytes: `head` elements before the first, `body` chunks, the rest behind the last.  The elements at the
+// ends (fewer than two chunks) go one to a thread.  `lead`: chunks from the last border of 128 bytes to the first chunk: threads
+// count from there, so that a wavefront's 64 chunks are whole lines.
 template <typename T>
 struct Cut {
   static constexpr int N = Lanes<T>::N;
-  int head, body, ends, vocab;
+  int head, body, ends, lead, vocab;
   GX_DEVINL Cut(const void* row, int v) : vocab(v) {
     const int off = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
     head = min(v, (N - off) % N);
     body = (v - head) / N;
-    ends = v - body * N;                                       // head and tail together
+    ends = v - body * N;                                       // before and behind together
+    lead = (int)((reinterpret_cast<uintptr_t>(row) + (uintptr_t)head * sizeof(T)) >> 4 & 7);
   }
+  GX_DEVINL bool has(int c) const { return (unsigned)c < (unsigned)body; }
   GX_DEVINL int end_at(int i) const { return i < head ? i : vocab - ends + i; }
 };
 
@@ -60,6 +67,23 @@ struct Ids {
   }
 };
 
+// Maximum and sum of exponentials (relative to the maximum) of a set of logits; the empty set has -inf and 0
+struct Sums {
+  float m;
+  double s;
+};
+
+// What a row's teacher says, as top_kernel leaves it: the sum of q; of q (log q - scale (z - m)); 1 - sum of q, or 0; and m and
+// the sum over the student's logits that have an entry.  An entry: its column, or -1, the student's logit there, q.
+struct TopRow {
+  double q_sum, terms, rest;
+  Sums own;
+};
+struct TopEntry {
+  int col;
+  float z, q, pad;
+};
+
 enum Kind { SCORE, TOKEN, POLICY, DISTILL };
 struct RowArgs {
   const void* z;
@@ -78,9 +102,9 @@ struct RowArgs {
   f32x2* stats;
   float* counted;
   // distillation
-  const void *top_ids, *top_logits;
-  const float* top_lse;
-  int top, top_id_bytes, top_bf16;
+  const TopRow* top_rows;
+  const TopEntry* entries;
+  int top, rest;
 };
 
 // exp(scale d) for d = z - maximum.  c_lo: the rounding of the constant would shift every term of a sum the same way.  It is
@@ -93,11 +117,6 @@ GX_DEVINL double wave_sum_f64(double v) {
   return v;
 }
 
-// Maximum and sum of exponentials (relative to the maximum) of a set of logits; the empty set has -inf and 0
-struct Sums {
-  float m;
-  double s;
-};
 GX_DEVINL float reference(float m) { return m == NO_LOGIT ? 0.f : m; }
 GX_DEVINL double rescaled(Sums x, float m, const RowArgs& a) {
   return x.s == 0.0 ? 0.0 : x.s * (double)exp_scaled(x.m - m, a.c_hi, a.c_lo);
@@ -116,13 +135,17 @@ GX_DEVINL void clear_row(T* row, int vocab, int tid, int threads) {
   if (tid < k.ends) row[k.end_at(tid)] = from_f32<T>(0.f);
 }
 
+// Past the caches: whoever reads the gradient next reads it as fast (1024 to 4096 rows of 32000, bf16: a sum over it 35 to 93 us, after stores
+// into the caches 35 to 101), and the row kernel takes 28 rather than 31 us at 1024 rows, 205 rather than 206 at 8192 of 32768, 190 rather
+// than 206 at 4096 of 64013.
 template <typename T>
 GX_DEVINL void store_chunk(T* p, const float (&x)[Lanes<T>::N], bool aligned) {
-  typename Lanes<T>::type v;
+  typedef typename Lanes<T>::type Raw;
+  Raw v;
 #pragma unroll
   for (int e = 0; e < Lanes<T>::N; e++) v[e] = from_f32<T>(x[e]);
   if (aligned) {
-    *reinterpret_cast<typename Lanes<T>::type*>(p) = v;
+    __builtin_nontemporal_store(v, reinterpret_cast<Raw*>(p));
   } else {                                                     // a gradient whose rows lie otherwise than the logits'
 #pragma unroll
     for (int e = 0; e < Lanes<T>::N; e++) p[e] = v[e];
@@ -153,91 +176,146 @@ GX_DEVINL double policy_loss(const RowArgs& a, double logp, float old, float ref
   return l;
 }
 
-// What a row's teacher says, in LDS: which columns have an entry (bit column - head + N), and the entries
-struct Top {
-  unsigned* mask;
-  int* col;                                                    // -1: the entry does not count
-  float *z, *t, *q;                                            // the student's logit, the teacher's scaled one, its probability
-  struct Shared {
-    double q_sum, terms, rest;                                 // sum of q; of q (log q - scale (z - m)); 1 - sum of q, or 0
-    Sums k;                                                    // of the student's logits that have an entry
-    int repeated;
-  }* sh;
+// Reads a row's teacher: WAVES wavefronts to a row, 4 to a workgroup.  Everything here is fp64 but the entry's q.
+// An index that comes twice is one column with two entries; the first of them stands for the column, with the sum of their q.
+// Whether there is such an index is asked of a table of at least twice as many places as entries (so that a search ends), and only
+// then entries are compared with all others.
+struct TopArgs {
+  const void* z;
+  long stride;
+  int rows, vocab, top, places, id_bytes, top_bf16;
+  float scale;
+  const void *ids, *logits;
+  const float *lse, *weights;
+  TopRow* out;
+  TopEntry* entries;
 };
-template <typename T>
-GX_DEVINL int top_bit(const Cut<T>& k, int col) { return col - k.head + Lanes<T>::N; }
-__host__ __device__ inline int top_words(int vocab) { return (vocab + 16) / 32 + 1; }
-inline size_t top_lds(int vocab, int top) { return (size_t)4 * top_words(vocab) + 16 * (size_t)top + 64; }
-
-GX_DEVINL int top_id(const RowArgs& a, long i) {
-  const long id = a.top_id_bytes == 8 ? static_cast<const long*>(a.top_ids)[i] : static_cast<const int*>(a.top_ids)[i];
-  return id >= 0 && id < a.vocab ? (int)id : -1;
-}
-
-// The first wavefront reads a row's entries.  An index that comes twice is one column with two entries: the first of them
-// stands for the column.
-template <typename T>
-GX_DEVINL void read_top(const RowArgs& a, const Cut<T>& k, const T* zr, int row, int lane, const Top& t) {
+template <typename T, int WAVES>
+__global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
+  constexpr int THREADS = 64 * WAVES, ROWS = 4 / WAVES;
+  extern __shared__ int lds_top[];
+  __shared__ double part[4];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), of_row = ROWS == 1 ? 0 : wave;
+  const int row = blockIdx.x * ROWS + of_row, tid = ROWS == 1 ? threadIdx.x : threadIdx.x & 63;
+  if (row >= a.rows) return;
+  if (a.weights && a.weights[row] == 0.f) return;              // nobody reads its record
+  auto all_here = [] {
+    if (WAVES > 1) __syncthreads();
+    else __threadfence_block();
+  };
+  auto sum = [&](double v) {
+    v = wave_sum_f64(v);
+    if (WAVES == 1) return v;
+    if ((threadIdx.x & 63) == 0) part[wave] = v;
+    __syncthreads();
+    v = (part[0] + part[1]) + (part[2] + part[3]);
+    __syncthreads();
+    return v;
+  };
+  auto largest = [&](float v) {
+    v = wave_max(v);
+    if (WAVES == 1) return v;
+    if ((threadIdx.x & 63) == 0) part[wave] = (double)v;
+    __syncthreads();
+    v = (float)fmax(fmax(part[0], part[1]), fmax(part[2], part[3]));
+    __syncthreads();
+    return v;
+  };
+  int* const table = lds_top + of_row * (a.places + 2 * a.top);
+  int* const cols = table + a.places;
+  float* const qs = reinterpret_cast<float*>(cols + a.top);
+  const T* zr = static_cast<const T*>(a.z) + (size_t)row * a.stride;
+  TopEntry* const entries = a.entries + (size_t)row * a.top;
+  const size_t first_entry = (size_t)row * a.top;
+  auto column = [&](int i) {
+    const long id = a.id_bytes == 8 ? static_cast<const long*>(a.ids)[first_entry + i] : static_cast<const int*>(a.ids)[first_entry + i];
+    return id >= 0 && id < a.vocab ? (int)id : -1;
+  };
+  auto teacher = [&](int i) {
+    return a.top_bf16 ? (float)static_cast<const bf16*>(a.logits)[first_entry + i] : static_cast<const float*>(a.logits)[first_entry + i];
+  };
+  // a thread's first entry stays in registers; more than THREADS entries are read again
+  const bool one = tid < a.top;
+  const int col0 = one ? column(tid) : -1;
+  const float t0 = one ? teacher(tid) : 0.f, z0 = col0 >= 0 ? to_f32(zr[col0]) : 0.f;
+  auto col_of = [&](int i) { return i == tid ? col0 : column(i); };
+  auto t_of = [&](int i) { return i == tid ? t0 : teacher(i); };
+  auto z_of = [&](int i, int col) { return i == tid ? z0 : to_f32(zr[col]); };
+  for (int i = tid; i < a.places; i += THREADS) table[i] = -1;
+  all_here();
   float mz = NO_LOGIT, mt = NO_LOGIT;
-  int repeated = 0;
-  for (int i = lane; i < a.top; i += 64) {
-    const long at = (long)row * a.top + i;
-    const int col = top_id(a, at);
-    const float tl = a.top_bf16 ? (float)static_cast<const bf16*>(a.top_logits)[at] : static_cast<const float*>(a.top_logits)[at];
-    t.col[i] = col;
-    t.t[i] = tl;
+  bool again = false;
+  for (int i = tid; i < a.top; i += THREADS) {
+    const int col = col_of(i);
+    cols[i] = col;
     if (col < 0) continue;
-    const float z = to_f32(zr[col]);
-    t.z[i] = z;
-    mz = fmaxf(mz, z);
-    mt = fmaxf(mt, tl);
-    const int bit = top_bit(k, col);
-    repeated |= (atomicOr(&t.mask[bit >> 5], 1u << (bit & 31)) >> (bit & 31)) & 1;
+    mz = fmaxf(mz, z_of(i, col));
+    mt = fmaxf(mt, t_of(i));
+    for (unsigned at = (unsigned)col * 2654435761u;; at++) {
+      const int there = atomicCAS(&table[at & (a.places - 1)], -1, col);
+      if (there == col) again = true;
+      if (there == col || there == -1) break;
+    }
   }
-  repeated = __any(repeated);
-  __threadfence_block();
-  mz = wave_max(mz);
-  mt = wave_max(mt);
+  const bool repeated = largest(again ? 1.f : 0.f) > 0.f;
+  mz = largest(mz);
+  mt = a.lse ? 0.f : largest(mt);
+  const double scale = (double)a.scale, ref = (double)reference(mz);
   double lse;
-  if (a.top_lse) {
-    lse = (double)a.top_lse[row];
+  if (a.lse) {
+    lse = (double)a.lse[row];
   } else {
     double s = 0.0;
-    for (int i = lane; i < a.top; i += 64)
-      if (t.col[i] >= 0) s += exp((double)a.scale * ((double)t.t[i] - (double)mt));
-    lse = (double)a.scale * (double)mt + log(wave_sum_f64(s));
+    for (int i = tid; i < a.top; i += THREADS)
+      if (cols[i] >= 0) s += exp(scale * ((double)t_of(i) - (double)mt));
+    lse = scale * (double)mt + log(sum(s));
   }
   double q_sum = 0.0, terms = 0.0, sz = 0.0;
-  for (int i = lane; i < a.top; i += 64) {
-    const int col = t.col[i];
-    if (col < 0) continue;
-    const double logq = (double)a.scale * (double)t.t[i] - lse, q = exp(logq), az = (double)a.scale * ((double)t.z[i] - (double)reference(mz));
-    q_sum += q;
-    if (q != 0.0) terms += q * (logq - az);
-    t.q[i] = (float)q;
-    bool first = true;
-    if (repeated)
-      for (int j = 0; j < i; j++) first &= t.col[j] != col;
-    if (first) sz += exp(az);
+  for (int i = tid; i < a.top; i += THREADS) {
+    TopEntry e = {cols[i], 0.f, 0.f, 0.f};
+    if (e.col >= 0) {
+      e.z = z_of(i, e.col);
+      const double logq = scale * (double)t_of(i) - lse, q = exp(logq), az = scale * ((double)e.z - ref);
+      q_sum += q;
+      if (q != 0.0) terms += q * (logq - az);
+      e.q = (float)q;
+      qs[i] = e.q;
+      bool first = true;
+      if (repeated)
+        for (int j = 0; j < i; j++) first &= cols[j] != e.col;
+      if (!first) e.col = -1;
+      else if (a.lse) sz += exp(az);
+    }
+    entries[i] = e;
   }
-  q_sum = wave_sum_f64(q_sum);
-  terms = wave_sum_f64(terms);
-  sz = wave_sum_f64(sz);
-  if (lane == 0) *t.sh = {q_sum, terms, a.top_lse ? fmax(0.0, 1.0 - q_sum) : 0.0, {mz, sz}, repeated};
+  if (repeated) {
+    all_here();
+    for (int i = tid; i < a.top; i += THREADS) {
+      if (entries[i].col < 0) continue;
+      float q = qs[i];
+      for (int j = i + 1; j < a.top; j++)
+        if (cols[j] == cols[i]) q += qs[j];
+      entries[i].q = q;
+    }
+  }
+  q_sum = sum(q_sum);
+  terms = sum(terms);
+  if (a.lse) sz = sum(sz);
+  if (tid == 0) a.out[row] = {q_sum, terms, a.lse ? fmax(0.0, 1.0 - q_sum) : 0.0, {mz, sz}};
 }
 
 // A row to a workgroup of THREADS, or with 64 one to each of a workgroup's four wavefronts.  A thread has CH chunks in flight; with
 // STREAM as many of those steps as the row needs, and reads them again for the gradient, without it one.
-template <typename T, int THREADS, int CH, bool STREAM, bool TOP>
-__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) loss_row_kernel(RowArgs a) {
+template <typename T, int THREADS, int CH, bool STREAM, bool TOP, bool AGAIN>
+__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_kernel(RowArgs a) {
   constexpr int N = Lanes<T>::N, WAVES = THREADS / 64, ROWS = THREADS < 256 ? 256 / THREADS : 1;
-  static_assert(!TOP || ROWS == 1, "");
   typedef typename Lanes<T>::type Raw;
-  extern __shared__ double lds[];
+  extern __shared__ unsigned lds[];
   __shared__ Sums part[WAVES];
-  const int row = ROWS == 1 ? blockIdx.x : blockIdx.x * ROWS + (threadIdx.x >> 6);
+  const int wave_of_group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int row = ROWS == 1 ? blockIdx.x : blockIdx.x * ROWS + wave_of_group;
   if (ROWS > 1 && row >= a.rows) return;
-  const int tid = ROWS == 1 ? threadIdx.x : threadIdx.x & 63, lane = threadIdx.x & 63, wave = ROWS == 1 ? threadIdx.x >> 6 : 0;
+  const int tid = ROWS == 1 ? threadIdx.x : lane, wave = ROWS == 1 ? wave_of_group : 0;
   const T* zr = static_cast<const T*>(a.z) + (size_t)row * a.stride;
   T* dr = a.dz ? static_cast<T*>(a.dz) + (size_t)row * a.grad_stride : nullptr;
   const float w = a.weights ? a.weights[row] : 1.f;
@@ -259,49 +337,63 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) loss_row_kernel
   }
   const Cut<T> k(zr, a.vocab);
   const Raw* body = reinterpret_cast<const Raw*>(zr + k.head);
+  // chunk j of a step, and whether this wavefront has one
+  auto chunk = [&](int base, int j) { return base + j * THREADS + tid - k.lead; };
+  auto there = [&](int base, int j) { return base + j * THREADS + wave * 64 - k.lead < k.body; };
+  const TopEntry* entries = TOP ? a.entries + (size_t)row * a.top : nullptr;
+  int col = -1;
+  if (TOP && a.rest && tid < a.top) col = entries[tid].col;
   Raw v[CH];
-  auto load = [&](int base) {
+  auto load = [&](int base, auto past) {
 #pragma unroll
     for (int j = 0; j < CH; j++) {
-      const int c = base + j * THREADS + tid;
+      const int c = chunk(base, j);
       v[j] = splat<T>(NO_LOGIT);
-      if (c < k.body) v[j] = body[c];
+      if (k.has(c)) {
+        if (decltype(past)::value) v[j] = __builtin_nontemporal_load(body + c);
+        else v[j] = body[c];
+      }
     }
   };
-  load(0);
+  const Flag<!AGAIN && !STREAM> only_time;                     // a row that is read twice is to stay near in between
+  load(0, only_time);
   const bool has_end = tid < k.ends;
   const int end_col = k.end_at(tid);
   float end = has_end ? to_f32(zr[end_col]) : NO_LOGIT;
   float zy = 0.f;
   if (!TOP && y >= 0) zy = to_f32(zr[y]);
 
-  Top top;
-  if (TOP) {
-    top.sh = reinterpret_cast<Top::Shared*>(lds);
-    top.mask = reinterpret_cast<unsigned*>(lds + 8);
-    const int words = top_words(a.vocab);
-    top.col = reinterpret_cast<int*>(top.mask + words);
-    top.z = reinterpret_cast<float*>(top.col + a.top);
-    top.t = top.z + a.top;
-    top.q = top.t + a.top;
-    for (int i = tid; i < words; i += THREADS) top.mask[i] = 0;
-    __syncthreads();
-    if (wave == 0) read_top(a, k, zr, row, lane, top);
-    __syncthreads();
-    if (has_end) {
-      const int bit = top_bit(k, end_col);
-      if (top.mask[bit >> 5] >> (bit & 31) & 1) end = NO_LOGIT;
+  // With a rest, columns that have an entry are taken out of the row: the others' sum can be far smaller than theirs
+  const bool take = TOP && a.rest;
+  unsigned* const columns_out = lds + (ROWS > 1 ? wave_of_group * ((k.body + 5) >> 2) : 0);   // a byte for the ends before, for each
+                                                                                            // chunk, for the ends behind
+  auto all_here = [] {                                         // the threads of a row; LDS keeps a wavefront's order
+    if (WAVES > 1) __syncthreads();
+    else __threadfence_block();
+  };
+  auto out_at = [&](int c) { return (columns_out[(c + 1) >> 2] >> ((c + 1) & 3) * 8) & 255; };
+  if (take) {
+    for (int i = tid; i < (k.body + 5) >> 2; i += THREADS) columns_out[i] = 0;
+    all_here();
+    for (int i = tid;;) {
+      if (col >= 0) {
+        const int at = col - k.head, c = at < 0 ? -1 : min(at / N, k.body), e = at < 0 ? col : at - c * N;
+        atomicOr(&columns_out[(c + 1) >> 2], 1u << (((c + 1) & 3) * 8 + e));
+      }
+      i += THREADS;
+      if (i >= a.top) break;
+      col = entries[i].col;
     }
+    all_here();
+    if (has_end && (end_col < k.head ? out_at(-1) >> end_col : out_at(k.body) >> (end_col - k.head - k.body * N)) & 1) end = NO_LOGIT;
   }
-  // with TOP, the logits that have an entry of their own are taken out
   auto take_out = [&](int base) {
-    if (!TOP) return;
+    if (!take) return;
 #pragma unroll
     for (int j = 0; j < CH; j++) {
-      const int c = base + j * THREADS + tid;
-      if (c >= k.body) continue;
-      const int bit = (c + 1) * N;
-      const unsigned on = top.mask[bit >> 5] >> (bit & 31) & ((1u << N) - 1);
+      const int c = chunk(base, j);
+      if (!k.has(c)) continue;
+      const unsigned on = out_at(c);
       if (on) {
 #pragma unroll
         for (int e = 0; e < N; e++)
@@ -317,20 +409,24 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) loss_row_kernel
     take_out(base);
     float top_here = m;
 #pragma unroll
-    for (int j = 0; j < CH; j++)
+    for (int j = 0; j < CH; j++) {
+      if (!there(base, j)) break;
 #pragma unroll
       for (int e = 0; e < N; e++) top_here = fmaxf(top_here, to_f32(v[j][e]));
+    }
     const float ref = reference(top_here);
     if (s != 0.f) s *= exp_scaled(m - ref, a.c_hi, a.c_lo);
     m = top_here;
 #pragma unroll
-    for (int j = 0; j < CH; j++)
+    for (int j = 0; j < CH; j++) {
+      if (!there(base, j)) break;
 #pragma unroll
       for (int e = 0; e < N; e++) s += exp_scaled(to_f32(v[j][e]) - ref, a.c_hi, a.c_lo);
+    }
     if (!STREAM) break;
     base += THREADS * CH;
-    if (base >= k.body) break;
-    load(base);
+    if (base >= k.body + k.lead) break;
+    load(base, only_time);
   }
   Sums all;
   all.m = wave_max(m);
@@ -347,104 +443,97 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) loss_row_kernel
   }
 
   // the gradient is slope * exp(scale (z - ref)) of every element that has no value of its own
-  float ref = all.m, slope = 0.f;
-  float own = 0.f;                                             // g scale
+  const double scale = (double)a.scale;
+  const double weight = (double)w;
+  float ref = all.m, slope = 0.f, own = 0.f;                   // own: the gradient by logp
+  double logp = 0.0, log_s = 0.0;
   float p_top = 0.f, ref_top = 0.f, mass = 0.f;                // TOP: p of an entry's column is p_top exp(scale (z - ref_top))
+  bool others = false;                                         // TOP: whether there are columns without an entry
   if (TOP) {
-    const Top::Shared sh = *top.sh;
-    const bool others = all.m != NO_LOGIT || all.s != 0.0;     // columns without an entry
-    const double r = others ? sh.rest : 0.0, total = sh.q_sum + r;
-    const Sums row_sums = joined(all, sh.k, a);
-    const double log_all = log_sum(row_sums, a);
-    if (tid == 0 && a.loss) {
-      double l = sh.terms + sh.q_sum * (log_all - (double)a.scale * (double)reference(sh.k.m));
-      if (r > 0.0) l += r * (log(r) - (log_sum(all, a) - log_all));
-      a.loss[row] = (float)((double)w * l);
-    }
-    if (!dr) return;
+    const TopRow& t = a.top_rows[row];
+    others = a.rest && (all.m != NO_LOGIT || all.s != 0.0);
+    const double r = others ? t.rest : 0.0, total = t.q_sum + r;
+    const Sums row_sums = a.rest ? joined(all, t.own, a) : all;
     // total p - r exp(a - lse of the others), and what that is relative to the others' own sum
-    const double p_others = rescaled(all, row_sums.m, a) / row_sums.s;
-    const double ws = (double)w * (double)a.scale;
-    slope = others ? (float)(ws * (total * p_others - r) / all.s) : 0.f;
+    slope = (float)(weight * scale * (total * rescaled(all, row_sums.m, a) / row_sums.s - r) / all.s);
+    if (a.rest && !others && row_sums.s != 0.0) slope = 0.f;   // there is nothing to write, or zeros
     ref = reference(all.m);
     ref_top = row_sums.m;
     p_top = (float)(1.0 / row_sums.s);
     mass = (float)total;
   } else {
-    // of the cross entropy's wavefronts only the first has a use for it
-    const double log_s = a.kind == TOKEN && wave > 0 ? 0.0 : log(all.s);
-    double logp = (double)a.scale * ((double)zy - (double)all.m) - log_s;
-    if (y == ELSEWHERE) logp = -((double)a.scale * (double)all.m + log_s);
-    if (y == INVALID) logp = __builtin_nan("");
-    if (tid == 0) {
-      if (a.logp) a.logp[row] = (float)logp;
-      if (a.lse) a.lse[row] = (float)((double)a.scale * (double)all.m + log_s);
-      if (a.logp64) {
-        a.logp64[row] = logp;
-        a.stats[row] = f32x2{all.m, (float)(1.0 / all.s)};
-        a.counted[row] = w;
-      }
-      if (a.kind == TOKEN) a.loss[row] = (float)(-(double)w * logp);
+    own = -w;
+    if (a.kind == POLICY) {                                    // (the others' logarithms can wait until the registers are free)
+      log_s = log(all.s);
+      logp = scale * ((double)zy - (double)all.m) - log_s;
+      own = w * policy_slope(a, logp, a.old_logp[row], a.kl != 0.f ? a.ref_logp[row] : 0.f, a.adv[row]);
     }
-    float g = -w;
-    if (a.kind == POLICY) {
-      const float old = a.old_logp[row], refp = a.kl != 0.f ? a.ref_logp[row] : 0.f, adv = a.adv[row];
-      g = w * policy_slope(a, logp, old, refp, adv);
-      if (tid == 0) a.loss[row] = (float)((double)w * policy_loss(a, logp, old, refp, adv));
+    if (y == INVALID) own = __builtin_nanf("");
+    slope = (float)(-(double)own * scale / all.s);
+  }
+
+  if (dr) {
+    const bool aligned = ((reinterpret_cast<uintptr_t>(dr) ^ reinterpret_cast<uintptr_t>(zr)) & 15) == 0;
+    for (int base = 0;;) {
+      if (STREAM) {
+        load(base, Flag<true>());
+        take_out(base);
+      }
+#pragma unroll
+      for (int j = 0; j < CH; j++) {
+        const int c = chunk(base, j);
+        if (!k.has(c)) continue;
+        float x[N];
+#pragma unroll
+        for (int e = 0; e < N; e++) x[e] = slope * exp_scaled(to_f32(v[j][e]) - ref, a.c_hi, a.c_lo);
+        store_chunk(dr + k.head + (size_t)c * N, x, aligned);
+      }
+      if (!STREAM) break;
+      base += THREADS * CH;
+      if (base >= k.body + k.lead) break;
+    }
+    if (has_end && (TOP || end_col != y)) dr[end_col] = from_f32<T>(slope * exp_scaled(end - ref, a.c_hi, a.c_lo));
+  }
+
+  if (TOP) {
+    const TopRow& t = a.top_rows[row];
+    if (tid == 0) {
+      const double r = others ? t.rest : 0.0, log_all = log_sum(a.rest ? joined(all, t.own, a) : all, a);
+      double l = t.terms;
+      if (t.q_sum != 0.0) l += t.q_sum * (log_all - scale * (double)reference(t.own.m));
+      if (r > 0.0) l += r * (log(r) - (log_sum(all, a) - log_all));
+      a.loss[row] = (float)(weight * l);
     }
     if (!dr) return;
-    if (y == INVALID) g = __builtin_nanf("");
-    slope = (float)(-(double)g * (double)a.scale / all.s);
-    own = g * a.scale;
-  }
-  // g scale (1 - p) at y, without the difference
-  auto at_y = [&]() { return own * -expm1f((float)((double)a.scale * ((double)zy - (double)all.m) - log(all.s))); };
-
-  const bool aligned = ((reinterpret_cast<uintptr_t>(dr) ^ reinterpret_cast<uintptr_t>(zr)) & 15) == 0;
-  for (int base = 0;;) {
-    if (STREAM) {
-      load(base);
-      take_out(base);
-    }
-#pragma unroll
-    for (int j = 0; j < CH; j++) {
-      const int c = base + j * THREADS + tid;
-      if (c >= k.body) continue;
-      float x[N];
-#pragma unroll
-      for (int e = 0; e < N; e++) x[e] = slope * exp_scaled(to_f32(v[j][e]) - ref, a.c_hi, a.c_lo);
-      store_chunk(dr + k.head + (size_t)c * N, x, aligned);
-    }
-    if (!STREAM) break;
-    base += THREADS * CH;
-    if (base >= k.body) break;
-  }
-  if (has_end) {
-    float x = slope * exp_scaled(end - ref, a.c_hi, a.c_lo);
-    if (!TOP && end_col == y) x = at_y();
-    dr[end_col] = from_f32<T>(x);
-  }
-  if (!TOP) {
-    // by the thread that has stored the chunk around it, after that
-    const int at = y - k.head;
-    if (y >= k.head && at < k.body * N && (at / N) % THREADS == tid) dr[y] = from_f32<T>(at_y());
-  } else {
-    __syncthreads();                                           // the chunks are stored
+    all_here();                                                // the chunks are stored
     const float ws = w * a.scale;
     for (int i = tid; i < a.top; i += THREADS) {
-      const int col = top.col[i];
-      if (col < 0) continue;
-      float q = top.q[i];
-      if (top.sh->repeated) {                                  // the first entry of a column writes for all of them
-        bool first = true;
-        for (int j = 0; j < i; j++) first &= top.col[j] != col;
-        if (!first) continue;
-        for (int j = i + 1; j < a.top; j++)
-          if (top.col[j] == col) q += top.q[j];
-      }
-      dr[col] = from_f32<T>(ws * (mass * p_top * exp_scaled(top.z[i] - ref_top, a.c_hi, a.c_lo) - q));
+      const TopEntry e = entries[i];
+      if (e.col >= 0) dr[e.col] = from_f32<T>(ws * (mass * p_top * exp_scaled(e.z - ref_top, a.c_hi, a.c_lo) - e.q));
     }
+    return;
   }
+  // the thread that has stored the chunk around y, or could have: it overwrites y after that
+  const int at = y - k.head, by_end = at < 0 ? y : at - k.body * N + k.head;
+  const int y_tid = y < 0 ? -1 : at >= 0 && at < k.body * N ? (at / N + k.lead) % THREADS : by_end;
+  if (tid != 0 && tid != y_tid) return;
+  if (a.kind != POLICY) {
+    log_s = log(all.s);
+    logp = scale * ((double)zy - (double)all.m) - log_s;
+  }
+  if (y == ELSEWHERE) logp = -(scale * (double)all.m + log_s);
+  if (y == INVALID) logp = __builtin_nan("");
+  if (dr && tid == y_tid) dr[y] = from_f32<T>(own * a.scale * -expm1f((float)logp));        // g scale (1 - p), without the difference
+  if (tid > 0) return;
+  if (a.logp) a.logp[row] = (float)logp;
+  if (a.lse) a.lse[row] = (float)(scale * (double)all.m + log_s);
+  if (a.logp64) {
+    a.logp64[row] = logp;
+    a.stats[row] = f32x2{all.m, (float)(1.0 / all.s)};
+    a.counted[row] = w;
+  }
+  if (a.kind == TOKEN) a.loss[row] = (float)(-weight * logp);
+  if (a.kind == POLICY) a.loss[row] = (float)(weight * policy_loss(a, logp, a.old_logp[row], a.kl != 0.f ? a.ref_logp[row] : 0.f, a.adv[row]));
 }
 
 // dz = g scale (1_y - p) where p = f exp(c (u z - m)): m = lse of the whole vocabulary (u = scale, c = 1, f = 1), or what the row
@@ -463,11 +552,12 @@ template <typename T, int CH>
 __global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a) {
   constexpr int N = Lanes<T>::N;
   typedef typename Lanes<T>::type Raw;
-  const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts, tid = threadIdx.x;
+  // from the last row on: of logits that have just been read whole, the last ones may still be near
+  const int block = gridDim.x - 1 - blockIdx.x, row = block / a.parts, part = block - row * a.parts, tid = threadIdx.x;
   const T* zr = static_cast<const T*>(a.z) + (size_t)row * a.stride;
   T* dr = static_cast<T*>(a.dz) + (size_t)row * a.grad_stride;
   const Cut<T> k(zr, a.vocab);
-  const int y = a.ids.column(row, a.vocab), first = part * 256 * CH;
+  const int y = a.ids.column(row, a.vocab), first = part * 256 * CH + tid - k.lead;
   float g = a.dlogp[row] * a.scale;
   const bool aligned = ((reinterpret_cast<uintptr_t>(dr) ^ reinterpret_cast<uintptr_t>(zr)) & 15) == 0;
   const bool counts = y != IGNORED && g != 0.f;
@@ -479,14 +569,17 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a) {
   if (counts) {
 #pragma unroll
     for (int j = 0; j < CH; j++) {
-      const int c = first + j * 256 + tid;
-      if (c < k.body) v[j] = reinterpret_cast<const Raw*>(zr + k.head)[c];
+      const int c = first + j * 256;
+      if (k.has(c)) {
+        const Raw* p = reinterpret_cast<const Raw*>(zr + k.head) + c;
+        v[j] = __builtin_nontemporal_load(p);
+      }
     }
   }
 #pragma unroll
   for (int j = 0; j < CH; j++) {
-    const int c = first + j * 256 + tid;
-    if (c >= k.body) continue;
+    const int c = first + j * 256;
+    if (!k.has(c)) continue;
     float x[N];
 #pragma unroll
     for (int e = 0; e < N; e++) x[e] = 0.f;
@@ -594,6 +687,12 @@ gx_status check(const gx_pairs_cfg* c) {
     return GX_ERR_SHAPE;
   return GX_OK;
 }
+gx_status check(const gx_distill_cfg* c) {
+  if (!c) return GX_ERR_NULL;
+  if (c->top_dtype != GX_F32 && c->top_dtype != GX_BF16) return GX_ERR_DTYPE;
+  if (c->flags) return GX_ERR_FLAGS;
+  return c->top <= 0 || c->top > MAX_TOP ? GX_ERR_SHAPE : GX_OK;
+}
 bool logits_misaligned(const gx_logits_cfg& c, const void* p) { return misaligned(p, c.dtype == GX_BF16 ? 2 : 4); }
 
 Ids ids_of(const gx_logits_cfg& c, const void* ids) {
@@ -605,6 +704,11 @@ void set_scale(float scale, float& hi, float& lo) {
   hi = (float)c;
   if ((double)hi >= c) hi = nextafterf(hi, 0.f);
   lo = (float)(c - (double)hi);
+}
+// The most chunks of a row, with those between a border of 128 bytes and the first
+int chunks_of(const gx_logits_cfg& c, const void* z, int64_t stride) {
+  const bool whole_lines = !misaligned(z, 128) && stride * (c.dtype == GX_BF16 ? 2 : 4) % 128 == 0;
+  return c.vocab / (c.dtype == GX_BF16 ? 8 : 4) + (whole_lines ? 0 : 7);
 }
 RowArgs row_args(const gx_logits_cfg& c, Kind kind, const void* logits, void* dlogits, const float* weights, float* loss) {
   RowArgs a = {};
@@ -622,18 +726,47 @@ RowArgs row_args(const gx_logits_cfg& c, Kind kind, const void* logits, void* dl
   return a;
 }
 
-gx_status run_rows(const gx_logits_cfg& c, const RowArgs& a, hipStream_t s) {
+// again: the logits are read once more right after this.
+// Rows stay in registers while a workgroup has room for them: the fewest threads that hold one in 16 chunks each do best (8192
+// rows of 8000 / 16384 / 32768, bf16 cross entropy with gradient: 256 threads 51 / 96 / 200 us, 512 threads 57 / 104 / 203; read twice 60 / 101 / 219), up to
+// 512 columns or so a wavefront a row; 50001: 294, read twice 335; 131072: 1024 threads with nothing beside them on a compute unit
+// 215, read twice 234.  With few rows, which do not fill the chip, more threads to a row (512 rows of 32000: 17 and 15 us).
+// Log probabilities alone, and entries to look up, do better reading twice than with 1024 threads and their barriers: 118 and 99 us, 275 and
+// 246.  The rule does not ask whether a gradient is wanted: a loss has the same bits with and without.
+gx_status run_rows(const gx_logits_cfg& c, const RowArgs& a, bool again, hipStream_t s) {
   if (!device_is_gfx950()) return GX_ERR_ARCH;
   const bool bf = c.dtype == GX_BF16, top = a.kind == DISTILL;
-  const size_t lds = top ? top_lds(a.vocab, a.top) : 0;
-  auto go = [&](auto kernel, int threads, int rows) {
-    if (lds > 65536 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+  const int per_row = chunks_of(c, a.z, c.stride);
+  const size_t lds = !top || !a.rest ? 0 : (((size_t)per_row + 5) & ~(size_t)3) * (per_row <= 512 ? 4 : 1);
+  bool refused = false;
+  auto go = [&](auto kernel, int threads) {
+    if (lds > 65536 &&
+        hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
+      refused = true;
       return;
-    hipLaunchKernelGGL(kernel, dim3(cdiv(a.rows, rows)), dim3(threads), lds, s, a);
+    }
+    hipLaunchKernelGGL(kernel, dim3(cdiv(a.rows, threads < 256 ? 256 / threads : 1)), dim3(threads < 256 ? 256 : threads), lds, s, a);
   };
-  if (top) bf ? go(loss_row_kernel<bf16, 256, 4, true, true>, 256, 1) : go(loss_row_kernel<float, 256, 4, true, true>, 256, 1);
-  else bf ? go(loss_row_kernel<bf16, 256, 4, true, false>, 256, 1) : go(loss_row_kernel<float, 256, 4, true, false>, 256, 1);
-  return launched();
+  auto with = [&](auto threads, auto ch, auto stream) {
+    constexpr int TH = decltype(threads)::value, CH = decltype(ch)::value;
+    constexpr bool ST = decltype(stream)::value;
+    if (top) bf ? go(loss_row_kernel<bf16, TH, CH, ST, true, false>, TH) : go(loss_row_kernel<float, TH, CH, ST, true, false>, TH);
+    else if (again) bf ? go(loss_row_kernel<bf16, TH, CH, ST, false, true>, TH) : go(loss_row_kernel<float, TH, CH, ST, false, true>, TH);
+    else bf ? go(loss_row_kernel<bf16, TH, CH, ST, false, false>, TH) : go(loss_row_kernel<float, TH, CH, ST, false, false>, TH);
+  };
+  const Flag<false> held;
+  const Flag<true> twice;
+  if (per_row <= 256) with(Int<64>(), Int<4>(), held);
+  else if (per_row <= 512) with(Int<64>(), Int<8>(), held);
+  else if (per_row <= 1024) with(Int<256>(), Int<4>(), held);
+  else if (per_row <= 2048) with(Int<256>(), Int<8>(), held);
+  else if (per_row <= 4096 && a.rows >= 1024) with(Int<256>(), Int<16>(), held);
+  else if (per_row <= 4096) with(Int<512>(), Int<8>(), held);
+  else if (per_row <= 8192) with(Int<512>(), Int<16>(), held);
+  else if (per_row <= 16384 && a.kind != SCORE && !top) with(Int<1024>(), Int<16>(), held);
+  else if (per_row <= 16384) with(Int<1024>(), Int<4>(), twice);
+  else with(Int<512>(), Int<8>(), twice);
+  return refused ? GX_ERR_LAUNCH : launched();
 }
 
 gx_status run_grad(const gx_logits_cfg& c, GradArgs a, hipStream_t s) {
@@ -644,12 +777,12 @@ gx_status run_grad(const gx_logits_cfg& c, GradArgs a, hipStream_t s) {
   a.rows = c.rows;
   a.vocab = c.vocab;
   a.scale = c.scale;
-  const int chunks = c.vocab / (bf ? 8 : 4);
+  const int chunks = chunks_of(c, a.z, c.stride);
   a.parts = chunks > 0 ? cdiv(chunks, 256 * CH) : 1;
   if ((long)c.rows * a.parts > MAX_GRID) return GX_ERR_SHAPE;
   const dim3 grid((unsigned)c.rows * (unsigned)a.parts);
-  if (bf) hipLaunchKernelGGL((loss_grad_kernel<bf16, CH>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((loss_grad_kernel<float, CH>), grid, dim3(256), 0, s, a);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
+  bf ? go(loss_grad_kernel<bf16, CH>) : go(loss_grad_kernel<float, CH>);
   return launched();
 }
 
@@ -679,6 +812,17 @@ PreferenceScratch preference_scratch(int rows) {
   return {0, 8 * n, 16 * n, 20 * n, 24 * n};
 }
 
+// Scratch of the distillation: what top_kernel leaves of every row's teacher
+struct DistillScratch {
+  size_t rows, entries, bytes;
+};
+DistillScratch distill_scratch(int rows, int top) {
+  const size_t head = (size_t)rows * sizeof(TopRow);
+  static_assert(sizeof(TopRow) % 8 == 0 && sizeof(TopEntry) == 16, "");
+  const size_t entries = (head + 15) & ~(size_t)15;
+  return {0, entries, entries + (size_t)rows * top * sizeof(TopEntry)};
+}
+
 }  // namespace
 
 extern "C" {
@@ -693,7 +837,7 @@ gx_status gx_logp_fwd(const gx_logits_cfg* cfg, const void* logits, const void* 
   a.ids = ids_of(*cfg, ids);
   a.logp = logp;
   a.lse = lse;
-  return run_rows(*cfg, a, static_cast<hipStream_t>(hip_stream));
+  return run_rows(*cfg, a, true, static_cast<hipStream_t>(hip_stream));
 }
 
 gx_status gx_logp_bwd(const gx_logits_cfg* cfg, const void* logits, const void* ids, const float* lse, const float* dlogp, void* dlogits,
@@ -729,7 +873,7 @@ gx_status gx_token_loss(const gx_logits_cfg* cfg, const void* logits, const void
   RowArgs a = row_args(*cfg, TOKEN, logits, dlogits, weights, loss);
   a.ids = ids_of(*cfg, ids);
   a.logp = logp;
-  return run_rows(*cfg, a, static_cast<hipStream_t>(hip_stream));
+  return run_rows(*cfg, a, false, static_cast<hipStream_t>(hip_stream));
 }
 
 gx_status gx_policy_loss(const gx_logits_cfg* cfg, const gx_policy_cfg* policy, const gx_policy_in* in, const void* logits,
@@ -756,7 +900,7 @@ gx_status gx_policy_loss(const gx_logits_cfg* cfg, const gx_policy_cfg* policy, 
   a.low = policy->clip_low;
   a.high = policy->clip_high;
   a.kl = policy->kl;
-  return run_rows(*cfg, a, static_cast<hipStream_t>(hip_stream));
+  return run_rows(*cfg, a, false, static_cast<hipStream_t>(hip_stream));
 }
 
 gx_status gx_pairs_loss(const gx_pairs_cfg* pairs, const gx_pairs_in* in, const float* logp, float* loss, float* rewards, float* dlogp,
@@ -799,7 +943,7 @@ gx_status gx_preference_loss(const gx_logits_cfg* cfg, const gx_pairs_cfg* pairs
   a.stats = reinterpret_cast<f32x2*>(ws + l.stats);
   a.counted = reinterpret_cast<float*>(ws + l.counted);
   float* dlogp = reinterpret_cast<float*>(ws + l.dlogp);
-  if (cfg->rows > 0 && (st = run_rows(*cfg, a, s)) != GX_OK) return st;
+  if (cfg->rows > 0 && (st = run_rows(*cfg, a, dlogits != nullptr, s)) != GX_OK) return st;
   st = run_pairs<double>(*pairs, *in, a.counted, a.logp64, loss, rewards, dlogits ? dlogp : nullptr, s);
   if (st != GX_OK || !dlogits || cfg->rows == 0) return st;
   GradArgs g = {};
@@ -813,28 +957,54 @@ gx_status gx_preference_loss(const gx_logits_cfg* cfg, const gx_pairs_cfg* pairs
   return run_grad(*cfg, g, s);
 }
 
+size_t gx_distill_workspace_bytes(const gx_logits_cfg* cfg, const gx_distill_cfg* distill) {
+  return check_whole(cfg) == GX_OK && check(distill) == GX_OK ? distill_scratch(cfg->rows, distill->top).bytes : 0;
+}
+
 gx_status gx_distill_loss(const gx_logits_cfg* cfg, const gx_distill_cfg* distill, const gx_distill_in* in, const void* logits,
-                          float* loss, void* dlogits, void* hip_stream) {
-  const gx_status st = check_whole(cfg);
+                          float* loss, void* dlogits, void* workspace, void* hip_stream) {
+  gx_status st = check_whole(cfg);
+  if (st == GX_OK) st = check(distill);
   if (st != GX_OK) return st;
-  if (!distill || !in) return GX_ERR_NULL;
-  if (distill->top_dtype != GX_F32 && distill->top_dtype != GX_BF16) return GX_ERR_DTYPE;
-  if (distill->flags) return GX_ERR_FLAGS;
-  if (distill->top <= 0 || distill->top > MAX_TOP) return GX_ERR_SHAPE;
+  if (!in) return GX_ERR_NULL;
   if (cfg->rows == 0) return GX_OK;
-  if (!logits || !loss || !in->top_ids || !in->top_logits) return GX_ERR_NULL;
+  if (!logits || !loss || !in->top_ids || !in->top_logits || !workspace) return GX_ERR_NULL;
   if (logits_misaligned(*cfg, logits) || logits_misaligned(*cfg, dlogits) || misaligned(in->top_ids, cfg->id_bytes) ||
       misaligned(in->top_logits, distill->top_dtype == GX_BF16 ? 2 : 4) || misaligned(in->top_lse, 4) || misaligned(in->weights, 4) ||
-      misaligned(loss, 4))
+      misaligned(loss, 4) || misaligned(workspace, 16))
     return GX_ERR_ALIGN;
+  if (!device_is_gfx950()) return GX_ERR_ARCH;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const DistillScratch l = distill_scratch(cfg->rows, distill->top);
+  char* ws = static_cast<char*>(workspace);
+  TopArgs t = {};
+  t.z = logits;
+  t.stride = (long)cfg->stride;
+  t.rows = cfg->rows;
+  t.vocab = cfg->vocab;
+  t.top = distill->top;
+  for (t.places = 64; t.places < 2 * t.top;) t.places *= 2;
+  t.id_bytes = cfg->id_bytes;
+  t.top_bf16 = distill->top_dtype == GX_BF16;
+  t.scale = cfg->scale;
+  t.ids = in->top_ids;
+  t.logits = in->top_logits;
+  t.lse = in->top_lse;
+  t.weights = in->weights;
+  t.out = reinterpret_cast<TopRow*>(ws + l.rows);
+  t.entries = reinterpret_cast<TopEntry*>(ws + l.entries);
+  const int rows = t.top <= 64 ? 4 : 1;                        // of a workgroup
+  const size_t lds = 4 * rows * ((size_t)t.places + 2 * t.top);
+  auto read = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(cdiv(t.rows, rows)), dim3(256), lds, s, t); };
+  if (rows == 4) cfg->dtype == GX_BF16 ? read(top_kernel<bf16, 1>) : read(top_kernel<float, 1>);
+  else cfg->dtype == GX_BF16 ? read(top_kernel<bf16, 4>) : read(top_kernel<float, 4>);
+  if ((st = launched()) != GX_OK) return st;
   RowArgs a = row_args(*cfg, DISTILL, logits, dlogits, in->weights, loss);
-  a.top_ids = in->top_ids;
-  a.top_logits = in->top_logits;
-  a.top_lse = in->top_lse;
   a.top = distill->top;
-  a.top_id_bytes = cfg->id_bytes;
-  a.top_bf16 = distill->top_dtype == GX_BF16;
-  return run_rows(*cfg, a, static_cast<hipStream_t>(hip_stream));
+  a.rest = in->top_lse != nullptr;
+  a.top_rows = t.out;
+  a.entries = t.entries;
+  return run_rows(*cfg, a, false, s);
 }
 
 }  // extern "C"

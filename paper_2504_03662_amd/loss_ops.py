@@ -215,8 +215,9 @@ class DeviceDistillation(_LogitsOperator):
         out, grad_stride = self._gradient(logits, stride, out) if gradient else (None, stride)
         loss = self._new(shape, torch.float32)
         distill = gx.DistillCfg(top_ids.shape[-1], gx.GX_BF16 if top_logits.dtype == torch.bfloat16 else gx.GX_F32, 0)
-        gx.distill_loss(self._cfg(shape, id_bytes, stride, grad_stride), distill, gx.distill_in(top_ids, top_logits, top_lse, weights),
-                        logits, loss, out, self._stream())
+        cfg, stream = self._cfg(shape, id_bytes, stride, grad_stride), self._stream()
+        gx.distill_loss(cfg, distill, gx.distill_in(top_ids, top_logits, top_lse, weights), logits, loss, out,
+                        self._workspace(gx.distill_workspace_bytes(cfg, distill), stream), stream)
         return loss, out
 
     def forward(self, logits, top_ids, top_logits, top_lse=None, weights=None):

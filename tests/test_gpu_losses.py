@@ -257,8 +257,11 @@ def test_over_the_logits_and_otherwise_laid_out(name, dtype, vocab):
     got = call(view)
     lie = [(t.data_ptr() % 16, t.stride(0) * t.element_size() % 16) for t in (view, got[-1])]
     assert lie[0] == lie[1]
+    # Each of the two is off by delta in its log sums: by delta of itself where it has a factor exp(logp - old), by up to delta times
+    # the sum of weights (below 11, or 0.1 x 11 for pairs) where it is a loss
     for x, y in zip(got, want):
-        assert float((x.double() - y.double()).abs().max()) <= 4 * HALF_STEP[dtype] * float(y.double().abs().max()) + 1e-4 * (x is not got[-1])
+        bound = 4 * (HALF_STEP[dtype] + delta(vocab)) * float(y.double().abs().max()) + 22 * delta(vocab) * (x is not got[-1])
+        assert float((x.double() - y.double()).abs().max()) <= bound
     inside = z.clone()
     got = call(inside, inside)
     assert got[-1] is inside and _same(got, want)

@@ -43,7 +43,7 @@ CALLS = dict(
     token=lambda c, z=P, ids=P, a=P, b=P, d=P: gx.token_loss(c, z, ids, P, a, b, d, check=False),
     policy=lambda c, z=P, ids=P, a=P, b=P, d=P: gx.policy_loss(c, _policy(), IN, z, ids, a, b, d, check=False),
     preference=lambda c, z=P, ids=P, a=P, b=P, d=P: gx.preference_loss(c, _pairs(), IN, z, ids, a, b, d, P, check=False),
-    distill=lambda c, z=P, ids=P, a=P, d=P: gx.distill_loss(c, _distill(), gx.distill_in(ids, P, P, P), z, a, d, check=False))
+    distill=lambda c, z=P, ids=P, a=P, d=P: gx.distill_loss(c, _distill(), gx.distill_in(ids, P, P, P), z, a, d, P, check=False))
 
 
 @pytest.mark.parametrize("name", CALLS)
@@ -131,9 +131,13 @@ def test_pairs_inputs():
 
 
 def test_distillation():
-    call = lambda c, i: gx.distill_loss(_cfg(), c, i, P, P, P, check=False)
+    call = lambda c, i, ws=P: gx.distill_loss(_cfg(), c, i, P, P, P, ws, check=False)
     for kw, status in ((dict(top=0), 2), (dict(top=1025), 2), (dict(dtype=3), 4), (dict(flags=1), 6)):
         assert call(_distill(**kw), IN) == status
+        assert gx.distill_workspace_bytes(_cfg(), _distill(**kw)) == gx.distill_workspace_bytes(_cfg(rows=-1), _distill()) == 0
+    assert call(_distill(), IN, None) == 1 and call(_distill(), IN, P + 8) == 5
+    # a record of every entry
+    assert gx.distill_workspace_bytes(_cfg(rows=1000), _distill(top=64)) >= 1000 * 64 * 16
     assert call(_distill(), gx.distill_in(None, P)) == call(_distill(), gx.distill_in(P, None)) == call(None, IN) == 1
     assert call(_distill(), gx.distill_in(P, P + 2)) == call(_distill(), gx.distill_in(P, P, P + 2)) == 5
     if not torch.cuda.is_available():
@@ -146,7 +150,7 @@ def test_nothing_to_do():
     assert gx.logp_bwd(none, None, None, None, None, None, check=False) == gx.GX_OK
     assert gx.token_loss(none, None, None, None, None, None, None, check=False) == gx.GX_OK
     assert gx.policy_loss(none, _policy(), IN, None, None, None, None, None, check=False) == gx.GX_OK
-    assert gx.distill_loss(none, _distill(), IN, None, None, None, check=False) == gx.GX_OK
+    assert gx.distill_loss(none, _distill(), IN, None, None, None, None, check=False) == gx.GX_OK
 
 
 def test_scratch_grows_with_rows():
