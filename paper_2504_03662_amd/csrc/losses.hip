@@ -17,6 +17,10 @@ namespace {
 using namespace gx;
 
 constexpr int MAX_ROWS = 1 << 21, MAX_VOCAB = 1 << 19, MAX_TOP = 1024, MAX_PAIRS = 1 << 20;
+// So few rows that read their teachers in one launch with the rest; more of them in a launch before, where no registers wait for it
+constexpr int READ_HERE = 256;
+// So few rows and pairs that a launch of its own for the pairs takes longer than adding them up for every row
+constexpr int FEW_ROWS = 1024, FEW_PAIRS = 256;
 constexpr long MAX_GRID = (1 << 24) - 1;                       // workgroups of 256: a launch has less than 2^32 threads
 constexpr float NO_LOGIT = -INFINITY, MIN_SCALE = 1.f / (1 << 20);
 
@@ -67,6 +71,32 @@ struct Ids {
   }
 };
 
+// Exponential and logarithm in fp64, to about 2^-50: a power of two, and a series in what is left of it (of exp up to the 12th power for
+// |r| <= log(2) / 2, of log m = 2 atanh((m - 1) / (m + 1)) up to the 19th for m between sqrt(1/2) and sqrt(2)).  Every
+// wavefront of a row computes a few of them: a quarter of the instructions of a library's.
+GX_DEVINL double exp_f64(double x) {
+  const double c = fmin(fmax(x, -1100.0), 1100.0), n = rint(c * 1.4426950408889634074), r = fma(n, -0.69314718055994530942, c);
+  double p = 1.0 / 479001600.0;
+  const double coef[12] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0,
+                           1.0 / 6.0, 0.5, 1.0, 1.0};
+#pragma unroll
+  for (int i = 0; i < 12; i++) p = fma(p, r, coef[i]);
+  return x == x ? ldexp(p, (int)n) : x;
+}
+GX_DEVINL double log_f64(double x) {                           // of 0, of positive normal numbers or of NaN
+  int n = __builtin_amdgcn_frexp_exp(x);
+  double m = __builtin_amdgcn_frexp_mant(x);                   // 0.5 .. 1
+  if (m < 0.70710678118654752440) {
+    m *= 2.0;
+    n--;
+  }
+  const double t = (m - 1.0) / (m + 1.0), t2 = t * t;
+  double p = 2.0 / 19.0;
+#pragma unroll
+  for (int k = 17; k > 0; k -= 2) p = fma(p, t2, 2.0 / k);
+  return x == 0.0 ? -(double)INFINITY : fma((double)n, 0.69314718055994530942, p * t);
+}
+
 // Maximum and sum of exponentials (relative to the maximum) of a set of logits; the empty set has -inf and 0
 struct Sums {
   float m;
@@ -83,6 +113,8 @@ struct TopEntry {
   int col;
   float z, q, pad;
 };
+
+struct None {};
 
 enum Kind { SCORE, TOKEN, POLICY, DISTILL };
 struct RowArgs {
@@ -102,14 +134,20 @@ struct RowArgs {
   f32x2* stats;
   float* counted;
   // distillation
-  const TopRow* top_rows;
+  const TopRow* top_rows;                                      // null: the row's workgroup reads its teacher itself
   const TopEntry* entries;
-  int top, rest;
+  int top, rest, lds_bytes;                                    // lds_bytes: of a row's columns that are taken out
 };
 
 // exp(scale d) for d = z - maximum.  c_lo: the rounding of the constant would shift every term of a sum the same way.  It is
 // positive, so that d = -inf gives 0.
 GX_DEVINL float exp_scaled(float d, float c_hi, float c_lo) { return __builtin_amdgcn_exp2f(fmaf(d, c_lo, d * c_hi)); }
+
+// the same for a gradient of type T: of bf16 the constant's low part would be lost
+template <typename T>
+GX_DEVINL float exp_gradient(float d, float c_hi, float c_lo) {
+  return sizeof(T) == 2 ? __builtin_amdgcn_exp2f(d * c_hi) : exp_scaled(d, c_hi, c_lo);
+}
 
 GX_DEVINL double wave_sum_f64(double v) {
 #pragma unroll
@@ -125,7 +163,7 @@ GX_DEVINL Sums joined(Sums x, Sums y, const RowArgs& a) {
   const float m = fmaxf(x.m, y.m);
   return {m, rescaled(x, m, a) + rescaled(y, m, a)};
 }
-GX_DEVINL double log_sum(Sums x, const RowArgs& a) { return (double)a.scale * (double)x.m + log(x.s); }
+GX_DEVINL double log_sum(Sums x, const RowArgs& a) { return (double)a.scale * (double)x.m + log_f64(x.s); }
 
 template <typename T>
 GX_DEVINL void clear_row(T* row, int vocab, int tid, int threads) {
@@ -162,7 +200,7 @@ GX_DEVINL float policy_slope(const RowArgs& a, double logp, float old, float ref
   return g;
 }
 GX_DEVINL double policy_loss(const RowArgs& a, double logp, float old, float ref, float adv) {
-  const double r = exp(logp - (double)old);
+  const double r = exp_f64(logp - (double)old);
   double l = 0.0;
   if (adv != 0.f) {
     const double cut = fmin(fmax(r, 1.0 - (double)a.low), 1.0 + (double)a.high), gain = r * (double)adv;
@@ -171,12 +209,12 @@ GX_DEVINL double policy_loss(const RowArgs& a, double logp, float old, float ref
   }
   if (a.kl != 0.f) {
     const double d = (double)ref - logp;
-    l += (double)a.kl * (exp(d) - d - 1.0);
+    l += (double)a.kl * (exp_f64(d) - d - 1.0);
   }
   return l;
 }
 
-// Reads a row's teacher: WAVES wavefronts to a row, 4 to a workgroup.  Everything here is fp64 but the entry's q.
+// Reads a row's teacher with THREADS threads, in fp64 but for the entry's q.
 // An index that comes twice is one column with two entries; the first of them stands for the column, with the sum of their q.
 // Whether there is such an index is asked of a table of at least twice as many places as entries (so that a search ends), and only
 // then entries are compared with all others.
@@ -190,38 +228,16 @@ struct TopArgs {
   TopRow* out;
   TopEntry* entries;
 };
-template <typename T, int WAVES>
-__global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
-  constexpr int THREADS = 64 * WAVES, ROWS = 4 / WAVES;
-  extern __shared__ int lds_top[];
-  __shared__ double part[4];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), of_row = ROWS == 1 ? 0 : wave;
-  const int row = blockIdx.x * ROWS + of_row, tid = ROWS == 1 ? threadIdx.x : threadIdx.x & 63;
-  if (row >= a.rows) return;
-  if (a.weights && a.weights[row] == 0.f) return;              // nobody reads its record
+__host__ __device__ inline int top_words(const TopArgs& a) { return a.places + 2 * a.top; }       // of LDS for a row
+
+template <typename T, int THREADS>
+GX_DEVINL TopRow read_top(const TopArgs& a, int row, int tid, int* table, double (*part)[3]) {
+  constexpr int WAVES = THREADS / 64;
+  const int wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
   auto all_here = [] {
     if (WAVES > 1) __syncthreads();
     else __threadfence_block();
   };
-  auto sum = [&](double v) {
-    v = wave_sum_f64(v);
-    if (WAVES == 1) return v;
-    if ((threadIdx.x & 63) == 0) part[wave] = v;
-    __syncthreads();
-    v = (part[0] + part[1]) + (part[2] + part[3]);
-    __syncthreads();
-    return v;
-  };
-  auto largest = [&](float v) {
-    v = wave_max(v);
-    if (WAVES == 1) return v;
-    if ((threadIdx.x & 63) == 0) part[wave] = (double)v;
-    __syncthreads();
-    v = (float)fmax(fmax(part[0], part[1]), fmax(part[2], part[3]));
-    __syncthreads();
-    return v;
-  };
-  int* const table = lds_top + of_row * (a.places + 2 * a.top);
   int* const cols = table + a.places;
   float* const qs = reinterpret_cast<float*>(cols + a.top);
   const T* zr = static_cast<const T*>(a.z) + (size_t)row * a.stride;
@@ -244,7 +260,7 @@ __global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
   for (int i = tid; i < a.places; i += THREADS) table[i] = -1;
   all_here();
   float mz = NO_LOGIT, mt = NO_LOGIT;
-  bool again = false;
+  int again = 0;
   for (int i = tid; i < a.top; i += THREADS) {
     const int col = col_of(i);
     cols[i] = col;
@@ -253,13 +269,30 @@ __global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
     mt = fmaxf(mt, t_of(i));
     for (unsigned at = (unsigned)col * 2654435761u;; at++) {
       const int there = atomicCAS(&table[at & (a.places - 1)], -1, col);
-      if (there == col) again = true;
+      if (there == col) again = 1;
       if (there == col || there == -1) break;
     }
   }
-  const bool repeated = largest(again ? 1.f : 0.f) > 0.f;
-  mz = largest(mz);
-  mt = a.lse ? 0.f : largest(mt);
+  again = __any(again);
+  mz = wave_max(mz);
+  if (!a.lse) mt = wave_max(mt);
+  if (WAVES > 1) {
+    if ((tid & 63) == 0) {
+      part[wave][0] = (double)mz;
+      part[wave][1] = (double)mt;
+      part[wave][2] = (double)again;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < WAVES; k++) {
+      mz = fmaxf(mz, (float)part[k][0]);
+      mt = fmaxf(mt, (float)part[k][1]);
+      again |= part[k][2] != 0.0;
+    }
+    __syncthreads();
+  } else {
+    __threadfence_block();
+  }
   const double scale = (double)a.scale, ref = (double)reference(mz);
   double lse;
   if (a.lse) {
@@ -267,28 +300,37 @@ __global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
   } else {
     double s = 0.0;
     for (int i = tid; i < a.top; i += THREADS)
-      if (cols[i] >= 0) s += exp(scale * ((double)t_of(i) - (double)mt));
-    lse = scale * (double)mt + log(sum(s));
+      if (cols[i] >= 0) s += exp_f64(scale * ((double)t_of(i) - (double)mt));
+    s = wave_sum_f64(s);
+    if (WAVES > 1) {
+      if ((tid & 63) == 0) part[wave][0] = s;
+      __syncthreads();
+      s = 0.0;
+#pragma unroll
+      for (int k = 0; k < WAVES; k++) s += part[k][0];
+      __syncthreads();
+    }
+    lse = scale * (double)mt + log_f64(s);
   }
-  double q_sum = 0.0, terms = 0.0, sz = 0.0;
+  double sums[3] = {0.0, 0.0, 0.0};
   for (int i = tid; i < a.top; i += THREADS) {
     TopEntry e = {cols[i], 0.f, 0.f, 0.f};
     if (e.col >= 0) {
       e.z = z_of(i, e.col);
-      const double logq = scale * (double)t_of(i) - lse, q = exp(logq), az = scale * ((double)e.z - ref);
-      q_sum += q;
-      if (q != 0.0) terms += q * (logq - az);
+      const double logq = scale * (double)t_of(i) - lse, q = exp_f64(logq), az = scale * ((double)e.z - ref);
+      sums[0] += q;
+      if (q != 0.0) sums[1] += q * (logq - az);
       e.q = (float)q;
       qs[i] = e.q;
       bool first = true;
-      if (repeated)
+      if (again)
         for (int j = 0; j < i; j++) first &= cols[j] != e.col;
       if (!first) e.col = -1;
-      else if (a.lse) sz += exp(az);
+      else if (a.lse) sums[2] += exp_f64(az);
     }
     entries[i] = e;
   }
-  if (repeated) {
+  if (again) {
     all_here();
     for (int i = tid; i < a.top; i += THREADS) {
       if (entries[i].col < 0) continue;
@@ -298,16 +340,43 @@ __global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
       entries[i].q = q;
     }
   }
-  q_sum = sum(q_sum);
-  terms = sum(terms);
-  if (a.lse) sz = sum(sz);
-  if (tid == 0) a.out[row] = {q_sum, terms, a.lse ? fmax(0.0, 1.0 - q_sum) : 0.0, {mz, sz}};
+#pragma unroll
+  for (int n = 0; n < 3; n++) {
+    if (n == 2 && !a.lse) continue;
+    sums[n] = wave_sum_f64(sums[n]);
+    if (WAVES > 1 && (tid & 63) == 0) part[wave][n] = sums[n];
+  }
+  if (WAVES > 1) {
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 3; n++) {
+      sums[n] = 0.0;
+      if (n == 2 && !a.lse) continue;
+#pragma unroll
+      for (int k = 0; k < WAVES; k++) sums[n] += part[k][n];
+    }
+  }
+  return {sums[0], sums[1], a.lse ? fmax(0.0, 1.0 - sums[0]) : 0.0, {mz, sums[2]}};
+}
+
+// A row to a wavefront, or for more than 64 entries to a workgroup
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
+  constexpr int ROWS = 256 / THREADS;
+  extern __shared__ int lds_top[];
+  __shared__ double part[4][3];
+  const int of_group = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = blockIdx.x * ROWS + of_group, tid = ROWS == 1 ? threadIdx.x : threadIdx.x & 63;
+  if (row >= a.rows) return;
+  if (a.weights && a.weights[row] == 0.f) return;              // nobody reads its record
+  const TopRow t = read_top<T, THREADS>(a, row, tid, lds_top + of_group * top_words(a), part);
+  if (tid == 0) a.out[row] = t;
 }
 
 // A row to a workgroup of THREADS, or with 64 one to each of a workgroup's four wavefronts.  A thread has CH chunks in flight; with
 // STREAM as many of those steps as the row needs, and reads them again for the gradient, without it one.
 template <typename T, int THREADS, int CH, bool STREAM, bool TOP, bool AGAIN>
-__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_kernel(RowArgs a) {
+__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_kernel(RowArgs a, std::conditional_t<TOP, TopArgs, None> teacher) {
   constexpr int N = Lanes<T>::N, WAVES = THREADS / 64, ROWS = THREADS < 256 ? 256 / THREADS : 1;
   typedef typename Lanes<T>::type Raw;
   extern __shared__ unsigned lds[];
@@ -335,6 +404,17 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
     if (dr) clear_row(dr, a.vocab, tid, THREADS);
     return;
   }
+  __shared__ TopRow read_here[ROWS];
+  if constexpr (TOP) {
+    if (!a.top_rows) {
+      __shared__ double sums[WAVES][3];
+      const TopRow t = read_top<T, THREADS>(teacher, row, tid, reinterpret_cast<int*>(lds) + (ROWS > 1 ? wave_of_group * top_words(teacher) : 0), sums);
+      if (tid == 0) read_here[ROWS > 1 ? wave_of_group : 0] = t;
+      if (WAVES > 1) __syncthreads();
+      else __threadfence_block();
+    }
+  }
+  auto top_row = [&]() { return a.top_rows ? a.top_rows[row] : read_here[ROWS > 1 ? wave_of_group : 0]; };
   const Cut<T> k(zr, a.vocab);
   const Raw* body = reinterpret_cast<const Raw*>(zr + k.head);
   // chunk j of a step, and whether this wavefront has one
@@ -365,39 +445,40 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
 
   // With a rest, columns that have an entry are taken out of the row: the others' sum can be far smaller than theirs
   const bool take = TOP && a.rest;
-  unsigned* const columns_out = lds + (ROWS > 1 ? wave_of_group * ((k.body + 5) >> 2) : 0);   // a byte for the ends before, for each
-                                                                                            // chunk, for the ends behind
+  // a byte for each chunk, that of chunk c at c + 8; c = -1 and c = body stand for the ends
+  unsigned* const columns_out = lds + (ROWS > 1 ? wave_of_group * (a.lds_bytes / 4) : 0);
+  const unsigned char* const out_bytes = reinterpret_cast<const unsigned char*>(columns_out) + 8;
   auto all_here = [] {                                         // the threads of a row; LDS keeps a wavefront's order
     if (WAVES > 1) __syncthreads();
     else __threadfence_block();
   };
-  auto out_at = [&](int c) { return (columns_out[(c + 1) >> 2] >> ((c + 1) & 3) * 8) & 255; };
   if (take) {
-    for (int i = tid; i < (k.body + 5) >> 2; i += THREADS) columns_out[i] = 0;
+    for (int i = tid; i < a.lds_bytes / 4; i += THREADS) columns_out[i] = 0;
     all_here();
     for (int i = tid;;) {
       if (col >= 0) {
         const int at = col - k.head, c = at < 0 ? -1 : min(at / N, k.body), e = at < 0 ? col : at - c * N;
-        atomicOr(&columns_out[(c + 1) >> 2], 1u << (((c + 1) & 3) * 8 + e));
+        atomicOr(&columns_out[(c + 8) >> 2], 1u << (((c + 8) & 3) * 8 + e));
       }
       i += THREADS;
       if (i >= a.top) break;
       col = entries[i].col;
     }
     all_here();
-    if (has_end && (end_col < k.head ? out_at(-1) >> end_col : out_at(k.body) >> (end_col - k.head - k.body * N)) & 1) end = NO_LOGIT;
+    if (has_end && (end_col < k.head ? out_bytes[-1] >> end_col : out_bytes[k.body] >> (end_col - k.head - k.body * N)) & 1) end = NO_LOGIT;
   }
+  // (a thread without a chunk has a byte nevertheless, and nothing but -inf to lose)
   auto take_out = [&](int base) {
     if (!take) return;
+    unsigned on[CH];
+#pragma unroll
+    for (int j = 0; j < CH; j++) on[j] = out_bytes[chunk(base, j)];
 #pragma unroll
     for (int j = 0; j < CH; j++) {
-      const int c = chunk(base, j);
-      if (!k.has(c)) continue;
-      const unsigned on = out_at(c);
-      if (on) {
+      if (on[j]) {
 #pragma unroll
         for (int e = 0; e < N; e++)
-          if (on >> e & 1) v[j][e] = from_f32<T>(NO_LOGIT);
+          if (on[j] >> e & 1) v[j][e] = from_f32<T>(NO_LOGIT);
       }
     }
   };
@@ -450,7 +531,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
   float p_top = 0.f, ref_top = 0.f, mass = 0.f;                // TOP: p of an entry's column is p_top exp(scale (z - ref_top))
   bool others = false;                                         // TOP: whether there are columns without an entry
   if (TOP) {
-    const TopRow& t = a.top_rows[row];
+    const TopRow t = top_row();
     others = a.rest && (all.m != NO_LOGIT || all.s != 0.0);
     const double r = others ? t.rest : 0.0, total = t.q_sum + r;
     const Sums row_sums = a.rest ? joined(all, t.own, a) : all;
@@ -464,7 +545,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
   } else {
     own = -w;
     if (a.kind == POLICY) {                                    // (the others' logarithms can wait until the registers are free)
-      log_s = log(all.s);
+      log_s = log_f64(all.s);
       logp = scale * ((double)zy - (double)all.m) - log_s;
       own = w * policy_slope(a, logp, a.old_logp[row], a.kl != 0.f ? a.ref_logp[row] : 0.f, a.adv[row]);
     }
@@ -485,7 +566,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
         if (!k.has(c)) continue;
         float x[N];
 #pragma unroll
-        for (int e = 0; e < N; e++) x[e] = slope * exp_scaled(to_f32(v[j][e]) - ref, a.c_hi, a.c_lo);
+        for (int e = 0; e < N; e++) x[e] = slope * exp_gradient<T>(to_f32(v[j][e]) - ref, a.c_hi, a.c_lo);
         store_chunk(dr + k.head + (size_t)c * N, x, aligned);
       }
       if (!STREAM) break;
@@ -496,16 +577,16 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
   }
 
   if (TOP) {
-    const TopRow& t = a.top_rows[row];
+    const TopRow t = top_row();
     if (tid == 0) {
       const double r = others ? t.rest : 0.0, log_all = log_sum(a.rest ? joined(all, t.own, a) : all, a);
       double l = t.terms;
       if (t.q_sum != 0.0) l += t.q_sum * (log_all - scale * (double)reference(t.own.m));
-      if (r > 0.0) l += r * (log(r) - (log_sum(all, a) - log_all));
+      if (r > 0.0) l += r * (log_f64(r) - (log_sum(all, a) - log_all));
       a.loss[row] = (float)(weight * l);
     }
     if (!dr) return;
-    all_here();                                                // the chunks are stored
+    all_here();                                                // (the chunks are stored)
     const float ws = w * a.scale;
     for (int i = tid; i < a.top; i += THREADS) {
       const TopEntry e = entries[i];
@@ -518,7 +599,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
   const int y_tid = y < 0 ? -1 : at >= 0 && at < k.body * N ? (at / N + k.lead) % THREADS : by_end;
   if (tid != 0 && tid != y_tid) return;
   if (a.kind != POLICY) {
-    log_s = log(all.s);
+    log_s = log_f64(all.s);
     logp = scale * ((double)zy - (double)all.m) - log_s;
   }
   if (y == ELSEWHERE) logp = -(scale * (double)all.m + log_s);
@@ -536,8 +617,83 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
   if (a.kind == POLICY) a.loss[row] = (float)(weight * policy_loss(a, logp, a.old_logp[row], a.kl != 0.f ? a.ref_logp[row] : 0.f, a.adv[row]));
 }
 
+// Pairs of sequences: sequence j's reward is beta times the sum of w (logp - ref) over its tokens, the pair's loss a function of the
+// difference of two rewards, and a token's share of the gradient its weight times the pair's slope.
+struct PairArgs {
+  const void* logp;
+  const float *ref, *weights, *pair_weights;
+  const int* starts;
+  float *loss, *rewards, *dlogp;
+  int pairs, rows;
+  float beta, margin, smoothing;
+};
+GX_DEVINL int start_of(const PairArgs& a, int i) { return min(max(a.starts[i], 0), a.rows); }
+
+// A workgroup of 256 adds up a pair: two rewards, and the slope of its loss by the chosen sequence's log probability
+struct Pair {
+  int at[3];
+  double reward[2], x, slope;
+  float weight;
+  template <typename L>
+  GX_DEVINL void add_up(const PairArgs& a, int pair, double (*part)[4]) {
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int h = 0; h < 3; h++) at[h] = start_of(a, 2 * pair + h);
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      double s = 0.0;
+      for (int t = at[h] + tid; t < at[h + 1]; t += 256) {
+        const float w = a.weights ? a.weights[t] : 1.f;
+        if (w != 0.f) s += (double)w * ((double)static_cast<const L*>(a.logp)[t] - (a.ref ? (double)a.ref[t] : 0.0));
+      }
+      s = wave_sum_f64(s);
+      if ((tid & 63) == 0) part[h][tid >> 6] = s;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; h++) reward[h] = (double)a.beta * ((part[h][0] + part[h][1]) + (part[h][2] + part[h][3]));
+    weight = a.pair_weights ? a.pair_weights[pair] : 1.f;
+    x = reward[0] - reward[1] - (double)a.margin;
+    // the derivative by x is smoothing - sigmoid(-x), formed without a difference of numbers near 1
+    slope = (double)a.beta * (double)weight * ((double)a.smoothing - 1.0 / (1.0 + exp_f64(x)));
+  }
+  GX_DEVINL void write(const PairArgs& a, int pair) const {
+    const double low = log1p(exp_f64(-fabs(x))), sm = (double)a.smoothing;       // low: -log sigmoid(|x|)
+    const double l = (1.0 - sm) * (low + fmax(-x, 0.0)) + sm * (low + fmax(x, 0.0));
+    a.loss[pair] = weight != 0.f ? (float)((double)weight * (x == x ? l : x)) : 0.f;
+    if (a.rewards) {
+      a.rewards[2 * pair] = (float)reward[0];
+      a.rewards[2 * pair + 1] = (float)reward[1];
+    }
+  }
+  GX_DEVINL float by_logp(const PairArgs& a, bool rejected, int t) const {
+    const float w = a.weights ? a.weights[t] : 1.f;
+    return w != 0.f && weight != 0.f ? (float)((rejected ? -slope : slope) * (double)w) : 0.f;
+  }
+};
+
+// A workgroup to a pair, one more to the tokens of no sequence
+template <typename L>
+__global__ void __launch_bounds__(256) pairs_kernel(PairArgs a) {
+  __shared__ double part[2][4];
+  const int tid = threadIdx.x, pair = blockIdx.x;
+  if (pair == a.pairs) {
+    for (int t = tid; t < start_of(a, 0); t += 256) a.dlogp[t] = 0.f;
+    for (int t = start_of(a, 2 * a.pairs) + tid; t < a.rows; t += 256) a.dlogp[t] = 0.f;
+    return;
+  }
+  Pair p;
+  p.add_up<L>(a, pair, part);
+  if (tid == 0) p.write(a, pair);
+  if (!a.dlogp) return;
+#pragma unroll
+  for (int h = 0; h < 2; h++)
+    for (int t = p.at[h] + tid; t < p.at[h + 1]; t += 256) a.dlogp[t] = p.by_logp(a, h, t);
+}
+
 // dz = g scale (1_y - p) where p = f exp(c (u z - m)): m = lse of the whole vocabulary (u = scale, c = 1, f = 1), or what the row
 // kernel has left (u = 1, c = scale, m the maximum, f = 1 / sum).  A workgroup takes 256 * CH chunks of a row.
+// PAIRS: g comes from the row's pair, which each of its rows' workgroups adds up, and one more to a pair for the losses
 struct GradArgs {
   const void* z;
   void* dz;
@@ -548,23 +704,46 @@ struct GradArgs {
   const float *lse, *dlogp;
   const f32x2* stats;
 };
-template <typename T, int CH>
-__global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a) {
+template <typename T, int CH, bool PAIRS>
+__global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a, std::conditional_t<PAIRS, PairArgs, None> pairs) {
   constexpr int N = Lanes<T>::N;
   typedef typename Lanes<T>::type Raw;
   // from the last row on: of logits that have just been read whole, the last ones may still be near
-  const int block = gridDim.x - 1 - blockIdx.x, row = block / a.parts, part = block - row * a.parts, tid = threadIdx.x;
+  const int tid = threadIdx.x, block = a.rows * a.parts - 1 - (int)blockIdx.x, row = block < 0 ? 0 : block / a.parts, part = block - row * a.parts;
+  float dlogp = 0.f;
+  if constexpr (PAIRS) {
+    __shared__ double sums[2][4];
+    __shared__ int found;
+    Pair p;
+    if (block < 0) {
+      p.add_up<double>(pairs, -1 - block, sums);
+      if (tid == 0) p.write(pairs, -1 - block);
+      return;
+    }
+    if (tid == 0) found = -1;
+    __syncthreads();
+    for (int i = tid; i < 2 * pairs.pairs; i += 256)
+      if (start_of(pairs, i) <= row && row < start_of(pairs, i + 1)) found = i;
+    __syncthreads();
+    const int of = found;
+    if (of >= 0) {
+      p.add_up<double>(pairs, of / 2, sums);
+      dlogp = p.by_logp(pairs, of & 1, row);
+    }
+  } else {
+    dlogp = a.dlogp[row];
+  }
   const T* zr = static_cast<const T*>(a.z) + (size_t)row * a.stride;
   T* dr = static_cast<T*>(a.dz) + (size_t)row * a.grad_stride;
   const Cut<T> k(zr, a.vocab);
   const int y = a.ids.column(row, a.vocab), first = part * 256 * CH + tid - k.lead;
-  float g = a.dlogp[row] * a.scale;
+  float g = dlogp * a.scale;
   const bool aligned = ((reinterpret_cast<uintptr_t>(dr) ^ reinterpret_cast<uintptr_t>(zr)) & 15) == 0;
   const bool counts = y != IGNORED && g != 0.f;
   if (counts && y == INVALID) g = __builtin_nanf("");
   const f32x2 st = !counts ? f32x2{0.f, 0.f} : a.stats ? a.stats[row] : f32x2{a.lse[row], 1.f};
   const float slope = -g * st[1];
-  auto at = [&](float z) { return slope * exp_scaled(fmaf(z, a.unit, -st[0]), a.c_hi, a.c_lo); };
+  auto at = [&](float z) { return slope * exp_gradient<T>(fmaf(z, a.unit, -st[0]), a.c_hi, a.c_lo); };
   Raw v[CH];
   if (counts) {
 #pragma unroll
@@ -596,64 +775,6 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a) {
     const int col = k.end_at(tid);
     dr[col] = from_f32<T>(counts ? at(to_f32(zr[col])) + (col == y ? g : 0.f) : 0.f);
   }
-}
-
-// Pairs of sequences: sequence j's reward is beta times the sum of w (logp - ref) over its tokens, the pair's loss a function of the
-// difference of two rewards, and a token's share of the gradient its weight times the pair's slope.  A workgroup takes a pair, one
-// more the tokens of no sequence.
-struct PairArgs {
-  const void* logp;
-  const float *ref, *weights, *pair_weights;
-  const int* starts;
-  float *loss, *rewards, *dlogp;
-  int pairs, rows;
-  float beta, margin, smoothing;
-};
-template <typename L>
-__global__ void __launch_bounds__(256) pairs_kernel(PairArgs a) {
-  __shared__ double part[2][4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pair = blockIdx.x;
-  auto start = [&](int i) { return min(max(a.starts[i], 0), a.rows); };
-  if (pair == a.pairs) {
-    for (int t = tid; t < start(0); t += 256) a.dlogp[t] = 0.f;
-    for (int t = start(2 * a.pairs) + tid; t < a.rows; t += 256) a.dlogp[t] = 0.f;
-    return;
-  }
-  const int at[3] = {start(2 * pair), start(2 * pair + 1), start(2 * pair + 2)};
-#pragma unroll
-  for (int h = 0; h < 2; h++) {
-    double s = 0.0;
-    for (int t = at[h] + tid; t < at[h + 1]; t += 256) {
-      const float w = a.weights ? a.weights[t] : 1.f;
-      if (w != 0.f) s += (double)w * ((double)static_cast<const L*>(a.logp)[t] - (a.ref ? (double)a.ref[t] : 0.0));
-    }
-    s = wave_sum_f64(s);
-    if (lane == 0) part[h][wave] = s;
-  }
-  __syncthreads();
-  double reward[2];
-#pragma unroll
-  for (int h = 0; h < 2; h++) reward[h] = (double)a.beta * ((part[h][0] + part[h][1]) + (part[h][2] + part[h][3]));
-  const float pw = a.pair_weights ? a.pair_weights[pair] : 1.f;
-  const double x = reward[0] - reward[1] - (double)a.margin, sm = (double)a.smoothing;
-  if (tid == 0) {
-    const double low = log1p(exp(-fabs(x)));                   // -log sigmoid(|x|)
-    const double l = (1.0 - sm) * (low + fmax(-x, 0.0)) + sm * (low + fmax(x, 0.0));
-    a.loss[pair] = pw != 0.f ? (float)((double)pw * l) : 0.f;
-    if (a.rewards) {
-      a.rewards[2 * pair] = (float)reward[0];
-      a.rewards[2 * pair + 1] = (float)reward[1];
-    }
-  }
-  if (!a.dlogp) return;
-  // the derivative by x is smoothing - sigmoid(-x), formed without a difference of numbers near 1
-  const double slope = (double)a.beta * (double)pw * (sm - 1.0 / (1.0 + exp(x)));
-#pragma unroll
-  for (int h = 0; h < 2; h++)
-    for (int t = at[h] + tid; t < at[h + 1]; t += 256) {
-      const float w = a.weights ? a.weights[t] : 1.f;
-      a.dlogp[t] = w != 0.f && pw != 0.f ? (float)((h ? -slope : slope) * (double)w) : 0.f;
-    }
 }
 
 // ------------------------------------------------------------------------------- host
@@ -733,26 +854,33 @@ RowArgs row_args(const gx_logits_cfg& c, Kind kind, const void* logits, void* dl
 // 215, read twice 234.  With few rows, which do not fill the chip, more threads to a row (512 rows of 32000: 17 and 15 us).
 // Log probabilities alone, and entries to look up, do better reading twice than with 1024 threads and their barriers: 118 and 99 us, 275 and
 // 246.  The rule does not ask whether a gradient is wanted: a loss has the same bits with and without.
-gx_status run_rows(const gx_logits_cfg& c, const RowArgs& a, bool again, hipStream_t s) {
+gx_status run_rows(const gx_logits_cfg& c, RowArgs a, bool again, hipStream_t s, const TopArgs& teacher = TopArgs{}) {
   if (!device_is_gfx950()) return GX_ERR_ARCH;
   const bool bf = c.dtype == GX_BF16, top = a.kind == DISTILL;
   const int per_row = chunks_of(c, a.z, c.stride);
-  const size_t lds = !top || !a.rest ? 0 : (((size_t)per_row + 5) & ~(size_t)3) * (per_row <= 512 ? 4 : 1);
   bool refused = false;
-  auto go = [&](auto kernel, int threads) {
+  auto go = [&](auto kernel, int threads, int step, auto more) {
+    const int rows = threads < 256 ? 256 / threads : 1;
+    size_t lds = 0;
+    if (top) {                                                 // one after the other in the same place
+      a.lds_bytes = a.rest ? (per_row > 0 ? cdiv(per_row, step) : 1) * step + 16 : 0;
+      lds = a.top_rows ? 0 : (size_t)rows * 4 * top_words(teacher);
+      if (lds < (size_t)rows * a.lds_bytes) lds = (size_t)rows * a.lds_bytes;
+    }
     if (lds > 65536 &&
         hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
       refused = true;
       return;
     }
-    hipLaunchKernelGGL(kernel, dim3(cdiv(a.rows, threads < 256 ? 256 / threads : 1)), dim3(threads < 256 ? 256 : threads), lds, s, a);
+    hipLaunchKernelGGL(kernel, dim3(cdiv(a.rows, rows)), dim3(threads < 256 ? 256 : threads), lds, s, a, more);
   };
   auto with = [&](auto threads, auto ch, auto stream) {
     constexpr int TH = decltype(threads)::value, CH = decltype(ch)::value;
     constexpr bool ST = decltype(stream)::value;
-    if (top) bf ? go(loss_row_kernel<bf16, TH, CH, ST, true, false>, TH) : go(loss_row_kernel<float, TH, CH, ST, true, false>, TH);
-    else if (again) bf ? go(loss_row_kernel<bf16, TH, CH, ST, false, true>, TH) : go(loss_row_kernel<float, TH, CH, ST, false, true>, TH);
-    else bf ? go(loss_row_kernel<bf16, TH, CH, ST, false, false>, TH) : go(loss_row_kernel<float, TH, CH, ST, false, false>, TH);
+    auto run = [&](auto of_bf16, auto of_f32, auto more) { bf ? go(of_bf16, TH, TH * CH, more) : go(of_f32, TH, TH * CH, more); };
+    if (top) run(loss_row_kernel<bf16, TH, CH, ST, true, false>, loss_row_kernel<float, TH, CH, ST, true, false>, teacher);
+    else if (again) run(loss_row_kernel<bf16, TH, CH, ST, false, true>, loss_row_kernel<float, TH, CH, ST, false, true>, None());
+    else run(loss_row_kernel<bf16, TH, CH, ST, false, false>, loss_row_kernel<float, TH, CH, ST, false, false>, None());
   };
   const Flag<false> held;
   const Flag<true> twice;
@@ -763,13 +891,13 @@ gx_status run_rows(const gx_logits_cfg& c, const RowArgs& a, bool again, hipStre
   else if (per_row <= 4096 && a.rows >= 1024) with(Int<256>(), Int<16>(), held);
   else if (per_row <= 4096) with(Int<512>(), Int<8>(), held);
   else if (per_row <= 8192) with(Int<512>(), Int<16>(), held);
-  else if (per_row <= 16384 && a.kind != SCORE && !top) with(Int<1024>(), Int<16>(), held);
+  else if (per_row <= 16384 && a.kind != SCORE) with(Int<1024>(), Int<16>(), held);
   else if (per_row <= 16384) with(Int<1024>(), Int<4>(), twice);
   else with(Int<512>(), Int<8>(), twice);
   return refused ? GX_ERR_LAUNCH : launched();
 }
 
-gx_status run_grad(const gx_logits_cfg& c, GradArgs a, hipStream_t s) {
+gx_status run_grad(const gx_logits_cfg& c, GradArgs a, const PairArgs* pairs, hipStream_t s) {
   constexpr int CH = 4;
   const bool bf = c.dtype == GX_BF16;
   a.stride = (long)c.stride;
@@ -780,18 +908,21 @@ gx_status run_grad(const gx_logits_cfg& c, GradArgs a, hipStream_t s) {
   const int chunks = chunks_of(c, a.z, c.stride);
   a.parts = chunks > 0 ? cdiv(chunks, 256 * CH) : 1;
   if ((long)c.rows * a.parts > MAX_GRID) return GX_ERR_SHAPE;
-  const dim3 grid((unsigned)c.rows * (unsigned)a.parts);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
-  bf ? go(loss_grad_kernel<bf16, CH>) : go(loss_grad_kernel<float, CH>);
+  const dim3 grid((unsigned)(c.rows * a.parts + (pairs ? pairs->pairs : 0)));
+  auto go = [&](auto kernel, auto more) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, more); };
+  if (pairs) bf ? go(loss_grad_kernel<bf16, CH, true>, *pairs) : go(loss_grad_kernel<float, CH, true>, *pairs);
+  else bf ? go(loss_grad_kernel<bf16, CH, false>, None()) : go(loss_grad_kernel<float, CH, false>, None());
   return launched();
 }
 
+PairArgs pair_args(const gx_pairs_cfg& c, const gx_pairs_in& in, const float* weights, const void* logp, float* loss, float* rewards,
+                   float* dlogp) {
+  return PairArgs{logp, in.ref_logp, weights, in.pair_weights, in.starts, loss, rewards, dlogp, c.pairs, c.rows,
+                  c.beta, c.margin, c.smoothing};
+}
 template <typename L>
-gx_status run_pairs(const gx_pairs_cfg& c, const gx_pairs_in& in, const float* weights, const void* logp, float* loss, float* rewards,
-                    float* dlogp, hipStream_t s) {
-  const PairArgs a{logp, in.ref_logp, weights, in.pair_weights, in.starts, loss, rewards, dlogp, c.pairs, c.rows,
-                   c.beta, c.margin, c.smoothing};
-  hipLaunchKernelGGL(pairs_kernel<L>, dim3(c.pairs + (dlogp ? 1 : 0)), dim3(256), 0, s, a);
+gx_status run_pairs(const PairArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(pairs_kernel<L>, dim3(a.pairs + (a.dlogp ? 1 : 0)), dim3(256), 0, s, a);
   return launched();
 }
 
@@ -858,7 +989,7 @@ gx_status gx_logp_bwd(const gx_logits_cfg* cfg, const void* logits, const void* 
   a.ids = ids_of(*cfg, ids);
   a.lse = lse;
   a.dlogp = dlogp;
-  return run_grad(*cfg, a, static_cast<hipStream_t>(hip_stream));
+  return run_grad(*cfg, a, nullptr, static_cast<hipStream_t>(hip_stream));
 }
 
 gx_status gx_token_loss(const gx_logits_cfg* cfg, const void* logits, const void* ids, const float* weights, float* loss, float* logp,
@@ -913,7 +1044,7 @@ gx_status gx_pairs_loss(const gx_pairs_cfg* pairs, const gx_pairs_in* in, const 
   if (misaligned(logp, 4) || misaligned(rewards, 4) || misaligned(dlogp, 4)) return GX_ERR_ALIGN;
   if (pairs->pairs == 0 && (!dlogp || pairs->rows == 0)) return GX_OK;
   if (!device_is_gfx950()) return GX_ERR_ARCH;
-  return run_pairs<float>(*pairs, *in, in->weights, logp, loss, rewards, dlogp, static_cast<hipStream_t>(hip_stream));
+  return run_pairs<float>(pair_args(*pairs, *in, in->weights, logp, loss, rewards, dlogp), static_cast<hipStream_t>(hip_stream));
 }
 
 size_t gx_preference_workspace_bytes(const gx_logits_cfg* cfg) {
@@ -944,8 +1075,11 @@ gx_status gx_preference_loss(const gx_logits_cfg* cfg, const gx_pairs_cfg* pairs
   a.counted = reinterpret_cast<float*>(ws + l.counted);
   float* dlogp = reinterpret_cast<float*>(ws + l.dlogp);
   if (cfg->rows > 0 && (st = run_rows(*cfg, a, dlogits != nullptr, s)) != GX_OK) return st;
-  st = run_pairs<double>(*pairs, *in, a.counted, a.logp64, loss, rewards, dlogits ? dlogp : nullptr, s);
-  if (st != GX_OK || !dlogits || cfg->rows == 0) return st;
+  // few rows: the workgroups of their gradients add the pairs up themselves
+  const bool few = dlogits && cfg->rows > 0 && cfg->rows <= FEW_ROWS && pairs->pairs <= FEW_PAIRS;
+  const PairArgs p = pair_args(*pairs, *in, a.counted, a.logp64, loss, rewards, dlogits ? dlogp : nullptr);
+  if (!few && (st = run_pairs<double>(p, s)) != GX_OK) return st;
+  if (!dlogits || cfg->rows == 0) return GX_OK;
   GradArgs g = {};
   g.z = logits;
   g.dz = dlogits;
@@ -954,7 +1088,7 @@ gx_status gx_preference_loss(const gx_logits_cfg* cfg, const gx_pairs_cfg* pairs
   g.ids = a.ids;
   g.stats = a.stats;
   g.dlogp = dlogp;
-  return run_grad(*cfg, g, s);
+  return run_grad(*cfg, g, few ? &p : nullptr, s);
 }
 
 size_t gx_distill_workspace_bytes(const gx_logits_cfg* cfg, const gx_distill_cfg* distill) {
@@ -993,18 +1127,19 @@ gx_status gx_distill_loss(const gx_logits_cfg* cfg, const gx_distill_cfg* distil
   t.weights = in->weights;
   t.out = reinterpret_cast<TopRow*>(ws + l.rows);
   t.entries = reinterpret_cast<TopEntry*>(ws + l.entries);
-  const int rows = t.top <= 64 ? 4 : 1;                        // of a workgroup
-  const size_t lds = 4 * rows * ((size_t)t.places + 2 * t.top);
-  auto read = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(cdiv(t.rows, rows)), dim3(256), lds, s, t); };
-  if (rows == 4) cfg->dtype == GX_BF16 ? read(top_kernel<bf16, 1>) : read(top_kernel<float, 1>);
-  else cfg->dtype == GX_BF16 ? read(top_kernel<bf16, 4>) : read(top_kernel<float, 4>);
-  if ((st = launched()) != GX_OK) return st;
   RowArgs a = row_args(*cfg, DISTILL, logits, dlogits, in->weights, loss);
   a.top = distill->top;
   a.rest = in->top_lse != nullptr;
-  a.top_rows = t.out;
   a.entries = t.entries;
-  return run_rows(*cfg, a, false, s);
+  if (t.rows > READ_HERE) {
+    a.top_rows = t.out;
+    const int rows = t.top <= 64 ? 4 : 1;                      // of a workgroup
+    auto read = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(cdiv(t.rows, rows)), dim3(256), rows * 4 * (size_t)top_words(t), s, t); };
+    if (rows == 4) cfg->dtype == GX_BF16 ? read(top_kernel<bf16, 64>) : read(top_kernel<float, 64>);
+    else cfg->dtype == GX_BF16 ? read(top_kernel<bf16, 256>) : read(top_kernel<float, 256>);
+    if ((st = launched()) != GX_OK) return st;
+  }
+  return run_rows(*cfg, a, false, s, t);
 }
 
 }  // extern "C"

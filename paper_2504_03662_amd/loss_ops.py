@@ -15,6 +15,9 @@ from . import binding as gx
 from .decoder_ops import _need, _Operator
 
 
+_ID_BYTES = {torch.int32: 4, torch.int64: 8}
+
+
 class _LogitsOperator(_Operator):
     """Sizes and checks of an operator on logits"""
 
@@ -24,12 +27,13 @@ class _LogitsOperator(_Operator):
 
     def _rows(self, name, t, shape=None):
         """The distance between the rows of a tensor of logits"""
+        if t.is_contiguous() and t.dtype is self.tdtype and t.get_device() == self.index and t.dim() > 1 and t.shape[-1] == self.vocab and (
+                shape is None or t.shape == shape):
+            return self.vocab
         if shape is None:
             shape = t.shape
             _need(len(shape) > 1 and shape[-1] == self.vocab, f"{name}: not [..., {self.vocab}]")
         self._check(name, t, shape, self.tdtype, False)
-        if t.is_contiguous():
-            return self.vocab
         st = t.stride()
         _need(st[-1] == 1 or self.vocab == 1, f"{name}: columns are not contiguous")
         # dimensions of one row have no distance that counts
@@ -43,10 +47,11 @@ class _LogitsOperator(_Operator):
         """(where the gradient goes, the distance of its rows): `out`, or a new tensor whose rows lie as the logits' do"""
         if out is not None:
             return out, self._rows("out", out, logits.shape)
-        per = 8 if self.tdtype == torch.bfloat16 else 4             # elements of 16 bytes
-        begin = logits.data_ptr() % 16 // (16 // per)
+        begin = logits.data_ptr() % 16
         if stride == self.vocab and begin == 0:
-            return torch.empty(logits.shape, dtype=self.tdtype, device=self.device), stride
+            return torch.empty_like(logits, memory_format=torch.contiguous_format), stride
+        per = 8 if self.tdtype == torch.bfloat16 else 4             # elements of 16 bytes
+        begin //= 16 // per
         stride = self.vocab + (stride - self.vocab) % per
         flat = torch.empty(logits.numel() // self.vocab * stride + begin, dtype=self.tdtype, device=self.device)
         strides, step = [1], stride
@@ -55,19 +60,18 @@ class _LogitsOperator(_Operator):
             step *= n
         return flat.as_strided(logits.shape, strides[::-1], begin), stride
 
-    def _by_row(self, name, t, shape, dtype=torch.float32):
+    def _by_row(self, name, t, shape):
         if t is not None:
-            self._check(name, t, shape, dtype)
+            self._check(name, t, shape, torch.float32)
 
     def _ids(self, ids, shape):
-        _need(ids.dtype in (torch.int32, torch.int64), f"ids: {ids.dtype}, not int32 or int64")
+        id_bytes = _ID_BYTES.get(ids.dtype)
+        if id_bytes is None:
+            raise ValueError(f"ids: {ids.dtype}, not int32 or int64")
         self._check("ids", ids, shape, ids.dtype)
-        return ids.element_size()
+        return id_bytes
 
-    def _cfg(self, shape, id_bytes, stride, grad_stride):
-        rows = 1
-        for n in shape:
-            rows *= n
+    def _cfg(self, rows, id_bytes, stride, grad_stride):
         return gx.LogitsCfg(rows, self.vocab, self.gtype, id_bytes, 0, self.scale, stride, grad_stride, self.first_id, self.whole_vocab,
                             self.ignore_id)
 
@@ -83,8 +87,9 @@ class DeviceTokenLoss(_LogitsOperator):
         """logits [..., vocab], ids [...] -> (logp, lse), fp32.  Over a shard lse is the shard's, and logp -lse where the token is another
         shard's: of the whole vocabulary lse = logsumexp of all lse, logp = sum of all (logp + lse) - lse."""
         stride, shape = self._rows("logits", logits), logits.shape[:-1]
-        cfg = self._cfg(shape, self._ids(ids, shape), stride, stride)
-        logp, lse = self._new(shape, torch.float32), self._new(shape, torch.float32)
+        cfg = self._cfg(ids.numel(), self._ids(ids, shape), stride, stride)
+        logp = self._new(shape, torch.float32)
+        lse = torch.empty_like(logp)
         gx.logp_fwd(cfg, logits, ids, logp, lse, self._stream())
         return logp, lse
 
@@ -95,7 +100,7 @@ class DeviceTokenLoss(_LogitsOperator):
         self._check("lse", lse, shape, torch.float32)
         self._check("dlogp", dlogp, shape, torch.float32)
         out, grad_stride = self._gradient(logits, stride, out)
-        gx.logp_bwd(self._cfg(shape, id_bytes, stride, grad_stride), logits, ids, lse, dlogp, out, self._stream())
+        gx.logp_bwd(self._cfg(ids.numel(), id_bytes, stride, grad_stride), logits, ids, lse, dlogp, out, self._stream())
         return out
 
     def _run(self, logits, ids, weights, gradient, out):
@@ -103,8 +108,8 @@ class DeviceTokenLoss(_LogitsOperator):
         id_bytes = self._ids(ids, shape)
         self._by_row("weights", weights, shape)
         out, grad_stride = self._gradient(logits, stride, out) if gradient else (None, stride)
-        loss = self._new(shape, torch.float32)
-        gx.token_loss(self._cfg(shape, id_bytes, stride, grad_stride), logits, ids, weights, loss, None, out, self._stream())
+        loss = self._new(shape, torch.float32) if weights is None else torch.empty_like(weights)
+        gx.token_loss(self._cfg(ids.numel(), id_bytes, stride, grad_stride), logits, ids, weights, loss, None, out, self._stream())
         return loss, out
 
     def forward(self, logits, ids, weights=None):
@@ -133,8 +138,8 @@ class DevicePolicyLoss(_LogitsOperator):
         self._by_row("ref_logp", ref_logp, shape)
         self._by_row("weights", weights, shape)
         out, grad_stride = self._gradient(logits, stride, out) if gradient else (None, stride)
-        loss, logp = self._new(shape, torch.float32), self._new(shape, torch.float32)
-        gx.policy_loss(self._cfg(shape, id_bytes, stride, grad_stride), gx.PolicyCfg(self.clip_low, self.clip_high, self.kl, 0),
+        loss, logp = torch.empty_like(old_logp), torch.empty_like(old_logp)
+        gx.policy_loss(self._cfg(ids.numel(), id_bytes, stride, grad_stride), gx.PolicyCfg(self.clip_low, self.clip_high, self.kl, 0),
                        gx.policy_in(old_logp, advantages, ref_logp, weights), logits, ids, loss, logp, out, self._stream())
         return loss, logp, out
 
@@ -182,7 +187,7 @@ class DevicePreferenceLoss(_LogitsOperator):
         n, pairs, inputs = self._pairs(ids.numel(), shape, starts, ref_logp, weights, pair_weights)
         out, grad_stride = self._gradient(logits, stride, out) if gradient else (None, stride)
         loss, rewards = self._new((n,), torch.float32), self._new((2 * n,), torch.float32)
-        cfg, stream = self._cfg(shape, id_bytes, stride, grad_stride), self._stream()
+        cfg, stream = self._cfg(ids.numel(), id_bytes, stride, grad_stride), self._stream()
         gx.preference_loss(cfg, pairs, inputs, logits, ids, loss, rewards, out,
                            self._workspace(gx.preference_workspace_bytes(cfg), stream), stream)
         return loss, rewards, out
@@ -213,9 +218,9 @@ class DeviceDistillation(_LogitsOperator):
         self._by_row("top_lse", top_lse, shape)
         self._by_row("weights", weights, shape)
         out, grad_stride = self._gradient(logits, stride, out) if gradient else (None, stride)
-        loss = self._new(shape, torch.float32)
+        loss = self._new(shape, torch.float32) if weights is None else torch.empty_like(weights)
         distill = gx.DistillCfg(top_ids.shape[-1], gx.GX_BF16 if top_logits.dtype == torch.bfloat16 else gx.GX_F32, 0)
-        cfg, stream = self._cfg(shape, id_bytes, stride, grad_stride), self._stream()
+        cfg, stream = self._cfg(loss.numel(), id_bytes, stride, grad_stride), self._stream()
         gx.distill_loss(cfg, distill, gx.distill_in(top_ids, top_logits, top_lse, weights), logits, loss, out,
                         self._workspace(gx.distill_workspace_bytes(cfg, distill), stream), stream)
         return loss, out
