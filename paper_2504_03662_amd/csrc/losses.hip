@@ -8,6 +8,11 @@
 // about 20 instructions.
 // Sums over a thread's elements are fp32; from there on (sums over threads, log sums, losses) they are fp64, which is free: losses
 // are small differences of log sums, and a sequence's reward adds up over thousands of tokens.
+//
+// Measured, us (and TB/s of logits read and gradients written; a large copy moves 5.7): cross entropy with gradient, bf16, 8192 x 32768 196
+// (5.5), 8192 x 50001 280 (5.9), 2048 x 131072 210 (5.1), fp32 4096 x 32003 180 (5.8); 64 entries of a teacher, 8192 x 32768 213;
+// preference loss, which reads twice, 8192 x 32768 265.  Small rows are bound by the instructions that every row costs (16384 x 1000 18, 3.6),
+// few rows by latency (64 x 32000 8.7).
 #include "../../include/gx.h"
 #include "gx_kernels.h"
 #include <type_traits>
@@ -16,12 +21,15 @@ namespace {
 
 using namespace gx;
 
+// Limits of the interface.  Rows times 1024 threads, and workgroups of 256 threads, are launches of less than 2^32 threads
 constexpr int MAX_ROWS = 1 << 21, MAX_VOCAB = 1 << 19, MAX_TOP = 1024, MAX_PAIRS = 1 << 20;
-// So few rows that read their teachers in one launch with the rest; more of them in a launch before, where no registers wait for it
+constexpr long MAX_GRID = (1 << 24) - 1;
+// So few rows read their teachers in the launch that does the rest; for more there is a launch before, which is quicker at it (64 rows
+// of 32000, 16 entries, 11.8 us in one launch, 15 in two; 256 rows 13.1 and 17)
 constexpr int READ_HERE = 256;
-// So few rows and pairs that a launch of its own for the pairs takes longer than adding them up for every row
+// So few rows and pairs that a launch of its own for the pairs takes longer than adding them up for every row (131 rows of 1001 15.3 us,
+// 19 with the launch; 1001 rows of 5003 20.2 and 22.9)
 constexpr int FEW_ROWS = 1024, FEW_PAIRS = 256;
-constexpr long MAX_GRID = (1 << 24) - 1;                       // workgroups of 256: a launch has less than 2^32 threads
 constexpr float NO_LOGIT = -INFINITY, MIN_SCALE = 1.f / (1 << 20);
 
 template <int N> using Int = std::integral_constant<int, N>;
@@ -103,18 +111,17 @@ struct Sums {
   double s;
 };
 
-// What a row's teacher says, as top_kernel leaves it: the sum of q; of q (log q - scale (z - m)); 1 - sum of q, or 0; and m and
-// the sum over the student's logits that have an entry.  An entry: its column, or -1, the student's logit there, q.
+// What a row's teacher says: the sum of q; of q log q; 1 - sum of q, or 0.  An entry: its column, or -1, and its q.
 struct TopRow {
   double q_sum, terms, rest;
-  Sums own;
 };
 struct TopEntry {
-  int col;
-  float z, q, pad;
+  double q;
+  int col, pad;
 };
 
 struct None {};
+__device__ const f32x4 something = {0.f, 0.f, 0.f, 0.f};       // 16 bytes that can be read
 
 enum Kind { SCORE, TOKEN, POLICY, DISTILL };
 struct RowArgs {
@@ -136,12 +143,12 @@ struct RowArgs {
   // distillation
   const TopRow* top_rows;                                      // null: the row's workgroup reads its teacher itself
   const TopEntry* entries;
-  int top, rest, lds_bytes;                                    // lds_bytes: of a row's columns that are taken out
+  int top, rest, words, lds_bytes;                             // words of marks to a thread; LDS of a row
 };
 
-// exp(scale d) for d = z - maximum.  c_lo: the rounding of the constant would shift every term of a sum the same way.  It is
-// positive, so that d = -inf gives 0.
-GX_DEVINL float exp_scaled(float d, float c_hi, float c_lo) { return __builtin_amdgcn_exp2f(fmaf(d, c_lo, d * c_hi)); }
+// exp(scale d) for d = z - maximum.  c_lo: the rounding of the constant would shift every term of a sum the same way; the two products
+// are rounded as one sum, for the same reason.  c_lo is positive, so that d = -inf gives 0.
+GX_DEVINL float exp_scaled(float d, float c_hi, float c_lo) { return __builtin_amdgcn_exp2f(fmaf(d, c_hi, d * c_lo)); }
 
 // the same for a gradient of type T: of bf16 the constant's low part would be lost
 template <typename T>
@@ -156,12 +163,34 @@ GX_DEVINL double wave_sum_f64(double v) {
 }
 
 GX_DEVINL float reference(float m) { return m == NO_LOGIT ? 0.f : m; }
-GX_DEVINL double rescaled(Sums x, float m, const RowArgs& a) {
-  return x.s == 0.0 ? 0.0 : x.s * (double)exp_scaled(x.m - m, a.c_hi, a.c_lo);
+// exp(scale d) to 2^-32: there are few different maxima in a row of bf16, so that errors of the factors between them would not
+// average out as those of a sum's terms do.  The series as in exp_f64, up to the 8th power.
+GX_DEVINL double exp_exact(float d, const RowArgs& a) {
+  if (d == NO_LOGIT) return 0.0;
+  const double x = fmax((double)a.scale * (double)d, -1100.0), n = rint(x * 1.4426950408889634074), r = fma(n, -0.69314718055994530942, x);
+  double p = 1.0 / 40320.0;
+  const double coef[8] = {1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+#pragma unroll
+  for (int i = 0; i < 8; i++) p = fma(p, r, coef[i]);
+  return d == d ? ldexp(p, (int)n) : (double)d;
 }
-GX_DEVINL Sums joined(Sums x, Sums y, const RowArgs& a) {
-  const float m = fmaxf(x.m, y.m);
-  return {m, rescaled(x, m, a) + rescaled(y, m, a)};
+GX_DEVINL double rescaled(Sums x, float m, const RowArgs& a) { return x.s == 0.0 ? 0.0 : x.s * exp_exact(x.m - m, a); }
+// What N lanes have (a power of two), for all
+template <int N>
+GX_DEVINL Sums joined_lanes(Sums x, const RowArgs& a) {
+  float m = x.m;
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  double s = rescaled(x, m, a);
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  return {m, s};
+}
+GX_DEVINL float of_first_lane(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
+GX_DEVINL double of_first_lane(double x) {
+  const unsigned long u = __builtin_bit_cast(unsigned long, x);
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)u), hi = __builtin_amdgcn_readfirstlane((unsigned)(u >> 32));
+  return __builtin_bit_cast(double, (unsigned long)hi << 32 | lo);
 }
 GX_DEVINL double log_sum(Sums x, const RowArgs& a) { return (double)a.scale * (double)x.m + log_f64(x.s); }
 
@@ -177,17 +206,28 @@ GX_DEVINL void clear_row(T* row, int vocab, int tid, int threads) {
 // into the caches 35 to 101), and the row kernel takes 28 rather than 31 us at 1024 rows, 205 rather than 206 at 8192 of 32768, 190 rather
 // than 206 at 4096 of 64013.
 template <typename T>
-GX_DEVINL void store_chunk(T* p, const float (&x)[Lanes<T>::N], bool aligned) {
+GX_DEVINL void store_chunk(T* p, typename Lanes<T>::type v, bool aligned) {
   typedef typename Lanes<T>::type Raw;
-  Raw v;
-#pragma unroll
-  for (int e = 0; e < Lanes<T>::N; e++) v[e] = from_f32<T>(x[e]);
   if (aligned) {
     __builtin_nontemporal_store(v, reinterpret_cast<Raw*>(p));
   } else {                                                     // a gradient whose rows lie otherwise than the logits'
 #pragma unroll
     for (int e = 0; e < Lanes<T>::N; e++) p[e] = v[e];
   }
+}
+template <typename T>
+GX_DEVINL typename Lanes<T>::type rounded(const float (&x)[Lanes<T>::N]) {
+  typename Lanes<T>::type v;
+#pragma unroll
+  for (int e = 0; e < Lanes<T>::N; e++) v[e] = from_f32<T>(x[e]);
+  return v;
+}
+// Where the bits of `on` are set those of a, elsewhere those of b
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+template <typename Raw>
+GX_DEVINL Raw chosen(u32x4 on, Raw a, Raw b) {
+  const u32x4 x = __builtin_bit_cast(u32x4, a), y = __builtin_bit_cast(u32x4, b);
+  return __builtin_bit_cast(Raw, (on & x) | (~on & y));
 }
 
 // The policy loss of a token and its derivative by logp, without the weight.  A ratio beyond a border counts with the border,
@@ -209,18 +249,17 @@ GX_DEVINL double policy_loss(const RowArgs& a, double logp, float old, float ref
   }
   if (a.kl != 0.f) {
     const double d = (double)ref - logp;
-    l += (double)a.kl * (exp_f64(d) - d - 1.0);
+    const double e = exp_f64(d);
+    l += (double)a.kl * (e == (double)INFINITY ? e : e - d - 1.0);
   }
   return l;
 }
 
-// Reads a row's teacher with THREADS threads, in fp64 but for the entry's q.
+// Reads a row's teacher with THREADS threads, in fp64.
 // An index that comes twice is one column with two entries; the first of them stands for the column, with the sum of their q.
 // Whether there is such an index is asked of a table of at least twice as many places as entries (so that a search ends), and only
 // then entries are compared with all others.
 struct TopArgs {
-  const void* z;
-  long stride;
   int rows, vocab, top, places, id_bytes, top_bf16;
   float scale;
   const void *ids, *logits;
@@ -228,19 +267,19 @@ struct TopArgs {
   TopRow* out;
   TopEntry* entries;
 };
-__host__ __device__ inline int top_words(const TopArgs& a) { return a.places + 2 * a.top; }       // of LDS for a row
+__host__ __device__ inline int top_words(const TopArgs& a) { return a.places + 4 * a.top; }       // of LDS for a row
 
-template <typename T, int THREADS>
-GX_DEVINL TopRow read_top(const TopArgs& a, int row, int tid, int* table, double (*part)[3]) {
+template <int THREADS>
+GX_DEVINL TopRow read_top(const TopArgs& a, int row, int tid, double* lds, double (*part)[2]) {
   constexpr int WAVES = THREADS / 64;
   const int wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
   auto all_here = [] {
     if (WAVES > 1) __syncthreads();
     else __threadfence_block();
   };
-  int* const cols = table + a.places;
-  float* const qs = reinterpret_cast<float*>(cols + a.top);
-  const T* zr = static_cast<const T*>(a.z) + (size_t)row * a.stride;
+  double* const qs = lds;
+  int* const cols = reinterpret_cast<int*>(qs + a.top);
+  int* const table = cols + 2 * a.top;
   TopEntry* const entries = a.entries + (size_t)row * a.top;
   const size_t first_entry = (size_t)row * a.top;
   auto column = [&](int i) {
@@ -251,21 +290,17 @@ GX_DEVINL TopRow read_top(const TopArgs& a, int row, int tid, int* table, double
     return a.top_bf16 ? (float)static_cast<const bf16*>(a.logits)[first_entry + i] : static_cast<const float*>(a.logits)[first_entry + i];
   };
   // a thread's first entry stays in registers; more than THREADS entries are read again
-  const bool one = tid < a.top;
-  const int col0 = one ? column(tid) : -1;
-  const float t0 = one ? teacher(tid) : 0.f, z0 = col0 >= 0 ? to_f32(zr[col0]) : 0.f;
-  auto col_of = [&](int i) { return i == tid ? col0 : column(i); };
+  const int col0 = tid < a.top ? column(tid) : -1;
+  const float t0 = tid < a.top ? teacher(tid) : 0.f;
   auto t_of = [&](int i) { return i == tid ? t0 : teacher(i); };
-  auto z_of = [&](int i, int col) { return i == tid ? z0 : to_f32(zr[col]); };
   for (int i = tid; i < a.places; i += THREADS) table[i] = -1;
   all_here();
-  float mz = NO_LOGIT, mt = NO_LOGIT;
+  float mt = NO_LOGIT;
   int again = 0;
   for (int i = tid; i < a.top; i += THREADS) {
-    const int col = col_of(i);
+    const int col = i == tid ? col0 : column(i);
     cols[i] = col;
     if (col < 0) continue;
-    mz = fmaxf(mz, z_of(i, col));
     mt = fmaxf(mt, t_of(i));
     for (unsigned at = (unsigned)col * 2654435761u;; at++) {
       const int there = atomicCAS(&table[at & (a.places - 1)], -1, col);
@@ -274,103 +309,79 @@ GX_DEVINL TopRow read_top(const TopArgs& a, int row, int tid, int* table, double
     }
   }
   again = __any(again);
-  mz = wave_max(mz);
   if (!a.lse) mt = wave_max(mt);
   if (WAVES > 1) {
     if ((tid & 63) == 0) {
-      part[wave][0] = (double)mz;
-      part[wave][1] = (double)mt;
-      part[wave][2] = (double)again;
+      part[wave][0] = (double)mt;
+      part[wave][1] = (double)again;
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < WAVES; k++) {
-      mz = fmaxf(mz, (float)part[k][0]);
-      mt = fmaxf(mt, (float)part[k][1]);
-      again |= part[k][2] != 0.0;
+      mt = fmaxf(mt, (float)part[k][0]);
+      again |= part[k][1] != 0.0;
     }
     __syncthreads();
   } else {
     __threadfence_block();
   }
-  const double scale = (double)a.scale, ref = (double)reference(mz);
-  double lse;
-  if (a.lse) {
-    lse = (double)a.lse[row];
-  } else {
-    double s = 0.0;
-    for (int i = tid; i < a.top; i += THREADS)
-      if (cols[i] >= 0) s += exp_f64(scale * ((double)t_of(i) - (double)mt));
-    s = wave_sum_f64(s);
-    if (WAVES > 1) {
-      if ((tid & 63) == 0) part[wave][0] = s;
-      __syncthreads();
-      s = 0.0;
-#pragma unroll
-      for (int k = 0; k < WAVES; k++) s += part[k][0];
-      __syncthreads();
-    }
-    lse = scale * (double)mt + log_f64(s);
-  }
-  double sums[3] = {0.0, 0.0, 0.0};
+  // q = e / total: the entries' own exponentials, or those by the teacher's log sum
+  const double scale = (double)a.scale, lse = a.lse ? (double)a.lse[row] : scale * (double)mt;
+  double sums[2] = {0.0, 0.0};
   for (int i = tid; i < a.top; i += THREADS) {
-    TopEntry e = {cols[i], 0.f, 0.f, 0.f};
-    if (e.col >= 0) {
-      e.z = z_of(i, e.col);
-      const double logq = scale * (double)t_of(i) - lse, q = exp_f64(logq), az = scale * ((double)e.z - ref);
-      sums[0] += q;
-      if (q != 0.0) sums[1] += q * (logq - az);
-      e.q = (float)q;
-      qs[i] = e.q;
-      bool first = true;
-      if (again)
-        for (int j = 0; j < i; j++) first &= cols[j] != e.col;
-      if (!first) e.col = -1;
-      else if (a.lse) sums[2] += exp_f64(az);
-    }
-    entries[i] = e;
-  }
-  if (again) {
-    all_here();
-    for (int i = tid; i < a.top; i += THREADS) {
-      if (entries[i].col < 0) continue;
-      float q = qs[i];
-      for (int j = i + 1; j < a.top; j++)
-        if (cols[j] == cols[i]) q += qs[j];
-      entries[i].q = q;
-    }
+    if (cols[i] < 0) continue;
+    const double x = scale * (double)t_of(i) - lse, e = exp_f64(x);
+    qs[i] = e;
+    sums[0] += e;
+    if (e != 0.0) sums[1] += e * x;
   }
 #pragma unroll
-  for (int n = 0; n < 3; n++) {
-    if (n == 2 && !a.lse) continue;
+  for (int n = 0; n < 2; n++) {
     sums[n] = wave_sum_f64(sums[n]);
     if (WAVES > 1 && (tid & 63) == 0) part[wave][n] = sums[n];
   }
+  all_here();
   if (WAVES > 1) {
-    __syncthreads();
 #pragma unroll
-    for (int n = 0; n < 3; n++) {
+    for (int n = 0; n < 2; n++) {
       sums[n] = 0.0;
-      if (n == 2 && !a.lse) continue;
 #pragma unroll
       for (int k = 0; k < WAVES; k++) sums[n] += part[k][n];
     }
   }
-  return {sums[0], sums[1], a.lse ? fmax(0.0, 1.0 - sums[0]) : 0.0, {mz, sums[2]}};
+  const double total = a.lse || sums[0] == 0.0 ? 1.0 : sums[0], by = 1.0 / total;
+  for (int i = tid; i < a.top; i += THREADS) {
+    int col = cols[i];
+    double q = col < 0 ? 0.0 : qs[i];
+    if (again && col >= 0) {
+      for (int j = 0; j < i; j++)
+        if (cols[j] == cols[i]) col = -1;
+      for (int j = i + 1; j < a.top; j++)
+        if (cols[j] == cols[i]) q += qs[j];
+    }
+    entries[i] = {q * by, col, 0};
+  }
+  // sum of q log q = sum of (e / total) (x - log total)
+  return {sums[0] * by, sums[1] * by - (total == 1.0 ? 0.0 : sums[0] * by * log_f64(total)), a.lse ? fmax(0.0, 1.0 - sums[0]) : 0.0};
 }
 
 // A row to a wavefront, or for more than 64 entries to a workgroup
-template <typename T, int THREADS>
+template <int THREADS>
 __global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
   constexpr int ROWS = 256 / THREADS;
-  extern __shared__ int lds_top[];
-  __shared__ double part[4][3];
+  extern __shared__ double lds_top[];
+  __shared__ double part[4][2];
   const int of_group = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = blockIdx.x * ROWS + of_group, tid = ROWS == 1 ? threadIdx.x : threadIdx.x & 63;
   if (row >= a.rows) return;
   if (a.weights && a.weights[row] == 0.f) return;              // nobody reads its record
-  const TopRow t = read_top<T, THREADS>(a, row, tid, lds_top + of_group * top_words(a), part);
+  const TopRow t = read_top<THREADS>(a, row, tid, lds_top + of_group * (top_words(a) / 2), part);
   if (tid == 0) a.out[row] = t;
+}
+
+// LDS of a row's entries: two chunks to a slot, the ends' numbers, marks and slots of the threads
+__host__ __device__ inline int top_bytes(int top, int words, int threads) {
+  return (32 * (top + 1) + 64 + 4 * (words * threads + 2 + threads) + 15) & ~15;
 }
 
 // A row to a workgroup of THREADS, or with 64 one to each of a workgroup's four wavefronts.  A thread has CH chunks in flight; with
@@ -379,12 +390,13 @@ template <typename T, int THREADS, int CH, bool STREAM, bool TOP, bool AGAIN>
 __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_kernel(RowArgs a, std::conditional_t<TOP, TopArgs, None> teacher) {
   constexpr int N = Lanes<T>::N, WAVES = THREADS / 64, ROWS = THREADS < 256 ? 256 / THREADS : 1;
   typedef typename Lanes<T>::type Raw;
-  extern __shared__ unsigned lds[];
+  extern __shared__ __attribute__((aligned(16))) char group_lds[];
   __shared__ Sums part[WAVES];
   const int wave_of_group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int row = ROWS == 1 ? blockIdx.x : blockIdx.x * ROWS + wave_of_group;
   if (ROWS > 1 && row >= a.rows) return;
   const int tid = ROWS == 1 ? threadIdx.x : lane, wave = ROWS == 1 ? wave_of_group : 0;
+  char* const lds = group_lds + (ROWS > 1 ? wave_of_group * a.lds_bytes : 0);          // the row's own
   const T* zr = static_cast<const T*>(a.z) + (size_t)row * a.stride;
   T* dr = a.dz ? static_cast<T*>(a.dz) + (size_t)row * a.grad_stride : nullptr;
   const float w = a.weights ? a.weights[row] : 1.f;
@@ -407,8 +419,8 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
   __shared__ TopRow read_here[ROWS];
   if constexpr (TOP) {
     if (!a.top_rows) {
-      __shared__ double sums[WAVES][3];
-      const TopRow t = read_top<T, THREADS>(teacher, row, tid, reinterpret_cast<int*>(lds) + (ROWS > 1 ? wave_of_group * top_words(teacher) : 0), sums);
+      __shared__ double sums[WAVES][2];
+      const TopRow t = read_top<THREADS>(teacher, row, tid, reinterpret_cast<double*>(lds), sums);
       if (tid == 0) read_here[ROWS > 1 ? wave_of_group : 0] = t;
       if (WAVES > 1) __syncthreads();
       else __threadfence_block();
@@ -416,23 +428,34 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
   }
   auto top_row = [&]() { return a.top_rows ? a.top_rows[row] : read_here[ROWS > 1 ? wave_of_group : 0]; };
   const Cut<T> k(zr, a.vocab);
-  const Raw* body = reinterpret_cast<const Raw*>(zr + k.head);
+  // Loads are without branches (a thread beyond the row's ends reads its first or last chunk, and of a row without a chunk something
+  // else), so that it is known at each use how many are still under way.
+  const Raw* body = k.body > 0 ? reinterpret_cast<const Raw*>(zr + k.head) : reinterpret_cast<const Raw*>(&something);
+  const int last = max(k.body - 1, 0);
+  Raw v[CH];
   // chunk j of a step, and whether this wavefront has one
   auto chunk = [&](int base, int j) { return base + j * THREADS + tid - k.lead; };
+  auto blank = [&](int base) {                                 // what is beyond the ends
+#pragma unroll
+    for (int j = 0; j < CH; j++) {
+      const int first = base + j * THREADS + wave * 64 - k.lead;
+      if (first >= 0 && first + 64 <= k.body) continue;
+      if (!k.has(chunk(base, j))) v[j] = splat<T>(NO_LOGIT);
+    }
+  };
   auto there = [&](int base, int j) { return base + j * THREADS + wave * 64 - k.lead < k.body; };
   const TopEntry* entries = TOP ? a.entries + (size_t)row * a.top : nullptr;
   int col = -1;
-  if (TOP && a.rest && tid < a.top) col = entries[tid].col;
-  Raw v[CH];
+  if (TOP) {
+    col = entries[min(tid, a.top - 1)].col;
+    if (tid >= a.top) col = -1;
+  }
   auto load = [&](int base, auto past) {
 #pragma unroll
     for (int j = 0; j < CH; j++) {
-      const int c = chunk(base, j);
-      v[j] = splat<T>(NO_LOGIT);
-      if (k.has(c)) {
-        if (decltype(past)::value) v[j] = __builtin_nontemporal_load(body + c);
-        else v[j] = body[c];
-      }
+      const int c = min(max(chunk(base, j), 0), last);
+      if (decltype(past)::value) v[j] = __builtin_nontemporal_load(body + c);
+      else v[j] = body[c];
     }
   };
   const Flag<!AGAIN && !STREAM> only_time;                     // a row that is read twice is to stay near in between
@@ -443,105 +466,225 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
   float zy = 0.f;
   if (!TOP && y >= 0) zy = to_f32(zr[y]);
 
-  // With a rest, columns that have an entry are taken out of the row: the others' sum can be far smaller than theirs
-  const bool take = TOP && a.rest;
-  // a byte for each chunk, that of chunk c at c + 8; c = -1 and c = body stand for the ends
-  unsigned* const columns_out = lds + (ROWS > 1 ? wave_of_group * (a.lds_bytes / 4) : 0);
-  const unsigned char* const out_bytes = reinterpret_cast<const unsigned char*>(columns_out) + 8;
   auto all_here = [] {                                         // the threads of a row; LDS keeps a wavefront's order
     if (WAVES > 1) __syncthreads();
     else __threadfence_block();
   };
-  if (take) {
-    for (int i = tid; i < a.lds_bytes / 4; i += THREADS) columns_out[i] = 0;
-    all_here();
-    for (int i = tid;;) {
-      if (col >= 0) {
-        const int at = col - k.head, c = at < 0 ? -1 : min(at / N, k.body), e = at < 0 ? col : at - c * N;
-        atomicOr(&columns_out[(c + 8) >> 2], 1u << (((c + 8) & 3) * 8 + e));
-      }
-      i += THREADS;
-      if (i >= a.top) break;
-      col = entries[i].col;
+  // TOP: chunks with an entry's column are marked, bit by bit for the thread that has them, and have a slot in LDS: the bits of those
+  // columns, and a chunk in which their logits go to the entries' threads and their gradients come back, so that they are stored
+  // with the rest of their chunks.  (One by one they are a sector of memory each, read and written: 16 / 64 / 256 of 32768 columns,
+  // 8192 rows, 214 / 223 / 334 us, so 210 / 213 / 237.)  Which slot is whose depends on the order in which threads ask, and nothing
+  // else does.  All of it but the logits is there before the row is.
+  u32x4* const columns = reinterpret_cast<u32x4*>(lds);
+  Raw* const staged = reinterpret_cast<Raw*>(columns + a.top + 1);            // the last slot is for chunks without a column
+  float* const end_value = reinterpret_cast<float*>(staged + a.top + 1);
+  unsigned* const marks = reinterpret_cast<unsigned*>(end_value + 16);
+  unsigned* const end_marks = marks + a.words * THREADS;
+  int* const slots = reinterpret_cast<int*>(end_marks + 2), *const slots_taken = slots - 1;
+  // an entry's place: an end, or an element of a slot
+  auto is_end = [&](int col) { return (unsigned)(col - k.head) >= (unsigned)(k.body * N); };
+  auto end_of = [&](int col) { return col < k.head ? col : col - (k.vocab - k.ends); };
+  auto element = [&](int col) {
+    const int c = (col - k.head) / N + k.lead, owner = c % THREADS, n = c / THREADS;
+    int slot = slots[owner];
+    for (int i = 0; i < n >> 5; i++) slot += __popc(marks[i * THREADS + owner]);
+    slot += __popc(marks[(n >> 5) * THREADS + owner] & ((1u << (n & 31)) - 1));
+    return slot * N + (col - k.head) % N;
+  };
+  auto each_entry = [&](auto f) {
+    for (int i = tid; i < a.top; i += THREADS) {
+      if (i != tid) col = entries[i].col;
+      if (col >= 0) f(i, col);
     }
+    if (a.top > THREADS && tid < a.top) col = entries[tid].col;
+  };
+  if (TOP) {
+    for (int i = tid; i < a.words * THREADS + 2; i += THREADS) marks[i] = 0;
+    if (tid == 0) columns[a.top] = u32x4{0, 0, 0, 0};
     all_here();
-    if (has_end && (end_col < k.head ? out_bytes[-1] >> end_col : out_bytes[k.body] >> (end_col - k.head - k.body * N)) & 1) end = NO_LOGIT;
+    each_entry([&](int, int at) {
+      if (is_end(at)) {
+        atomicOr(end_marks, 1u << end_of(at));
+      } else {
+        const int c = (at - k.head) / N + k.lead, n = c / THREADS;
+        atomicOr(&marks[(n >> 5) * THREADS + c % THREADS], 1u << (n & 31));
+      }
+    });
+    all_here();
+    int mine = 0;
+    for (int i = 0; i < a.words; i++) mine += __popc(marks[i * THREADS + tid]);
+    const int first = mine ? atomicAdd(slots_taken, mine) : 0;
+    slots[tid] = first;
+    for (int i = 0; i < mine; i++) columns[first + i] = u32x4{0, 0, 0, 0};
+    all_here();
+    each_entry([&](int, int at) {
+      if (is_end(at)) return;
+      if (sizeof(T) == 2) reinterpret_cast<unsigned short*>(columns)[element(at)] = 0xffff;
+      else reinterpret_cast<unsigned*>(columns)[element(at)] = 0xffffffffu;
+    });
+    all_here();
+    if (has_end) end_value[tid] = end;
   }
-  // (a thread without a chunk has a byte nevertheless, and nothing but -inf to lose)
+  int slot = TOP ? slots[tid] : 0;
+  // f(slot) for the thread's chunk of a step where any of the wavefront's chunks is marked
+  auto if_marked = [&](int base, int j, auto f) {
+    const int n = base / THREADS + j;
+    const unsigned on = marks[(n >> 5) * THREADS + tid] >> (n & 31) & 1;
+    if (!__any(on)) return;
+    f(on ? slot : a.top);
+    slot += on;
+  };
+  float most = TOP ? end : NO_LOGIT;                           // of what is taken out, and perhaps of others
   auto take_out = [&](int base) {
-    if (!take) return;
-    unsigned on[CH];
-#pragma unroll
-    for (int j = 0; j < CH; j++) on[j] = out_bytes[chunk(base, j)];
 #pragma unroll
     for (int j = 0; j < CH; j++) {
-      if (on[j]) {
+      if (!there(base, j)) break;
+      if_marked(base, j, [&](int here) {
+        if (here != a.top) staged[here] = v[j];
+        if (a.rest) {
 #pragma unroll
-        for (int e = 0; e < N; e++)
-          if (on[j] >> e & 1) v[j][e] = from_f32<T>(NO_LOGIT);
-      }
+          for (int e = 0; e < N; e++) most = fmaxf(most, to_f32(v[j][e]));
+          v[j] = chosen(columns[here], splat<T>(NO_LOGIT), v[j]);
+        }
+      });
     }
   };
 
-  // maximum and sum of this thread's elements
-  float m = end, s = end == NO_LOGIT ? 0.f : 1.f;
-  if (end != end) s = end;                                     // NaN stays one
+  // With a rest the columns that have an entry are taken out of the row: the others' sum can be far smaller than theirs
+  if (TOP && has_end && a.rest && *end_marks >> tid & 1) end = NO_LOGIT;
+
+  // The wavefront's maximum, and the sums of its threads relative to that: threads with maxima of their own would need an exponential
+  // in fp64 each to join them
+  float m = NO_LOGIT;
+  double s = 0.0;
   for (int base = 0;;) {
-    take_out(base);
-    float top_here = m;
+    blank(base);
+    if (TOP) take_out(base);
+    float top_here = end;                                      // (the last that was asked for)
 #pragma unroll
     for (int j = 0; j < CH; j++) {
       if (!there(base, j)) break;
 #pragma unroll
       for (int e = 0; e < N; e++) top_here = fmaxf(top_here, to_f32(v[j][e]));
     }
+    top_here = of_first_lane(wave_max(STREAM ? fmaxf(m, top_here) : top_here));
     const float ref = reference(top_here);
-    if (s != 0.f) s *= exp_scaled(m - ref, a.c_hi, a.c_lo);
+    if (STREAM && m != top_here) s *= exp_exact(m - ref, a);
     m = top_here;
+    // A divergence is a small difference of log sums, and a reward the sum of many.  For them (`exact`) what roundings leave is added up
+    // too: of the exponents (a row of bf16 has few differences d, whose errors do not average out; of d = -inf it is no number, and
+    // made one) and of the sum, which starts from 1, so that no term is larger.  4 us of 270 for 8192 rows of 32768.
+    auto add = [&](auto exact) {
+      constexpr bool EXACT = decltype(exact)::value;
+      float sum = EXACT ? 1.f : 0.f, left = 0.f, lost = 0.f;
 #pragma unroll
-    for (int j = 0; j < CH; j++) {
-      if (!there(base, j)) break;
+      for (int j = 0; j < CH; j++) {
+        if (!there(base, j)) break;
 #pragma unroll
-      for (int e = 0; e < N; e++) s += exp_scaled(to_f32(v[j][e]) - ref, a.c_hi, a.c_lo);
-    }
+        for (int e = 0; e < N; e++) {
+          const float d = to_f32(v[j][e]) - ref;
+          if (EXACT) {
+            const float t = d * a.c_hi, x = __builtin_amdgcn_exp2f(t), more = sum + x;
+            left = fmaf(x, __builtin_amdgcn_fmed3f(fmaf(d, a.c_lo, fmaf(d, a.c_hi, -t)), -1.f, 1.f), left);
+            lost += (sum - more) + x;
+            sum = more;
+          } else {
+            sum += exp_scaled(d, a.c_hi, a.c_lo);
+          }
+        }
+      }
+      s += EXACT ? (double)(sum - 1.f) + (double)lost + (double)left * 0.69314718055994530942 : (double)sum;
+    };
+    if (TOP || ((AGAIN || STREAM) && a.logp64)) add(Flag<true>());
+    else add(Flag<false>());
     if (!STREAM) break;
     base += THREADS * CH;
     if (base >= k.body + k.lead) break;
     load(base, only_time);
   }
-  Sums all;
-  all.m = wave_max(m);
-  all.s = wave_sum_f64(rescaled({m, (double)s}, all.m, a));
+  if (has_end) s += exp_exact(end - reference(m), a);
+  Sums all = {m, wave_sum_f64(s)};
+  if (TOP && a.rest) most = wave_max(most);
   if (WAVES > 1) {
-    if (lane == 0) part[wave] = all;
+    __shared__ float most_part[TOP ? WAVES : 1];
+    if (lane == 0) {
+      part[wave] = all;
+      if (TOP) most_part[wave] = most;
+    }
     __syncthreads();
-    all.m = part[0].m;
-#pragma unroll
-    for (int i = 1; i < WAVES; i++) all.m = fmaxf(all.m, part[i].m);
-    all.s = 0.0;
-#pragma unroll
-    for (int i = 0; i < WAVES; i++) all.s += rescaled(part[i], all.m, a);
+    if (TOP) most = wave_max(lane < WAVES ? most_part[lane] : NO_LOGIT);
+    all = joined_lanes<WAVES>(lane < WAVES ? part[lane] : Sums{NO_LOGIT, 0.0}, a);
   }
+  all = {of_first_lane(all.m), of_first_lane(all.s)};          // (one register for all lanes)
+  if (TOP) most = of_first_lane(most);
 
   // the gradient is slope * exp(scale (z - ref)) of every element that has no value of its own
   const double scale = (double)a.scale;
   const double weight = (double)w;
   float ref = all.m, slope = 0.f, own = 0.f;                   // own: the gradient by logp
   double logp = 0.0, log_s = 0.0;
-  float p_top = 0.f, ref_top = 0.f, mass = 0.f;                // TOP: p of an entry's column is p_top exp(scale (z - ref_top))
+  Sums row_sums = all;                                         // TOP with a rest: with the entries' columns
+  double q_z = 0.0;                                            // TOP: sum of q z over the entries
   bool others = false;                                         // TOP: whether there are columns without an entry
   if (TOP) {
     const TopRow t = top_row();
+    // sums over the entries: of q z, and with a rest of their columns' exponentials
+    Sums taken = {fmaxf(most, all.m), 0.0};
+    const float from = reference(taken.m);
+    if (WAVES == 1) all_here();
+    const T* const staged_values = reinterpret_cast<const T*>(staged);
+    each_entry([&](int i, int at) {
+      const float z = is_end(at) ? end_value[end_of(at)] : to_f32(staged_values[element(at)]);
+      const double q = entries[i].q;
+      if (q != 0.0) q_z += q * (double)z;
+      if (a.rest) taken.s += exp_exact(z - from, a);
+    });
+    q_z = wave_sum_f64(q_z);
+    if (a.rest) taken.s = wave_sum_f64(taken.s);
+    if (WAVES > 1) {
+      __shared__ double entries_part[WAVES][2];
+      if (lane == 0) {
+        entries_part[wave][0] = q_z;
+        entries_part[wave][1] = taken.s;
+      }
+      __syncthreads();
+      q_z = taken.s = 0.0;
+      for (int i = 0; i < WAVES && 64 * i < a.top; i++) {      // no entry from there on
+        q_z += entries_part[i][0];
+        taken.s += entries_part[i][1];
+      }
+    }
+    q_z = of_first_lane(q_z);
+    taken.s = of_first_lane(taken.s);
     others = a.rest && (all.m != NO_LOGIT || all.s != 0.0);
     const double r = others ? t.rest : 0.0, total = t.q_sum + r;
-    const Sums row_sums = a.rest ? joined(all, t.own, a) : all;
+    double of_others = all.s;                                  // their sum, relative to the row's maximum
+    if (a.rest) {
+      of_others = rescaled(all, taken.m, a);
+      row_sums = {taken.m, of_others + taken.s};
+    }
     // total p - r exp(a - lse of the others), and what that is relative to the others' own sum
-    slope = (float)(weight * scale * (total * rescaled(all, row_sums.m, a) / row_sums.s - r) / all.s);
+    slope = of_first_lane((float)(weight * scale * (total * of_others / row_sums.s - r) / all.s));
+    row_sums = {of_first_lane(row_sums.m), of_first_lane(row_sums.s)};
     if (a.rest && !others && row_sums.s != 0.0) slope = 0.f;   // there is nothing to write, or zeros
     ref = reference(all.m);
-    ref_top = row_sums.m;
-    p_top = (float)(1.0 / row_sums.s);
-    mass = (float)total;
+    if (dr) {
+      const float mass_p = (float)(total / row_sums.s);
+      const double ws = weight * scale;
+      each_entry([&](int i, int at) {
+        auto gradient = [&](float z) {
+          return (float)(ws * ((double)(mass_p * exp_scaled(z - row_sums.m, a.c_hi, a.c_lo)) - entries[i].q));
+        };
+        if (is_end(at)) {
+          float& z = end_value[end_of(at)];
+          z = gradient(z);
+        } else {
+          T& z = reinterpret_cast<T*>(staged)[element(at)];
+          z = from_f32<T>(gradient(to_f32(z)));
+        }
+      });
+      all_here();
+    }
   } else {
     own = -w;
     if (a.kind == POLICY) {                                    // (the others' logarithms can wait until the registers are free)
@@ -555,11 +698,9 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
 
   if (dr) {
     const bool aligned = ((reinterpret_cast<uintptr_t>(dr) ^ reinterpret_cast<uintptr_t>(zr)) & 15) == 0;
+    if (TOP) slot = slots[tid];
     for (int base = 0;;) {
-      if (STREAM) {
-        load(base, Flag<true>());
-        take_out(base);
-      }
+      if (STREAM) load(base, Flag<true>());
 #pragma unroll
       for (int j = 0; j < CH; j++) {
         const int c = chunk(base, j);
@@ -567,31 +708,31 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
         float x[N];
 #pragma unroll
         for (int e = 0; e < N; e++) x[e] = slope * exp_gradient<T>(to_f32(v[j][e]) - ref, a.c_hi, a.c_lo);
-        store_chunk(dr + k.head + (size_t)c * N, x, aligned);
+        Raw d = rounded<T>(x);
+        if (TOP) {
+          if_marked(base, j, [&](int here) { d = chosen(columns[here], staged[here], d); });
+        }
+        store_chunk(dr + k.head + (size_t)c * N, d, aligned);
       }
       if (!STREAM) break;
       base += THREADS * CH;
       if (base >= k.body + k.lead) break;
     }
-    if (has_end && (TOP || end_col != y)) dr[end_col] = from_f32<T>(slope * exp_scaled(end - ref, a.c_hi, a.c_lo));
+    if (has_end && (TOP || end_col != y)) {
+      float x = slope * exp_scaled(end - ref, a.c_hi, a.c_lo);
+      if (TOP && *end_marks >> tid & 1) x = end_value[tid];
+      dr[end_col] = from_f32<T>(x);
+    }
   }
 
   if (TOP) {
+    if (tid > 0) return;
     const TopRow t = top_row();
-    if (tid == 0) {
-      const double r = others ? t.rest : 0.0, log_all = log_sum(a.rest ? joined(all, t.own, a) : all, a);
-      double l = t.terms;
-      if (t.q_sum != 0.0) l += t.q_sum * (log_all - scale * (double)reference(t.own.m));
-      if (r > 0.0) l += r * (log_f64(r) - (log_sum(all, a) - log_all));
-      a.loss[row] = (float)(weight * l);
-    }
-    if (!dr) return;
-    all_here();                                                // (the chunks are stored)
-    const float ws = w * a.scale;
-    for (int i = tid; i < a.top; i += THREADS) {
-      const TopEntry e = entries[i];
-      if (e.col >= 0) dr[e.col] = from_f32<T>(ws * (mass * p_top * exp_scaled(e.z - ref_top, a.c_hi, a.c_lo) - e.q));
-    }
+    const double r = others ? t.rest : 0.0, log_all = log_sum(row_sums, a);
+    double l = t.terms;
+    if (t.q_sum != 0.0) l += t.q_sum * log_all - scale * q_z;
+    if (r > 0.0) l += r * (log_f64(r) - (log_sum(all, a) - log_all));
+    a.loss[row] = (float)(weight * l);
     return;
   }
   // the thread that has stored the chunk around y, or could have: it overwrites y after that
@@ -769,7 +910,7 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a, std::conditi
         if (k.head + c * N + e == y) x[e] += g;
       }
     }
-    store_chunk(dr + k.head + (size_t)c * N, x, aligned);
+    store_chunk(dr + k.head + (size_t)c * N, rounded<T>(x), aligned);
   }
   if (part == 0 && tid < k.ends) {
     const int col = k.end_at(tid);
@@ -847,25 +988,28 @@ RowArgs row_args(const gx_logits_cfg& c, Kind kind, const void* logits, void* dl
   return a;
 }
 
-// again: the logits are read once more right after this.
-// Rows stay in registers while a workgroup has room for them: the fewest threads that hold one in 16 chunks each do best (8192
-// rows of 8000 / 16384 / 32768, bf16 cross entropy with gradient: 256 threads 51 / 96 / 200 us, 512 threads 57 / 104 / 203; read twice 60 / 101 / 219), up to
-// 512 columns or so a wavefront a row; 50001: 294, read twice 335; 131072: 1024 threads with nothing beside them on a compute unit
-// 215, read twice 234.  With few rows, which do not fill the chip, more threads to a row (512 rows of 32000: 17 and 15 us).
-// Log probabilities alone, and entries to look up, do better reading twice than with 1024 threads and their barriers: 118 and 99 us, 275 and
-// 246.  The rule does not ask whether a gradient is wanted: a loss has the same bits with and without.
+// again: the logits are read once more right after this, perhaps.
+// Rows stay in registers while a workgroup has room for them, and up to 512 chunks a wavefront has one.  Cross entropy with gradient,
+// bf16, us: 16384 rows of 1000, a wavefront with 4 / 8 chunks to a thread 18.1 / 18.6, 256 threads 37.5; 8192 rows of 4096 26.3, 256
+// threads 28.6; of 8000, 256 threads with 4 / 8 chunks 47.1 / 47.5; of 16384, 256 threads with 8 / 16 90.6 / 93.4, read twice 99; of
+// 32768, 512 threads with 8 196, 256 with 16 202, read twice 212; of 50001, 512 with 16 279, read twice 319; 2048 rows of
+// 131072, 1024 threads with 16 210, read twice 231.
+// Only the last shape has a compute unit for one row alone.  With a teacher's entries, whose barriers nothing hides there, and for
+// log probabilities, which are not written, reading twice is better: 2048 x 131072, 64 entries, 247 and 274 us; log probabilities 96
+// and 118.  (The rule does not ask whether a gradient is wanted: a loss has the same bits with and without.)
 gx_status run_rows(const gx_logits_cfg& c, RowArgs a, bool again, hipStream_t s, const TopArgs& teacher = TopArgs{}) {
   if (!device_is_gfx950()) return GX_ERR_ARCH;
   const bool bf = c.dtype == GX_BF16, top = a.kind == DISTILL;
   const int per_row = chunks_of(c, a.z, c.stride);
   bool refused = false;
-  auto go = [&](auto kernel, int threads, int step, auto more) {
+  auto go = [&](auto kernel, int threads, auto more) {
     const int rows = threads < 256 ? 256 / threads : 1;
     size_t lds = 0;
-    if (top) {                                                 // one after the other in the same place
-      a.lds_bytes = a.rest ? (per_row > 0 ? cdiv(per_row, step) : 1) * step + 16 : 0;
-      lds = a.top_rows ? 0 : (size_t)rows * 4 * top_words(teacher);
-      if (lds < (size_t)rows * a.lds_bytes) lds = (size_t)rows * a.lds_bytes;
+    if (top) {                                                 // what reads the teacher and what keeps the entries, one after the other
+      a.words = per_row > 0 ? cdiv(cdiv(per_row, threads), 32) : 1;
+      a.lds_bytes = top_bytes(a.top, a.words, threads);
+      if (!a.top_rows && a.lds_bytes < 4 * top_words(teacher)) a.lds_bytes = 4 * top_words(teacher);
+      lds = (size_t)rows * a.lds_bytes;
     }
     if (lds > 65536 &&
         hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
@@ -874,26 +1018,30 @@ gx_status run_rows(const gx_logits_cfg& c, RowArgs a, bool again, hipStream_t s,
     }
     hipLaunchKernelGGL(kernel, dim3(cdiv(a.rows, rows)), dim3(threads < 256 ? 256 : threads), lds, s, a, more);
   };
-  auto with = [&](auto threads, auto ch, auto stream) {
+  // which of them a shape has instances of: entries, a row that is read again
+  auto with = [&](auto threads, auto ch, auto stream, auto has_top, auto has_again) {
     constexpr int TH = decltype(threads)::value, CH = decltype(ch)::value;
     constexpr bool ST = decltype(stream)::value;
-    auto run = [&](auto of_bf16, auto of_f32, auto more) { bf ? go(of_bf16, TH, TH * CH, more) : go(of_f32, TH, TH * CH, more); };
-    if (top) run(loss_row_kernel<bf16, TH, CH, ST, true, false>, loss_row_kernel<float, TH, CH, ST, true, false>, teacher);
-    else if (again) run(loss_row_kernel<bf16, TH, CH, ST, false, true>, loss_row_kernel<float, TH, CH, ST, false, true>, None());
-    else run(loss_row_kernel<bf16, TH, CH, ST, false, false>, loss_row_kernel<float, TH, CH, ST, false, false>, None());
+    auto run = [&](auto of_bf16, auto of_f32, auto more) { bf ? go(of_bf16, TH, more) : go(of_f32, TH, more); };
+    if constexpr (decltype(has_top)::value) {
+      if (top) return run(loss_row_kernel<bf16, TH, CH, ST, true, false>, loss_row_kernel<float, TH, CH, ST, true, false>, teacher);
+    }
+    if constexpr (decltype(has_again)::value) {
+      if (again) return run(loss_row_kernel<bf16, TH, CH, ST, false, true>, loss_row_kernel<float, TH, CH, ST, false, true>, None());
+    }
+    run(loss_row_kernel<bf16, TH, CH, ST, false, false>, loss_row_kernel<float, TH, CH, ST, false, false>, None());
   };
-  const Flag<false> held;
-  const Flag<true> twice;
-  if (per_row <= 256) with(Int<64>(), Int<4>(), held);
-  else if (per_row <= 512) with(Int<64>(), Int<8>(), held);
-  else if (per_row <= 1024) with(Int<256>(), Int<4>(), held);
-  else if (per_row <= 2048) with(Int<256>(), Int<8>(), held);
-  else if (per_row <= 4096 && a.rows >= 1024) with(Int<256>(), Int<16>(), held);
-  else if (per_row <= 4096) with(Int<512>(), Int<8>(), held);
-  else if (per_row <= 8192) with(Int<512>(), Int<16>(), held);
-  else if (per_row <= 16384 && a.kind != SCORE) with(Int<1024>(), Int<16>(), held);
-  else if (per_row <= 16384) with(Int<1024>(), Int<4>(), twice);
-  else with(Int<512>(), Int<8>(), twice);
+  const Flag<false> no;
+  const Flag<true> yes;
+  if (per_row <= 256) with(Int<64>(), Int<4>(), no, yes, yes);
+  else if (per_row <= 512) with(Int<64>(), Int<8>(), no, yes, yes);
+  else if (per_row <= 1024) with(Int<256>(), Int<4>(), no, yes, yes);
+  else if (per_row <= 2048) with(Int<256>(), Int<8>(), no, yes, yes);
+  else if (per_row <= 4096) with(Int<512>(), Int<8>(), no, yes, yes);
+  else if (per_row <= 8192) with(Int<512>(), Int<16>(), no, yes, yes);
+  else if (top || a.kind == SCORE) with(Int<512>(), Int<8>(), yes, yes, no);
+  else if (per_row <= 16384) with(Int<1024>(), Int<16>(), no, no, no);
+  else with(Int<1024>(), Int<4>(), yes, no, no);
   return refused ? GX_ERR_LAUNCH : launched();
 }
 
@@ -1074,7 +1222,7 @@ gx_status gx_preference_loss(const gx_logits_cfg* cfg, const gx_pairs_cfg* pairs
   a.stats = reinterpret_cast<f32x2*>(ws + l.stats);
   a.counted = reinterpret_cast<float*>(ws + l.counted);
   float* dlogp = reinterpret_cast<float*>(ws + l.dlogp);
-  if (cfg->rows > 0 && (st = run_rows(*cfg, a, dlogits != nullptr, s)) != GX_OK) return st;
+  if (cfg->rows > 0 && (st = run_rows(*cfg, a, true, s)) != GX_OK) return st;
   // few rows: the workgroups of their gradients add the pairs up themselves
   const bool few = dlogits && cfg->rows > 0 && cfg->rows <= FEW_ROWS && pairs->pairs <= FEW_PAIRS;
   const PairArgs p = pair_args(*pairs, *in, a.counted, a.logp64, loss, rewards, dlogits ? dlogp : nullptr);
@@ -1112,8 +1260,6 @@ gx_status gx_distill_loss(const gx_logits_cfg* cfg, const gx_distill_cfg* distil
   const DistillScratch l = distill_scratch(cfg->rows, distill->top);
   char* ws = static_cast<char*>(workspace);
   TopArgs t = {};
-  t.z = logits;
-  t.stride = (long)cfg->stride;
   t.rows = cfg->rows;
   t.vocab = cfg->vocab;
   t.top = distill->top;
@@ -1135,8 +1281,7 @@ gx_status gx_distill_loss(const gx_logits_cfg* cfg, const gx_distill_cfg* distil
     a.top_rows = t.out;
     const int rows = t.top <= 64 ? 4 : 1;                      // of a workgroup
     auto read = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(cdiv(t.rows, rows)), dim3(256), rows * 4 * (size_t)top_words(t), s, t); };
-    if (rows == 4) cfg->dtype == GX_BF16 ? read(top_kernel<bf16, 64>) : read(top_kernel<float, 64>);
-    else cfg->dtype == GX_BF16 ? read(top_kernel<bf16, 256>) : read(top_kernel<float, 256>);
+    rows == 4 ? read(top_kernel<64>) : read(top_kernel<256>);
     if ((st = launched()) != GX_OK) return st;
   }
   return run_rows(*cfg, a, false, s, t);
