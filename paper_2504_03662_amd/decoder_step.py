@@ -3,9 +3,12 @@ block -> normed and rotated queries and keys -> cross attention -> the embedding
 
 The task is to copy a ragged source that stands there in full, so the decoder can only know the next token by looking at the right
 position of the source.  Every operator is the library's (`DeviceEmbedding`, `DeviceLayer`, `DeviceHeadNorm`,
-`DeviceCrossAttention`, `adamw_step`); the projections and the loss are a few lines of torch.
+`DeviceCrossAttention`, `adamw_step`); the projections and the loss are a few lines of torch.  The losses of `loss_ops` take that
+loss's place with --learn: `tokens` from the start, the others for a second half of the steps, after a first half of `train_step`s.
+`distill` trains another decoder from the first one's top logits, `policy` rewards drawn tokens that are the source's, `prefer`
+prefers the source to the same with a few wrong tokens.
 
-    python -m paper_2504_03662_amd.decoder_step [--steps 200]
+    python -m paper_2504_03662_amd.decoder_step [--steps 200] [--learn tokens|distill|policy|prefer]
 """
 from __future__ import annotations
 
@@ -15,6 +18,7 @@ import torch
 
 from . import binding as gx, inputs as I
 from .decoder_ops import DeviceCrossAttention, DeviceEmbedding, DeviceHeadNorm
+from .loss_ops import DeviceDistillation, DevicePolicyLoss, DevicePreferenceLoss, DeviceTokenLoss
 from .runtime import DeviceLayer
 
 START = 1                                           # first decoder token; 0 pads
@@ -59,6 +63,11 @@ class CopyingDecoder:
         angle = torch.arange(length).double()[:, None] * THETA ** (-torch.arange(self.head_dim // 2).double() * 2 / self.head_dim)
         self.cos, self.sin = angle.cos().float().to(device), angle.sin().float().to(device)
         self.t = 0
+        logits = dict(dtype="f32", device=device)
+        self.token_loss = DeviceTokenLoss(vocab, ignore_id=0, **logits)
+        self.policy_loss = DevicePolicyLoss(vocab, kl=0.05, ignore_id=0, **logits)
+        self.preference_loss = DevicePreferenceLoss(vocab, ignore_id=0, **logits)
+        self.distillation = DeviceDistillation(vocab, **logits)
 
     def batch_of(self, seed):
         """(source ids, source lengths, decoder inputs): sources of different lengths, the rest of a row is padding"""
@@ -102,7 +111,12 @@ class CopyingDecoder:
         dlogits = logp.exp()
         dlogits.scatter_add_(1, target[:, None], torch.full_like(dlogits[:, :1], -1.0))
         dlogits *= (counts / counts.sum())[:, None]
+        self._update(source, src, lens, inp, f, dlogits, lr)
+        return loss
 
+    def _update(self, source, src, lens, inp, f, dlogits, lr):
+        """From the gradient of the logits to the weights"""
+        states, k, kn, v = source
         w, flat = self.weights, (lambda x: x.reshape(x.shape[0] * x.shape[1], -1))
         table = w["table"].value.float()
         w["table"].grad.copy_(dlogits.t() @ f["y"].float())
@@ -126,7 +140,78 @@ class CopyingDecoder:
         self.t += 1
         for x in w.values():
             x.step(self.t, lr, torch.cuda.current_stream().cuda_stream)
-        return loss
+
+    def learn(self, objective, src, lens, inp, lr=2e-3):
+        """A step with an objective: logits [batch, length, vocab] -> (losses, their sum's gradient by the logits) -> the losses' sum"""
+        source = self.read_source(src)
+        f = self.forward(inp, source, lens)
+        losses, dlogits = objective(f["logits"].view(*inp.shape, -1))
+        self._update(source, src, lens, inp, f, dlogits.view(-1, self.vocab), lr)
+        return losses.sum()
+
+    def take_weights(self, other):
+        for n, w in self.weights.items():
+            w.master.copy_(other.weights[n].master)
+            w.value.copy_(other.weights[n].value)
+
+    def logits(self, src, lens, inp):
+        return self.forward(inp, self.read_source(src), lens, want_lse=False)["logits"].view(*inp.shape, -1)
+
+    # Objectives.  Gradients are written over the logits.
+    def _mean(self, ids):
+        counts = (ids != 0).float()
+        return counts / counts.sum()
+
+    def tokens(self, src):
+        """Cross entropy"""
+        return lambda z: self.token_loss.forward_backward(z, src, self._mean(src), out=z)
+
+    def distill(self, src, teacher_logits, top=8):
+        """What another decoder has told of itself: its top logits, and their distance from its log sum"""
+        best, ids = teacher_logits.topk(top, dim=2)
+        _, lse = self.token_loss.logp(teacher_logits, src)
+        return lambda z: self.distillation.forward_backward(z, ids, best, lse, self._mean(src), out=z)
+
+    def policy(self, src, drawn, old_logp, ref_logp):
+        """Tokens that an older policy has drawn, and its log probabilities: those that are the source's are to come more often"""
+        right = (drawn == src).float()
+        advantages = right - (right * self._mean(src)).sum()
+
+        def objective(z):
+            losses, _, dlogits = self.policy_loss.forward_backward(z, drawn, old_logp, advantages, ref_logp, self._mean(src), out=z)
+            return losses, dlogits
+        return objective
+
+    def prefer(self, ids, ref_logp):
+        """Samples 2 i and 2 i + 1 are chosen and rejected answers to one source"""
+        starts = torch.arange(self.batch + 1, dtype=torch.int32, device=self.device) * self.length
+        each = torch.full((self.batch // 2,), 2.0 / self.batch, device=self.device)
+
+        def objective(z):
+            losses, _, dlogits = self.preference_loss.forward_backward(z, ids, starts, ref_logp, None, each, out=z)
+            return losses, dlogits
+        return objective
+
+    def drawn_from(self, src, lens, inp, seed):
+        """A token of every position, drawn after the source's tokens before it -> (tokens, their log probabilities)"""
+        z = self.logits(src, lens, inp)
+        gen = torch.Generator().manual_seed(seed)
+        p = torch.softmax(z, dim=2).cpu().view(-1, self.vocab)
+        drawn = torch.multinomial(p, 1, generator=gen).view(src.shape).to(self.device)
+        drawn = torch.where(src == 0, 0, drawn)
+        return drawn, self.token_loss.logp(z, drawn)[0]
+
+    def pairs_of(self, seed):
+        """(sources, lengths, decoder inputs, answers): every source twice, answered by itself and by a copy with wrong tokens"""
+        src, lens, _ = self.batch_of(seed)
+        src, lens = src[:self.batch // 2].repeat_interleave(2, dim=0), lens[:self.batch // 2].repeat_interleave(2)
+        gen = torch.Generator().manual_seed(seed + 1)
+        wrong = torch.rand(src.shape, generator=gen) < 0.2
+        wrong[0::2] = False
+        other = torch.randint(2, self.vocab, src.shape, generator=gen)
+        ids = torch.where(wrong.to(self.device) & (src != 0), other.to(self.device), src)
+        inp = torch.cat([torch.full_like(ids[:, :1], START), ids[:, :-1]], dim=1)
+        return src, lens, inp, ids
 
     def decode(self, src, lens):
         """Greedy: the source's keys and values stay as they are, and each step's queries are one token of every sample"""
@@ -154,13 +239,39 @@ def copied(src, lens, out):
     return float(((src == out) & counts).sum() / counts.sum())
 
 
+def taught(model, first, how, seed, lr):
+    """A step of an objective of `loss_ops` on a batch; `first` is the teacher, or what the decoder is held near"""
+    if how == "prefer":
+        src, lens, inp, ids = model.pairs_of(seed)
+        objective = model.prefer(ids, first.token_loss.logp(first.logits(src, lens, inp), ids)[0])
+        return model.learn(objective, src, lens, inp, lr)
+    data = src, _, _ = model.batch_of(seed)
+    if how == "tokens":
+        objective = model.tokens(src)
+    elif how == "distill":
+        objective = model.distill(src, first.logits(*data))
+    else:
+        drawn, old_logp = model.drawn_from(*data, seed)
+        objective = model.policy(src, drawn, old_logp, first.token_loss.logp(first.logits(*data), drawn)[0])
+    return model.learn(objective, *data, lr)
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--steps", type=int, default=200)
+    ap.add_argument("--learn", choices=("tokens", "distill", "policy", "prefer"))
     a = ap.parse_args()
-    model = CopyingDecoder()
+    model = first = CopyingDecoder()
+    half = 0 if a.learn == "tokens" else a.steps // 2
     for i in range(a.steps):
-        loss = model.train_step(*model.batch_of(i))
+        if a.learn and i == half > 0:
+            model = CopyingDecoder(seed=1)
+            if a.learn != "distill":
+                model.take_weights(first)
+        if a.learn and i >= half:
+            loss = taught(model, first, a.learn, i, 2e-4 if a.learn in ("policy", "prefer") else 2e-3)
+        else:
+            loss = model.train_step(*model.batch_of(i))
         if i % 20 == 0 or i == a.steps - 1:
             print(f"step {i:4d}  loss {float(loss):.4f}", flush=True)
     src, lens, _ = model.batch_of(10 ** 6)
