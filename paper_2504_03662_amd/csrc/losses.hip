@@ -571,32 +571,21 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
     const float ref = reference(top_here);
     if (STREAM && m != top_here) s *= exp_exact(m - ref, a);
     m = top_here;
-    // A divergence is a small difference of log sums, and a reward the sum of many.  For them (`exact`) what roundings leave is added up
-    // too: of the exponents (a row of bf16 has few differences d, whose errors do not average out; of d = -inf it is no number, and
-    // made one) and of the sum, which starts from 1, so that no term is larger.  4 us of 270 for 8192 rows of 32768.
-    auto add = [&](auto exact) {
-      constexpr bool EXACT = decltype(exact)::value;
-      float sum = EXACT ? 1.f : 0.f, left = 0.f, lost = 0.f;
+    // A chunk's exponentials are added up as a tree and the chunks in fp64: a divergence is a small difference of log sums, and a
+    // reward the sum of many
 #pragma unroll
-      for (int j = 0; j < CH; j++) {
-        if (!there(base, j)) break;
+    for (int j = 0; j < CH; j++) {
+      if (!there(base, j)) break;
+      float x[N];
 #pragma unroll
-        for (int e = 0; e < N; e++) {
-          const float d = to_f32(v[j][e]) - ref;
-          if (EXACT) {
-            const float t = d * a.c_hi, x = __builtin_amdgcn_exp2f(t), more = sum + x;
-            left = fmaf(x, __builtin_amdgcn_fmed3f(fmaf(d, a.c_lo, fmaf(d, a.c_hi, -t)), -1.f, 1.f), left);
-            lost += (sum - more) + x;
-            sum = more;
-          } else {
-            sum += exp_scaled(d, a.c_hi, a.c_lo);
-          }
-        }
+      for (int e = 0; e < N; e++) x[e] = exp_scaled(to_f32(v[j][e]) - ref, a.c_hi, a.c_lo);
+#pragma unroll
+      for (int n = N / 2; n > 0; n >>= 1) {
+#pragma unroll
+        for (int e = 0; e < n; e++) x[e] += x[e + n];
       }
-      s += EXACT ? (double)(sum - 1.f) + (double)lost + (double)left * 0.69314718055994530942 : (double)sum;
-    };
-    if (TOP || ((AGAIN || STREAM) && a.logp64)) add(Flag<true>());
-    else add(Flag<false>());
+      s += (double)x[0];
+    }
     if (!STREAM) break;
     base += THREADS * CH;
     if (base >= k.body + k.lead) break;
