@@ -171,7 +171,11 @@ GX_DEVINL double exp_exact(float d, const RowArgs& a) {
   double p = 1.0 / 40320.0;
   const double coef[8] = {1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
 #pragma unroll
-  for (int i = 0; i < 8; i++) p = fma(p, r, coef[i]);
+  for (int i = 0; i < 8; i++) {
+    double c = coef[i];
+    asm("" : "+s"(c));                                         // in scalar registers: in vector registers they cost a row's kernel a wavefront
+    p = fma(p, r, c);
+  }
   return d == d ? ldexp(p, (int)n) : (double)d;
 }
 GX_DEVINL double rescaled(Sums x, float m, const RowArgs& a) { return x.s == 0.0 ? 0.0 : x.s * exp_exact(x.m - m, a); }
@@ -387,7 +391,7 @@ __host__ __device__ inline int top_bytes(int top, int words, int threads) {
 // A row to a workgroup of THREADS, or with 64 one to each of a workgroup's four wavefronts.  A thread has CH chunks in flight; with
 // STREAM as many of those steps as the row needs, and reads them again for the gradient, without it one.
 template <typename T, int THREADS, int CH, bool STREAM, bool TOP, bool AGAIN>
-__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_kernel(RowArgs a, std::conditional_t<TOP, TopArgs, None> teacher) {
+__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, TOP && CH <= 8 ? 6 : 4) loss_row_kernel(RowArgs a, std::conditional_t<TOP, TopArgs, None> teacher) {
   constexpr int N = Lanes<T>::N, WAVES = THREADS / 64, ROWS = THREADS < 256 ? 256 / THREADS : 1;
   typedef typename Lanes<T>::type Raw;
   extern __shared__ __attribute__((aligned(16))) char group_lds[];
@@ -479,7 +483,9 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
   Raw* const staged = reinterpret_cast<Raw*>(columns + a.top + 1);            // the last slot is for chunks without a column
   float* const end_value = reinterpret_cast<float*>(staged + a.top + 1);
   unsigned* const marks = reinterpret_cast<unsigned*>(end_value + 16);
-  unsigned* const end_marks = marks + a.words * THREADS;
+  static_assert(CH <= 32);
+  const int words = STREAM ? a.words : 1;
+  unsigned* const end_marks = marks + words * THREADS;
   int* const slots = reinterpret_cast<int*>(end_marks + 2), *const slots_taken = slots - 1;
   // an entry's place: an end, or an element of a slot
   auto is_end = [&](int col) { return (unsigned)(col - k.head) >= (unsigned)(k.body * N); };
@@ -487,8 +493,10 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
   auto element = [&](int col) {
     const int c = (col - k.head) / N + k.lead, owner = c % THREADS, n = c / THREADS;
     int slot = slots[owner];
-    for (int i = 0; i < n >> 5; i++) slot += __popc(marks[i * THREADS + owner]);
-    slot += __popc(marks[(n >> 5) * THREADS + owner] & ((1u << (n & 31)) - 1));
+    const int word = STREAM ? n >> 5 : 0;                      // a row in registers has one step of CH chunks, of 32 at most
+#pragma unroll 1
+    for (int i = 0; i < word; i++) slot += __popc(marks[i * THREADS + owner]);
+    slot += __popc(marks[word * THREADS + owner] & ((1u << (n & 31)) - 1));
     return slot * N + (col - k.head) % N;
   };
   auto each_entry = [&](auto f) {
@@ -499,7 +507,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
     if (a.top > THREADS && tid < a.top) col = entries[tid].col;
   };
   if (TOP) {
-    for (int i = tid; i < a.words * THREADS + 2; i += THREADS) marks[i] = 0;
+    for (int i = tid; i < words * THREADS + 2; i += THREADS) marks[i] = 0;
     if (tid == 0) columns[a.top] = u32x4{0, 0, 0, 0};
     all_here();
     each_entry([&](int, int at) {
@@ -512,7 +520,8 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
     });
     all_here();
     int mine = 0;
-    for (int i = 0; i < a.words; i++) mine += __popc(marks[i * THREADS + tid]);
+#pragma unroll 1
+    for (int i = 0; i < words; i++) mine += __popc(marks[i * THREADS + tid]);
     const int first = mine ? atomicAdd(slots_taken, mine) : 0;
     slots[tid] = first;
     for (int i = 0; i < mine; i++) columns[first + i] = u32x4{0, 0, 0, 0};
@@ -528,7 +537,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, 4) loss_row_ker
   int slot = TOP ? slots[tid] : 0;
   // f(slot) for the thread's chunk of a step where any of the wavefront's chunks is marked
   auto if_marked = [&](int base, int j, auto f) {
-    const int n = base / THREADS + j;
+    const int n = STREAM ? base / THREADS + j : j;
     const unsigned on = marks[(n >> 5) * THREADS + tid] >> (n & 31) & 1;
     if (!__any(on)) return;
     f(on ? slot : a.top);
