@@ -6,13 +6,15 @@
 // row kernel: it reads a row, keeps maximum and sum of exponentials of what a thread has met, joins them over the workgroup, forms
 // the loss and c from them, and writes the gradient.  It is bound by memory: 8 bytes an element (fp32) or 4 (bf16) against
 // about 20 instructions.
-// Sums over a thread's elements are fp32; from there on (sums over threads, log sums, losses) they are fp64, which is free: losses
-// are small differences of log sums, and a sequence's reward adds up over thousands of tokens.
+// The exponentials of a chunk are added up in fp32 as a tree, and from there on (sums over chunks and threads, log sums, losses) all is
+// fp64, which costs nothing that could be measured: losses are small differences of log sums, and a sequence's reward adds up
+// over thousands of tokens.  A log sum of 32768 logits (bf16) is off by 2e-8, and by 1e-9 at the mean.
 //
-// Measured, us (and TB/s of logits read and gradients written; a large copy moves 5.7): cross entropy with gradient, bf16, 8192 x 32768 196
-// (5.5), 8192 x 50001 280 (5.9), 2048 x 131072 210 (5.1), fp32 4096 x 32003 180 (5.8); 64 entries of a teacher, 8192 x 32768 213;
-// preference loss, which reads twice, 8192 x 32768 265.  Small rows are bound by the instructions that every row costs (16384 x 1000 18, 3.6),
-// few rows by latency (64 x 32000 8.7).
+// Measured, us (and TB/s of logits read and gradients written; a large copy moves 5.7): cross entropy with gradient, bf16, 8192 x 32768 198
+// (5.4), 8192 x 50001 282 (5.8), 2048 x 131072 208 (5.2), fp32 4096 x 32003 180 (5.8); 64 entries of a teacher, 8192 x 32768 215
+// (5.0), 2048 x 131072 253 (4.2); preference loss, which reads twice, 8192 x 32768 270 (6.0, the second time in part from
+// caches).  Small rows are bound by the instructions that every row costs (16384 x 1000 18, 3.6; 64 entries 47), few rows by latency
+// (64 x 32000 8.7).
 #include "../../include/gx.h"
 #include "gx_kernels.h"
 #include <type_traits>
@@ -24,11 +26,11 @@ using namespace gx;
 // Limits of the interface.  Rows times 1024 threads, and workgroups of 256 threads, are launches of less than 2^32 threads
 constexpr int MAX_ROWS = 1 << 21, MAX_VOCAB = 1 << 19, MAX_TOP = 1024, MAX_PAIRS = 1 << 20;
 constexpr long MAX_GRID = (1 << 24) - 1;
-// So few rows read their teachers in the launch that does the rest; for more there is a launch before, which is quicker at it (64 rows
-// of 32000, 16 entries, 11.8 us in one launch, 15 in two; 256 rows 13.1 and 17)
+// So few rows read their teachers in the launch that does the rest; for more there is a launch before, which is quicker at it (16
+// entries of 32000 columns, 256 rows 15.4 us in one launch; 257 rows, two launches, 18.7)
 constexpr int READ_HERE = 256;
-// So few rows and pairs that a launch of its own for the pairs takes longer than adding them up for every row (131 rows of 1001 15.3 us,
-// 19 with the launch; 1001 rows of 5003 20.2 and 22.9)
+// So few rows and pairs that a launch of its own for the pairs takes longer than adding them up for every row (131 rows of 1001 15.4 us,
+// 19 with the launch; 1001 rows of 5003 16.0, and 1025, with the launch, 18.9)
 constexpr int FEW_ROWS = 1024, FEW_PAIRS = 256;
 constexpr float NO_LOGIT = -INFINITY, MIN_SCALE = 1.f / (1 << 20);
 
@@ -389,7 +391,8 @@ __host__ __device__ inline int top_bytes(int top, int words, int threads) {
 }
 
 // A row to a workgroup of THREADS, or with 64 one to each of a workgroup's four wavefronts.  A thread has CH chunks in flight; with
-// STREAM as many of those steps as the row needs, and reads them again for the gradient, without it one.
+// STREAM as many of those steps as the row needs, and reads them again for the gradient, without it one.  Entries have barriers to wait at,
+// so a compute unit is to have three workgroups of 512 (8192 x 32768, 64 entries, 220 us; with two, 248).
 template <typename T, int THREADS, int CH, bool STREAM, bool TOP, bool AGAIN>
 __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, TOP && CH <= 8 ? 6 : 4) loss_row_kernel(RowArgs a, std::conditional_t<TOP, TopArgs, None> teacher) {
   constexpr int N = Lanes<T>::N, WAVES = THREADS / 64, ROWS = THREADS < 256 ? 256 / THREADS : 1;
@@ -477,7 +480,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, TOP && CH <= 8 
   // TOP: chunks with an entry's column are marked, bit by bit for the thread that has them, and have a slot in LDS: the bits of those
   // columns, and a chunk in which their logits go to the entries' threads and their gradients come back, so that they are stored
   // with the rest of their chunks.  (One by one they are a sector of memory each, read and written: 16 / 64 / 256 of 32768 columns,
-  // 8192 rows, 214 / 223 / 334 us, so 210 / 213 / 237.)  Which slot is whose depends on the order in which threads ask, and nothing
+  // 8192 rows, 214 / 223 / 334 us, so 210 / 215 / 239.)  Which slot is whose depends on the order in which threads ask, and nothing
   // else does.  All of it but the logits is there before the row is.
   u32x4* const columns = reinterpret_cast<u32x4*>(lds);
   Raw* const staged = reinterpret_cast<Raw*>(columns + a.top + 1);            // the last slot is for chunks without a column
@@ -781,9 +784,11 @@ struct Pair {
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       double s = 0.0;
-      for (int t = at[h] + tid; t < at[h + 1]; t += 256) {
+#pragma unroll 4
+      for (int t = at[h] + tid; t < at[h + 1]; t += 256) {     // (loads that wait for nothing)
+        const double logp = (double)static_cast<const L*>(a.logp)[t], ref = a.ref ? (double)a.ref[t] : 0.0;
         const float w = a.weights ? a.weights[t] : 1.f;
-        if (w != 0.f) s += (double)w * ((double)static_cast<const L*>(a.logp)[t] - (a.ref ? (double)a.ref[t] : 0.0));
+        s += w != 0.f ? (double)w * (logp - ref) : 0.0;
       }
       s = wave_sum_f64(s);
       if ((tid & 63) == 0) part[h][tid >> 6] = s;
@@ -831,7 +836,7 @@ __global__ void __launch_bounds__(256) pairs_kernel(PairArgs a) {
 }
 
 // dz = g scale (1_y - p) where p = f exp(c (u z - m)): m = lse of the whole vocabulary (u = scale, c = 1, f = 1), or what the row
-// kernel has left (u = 1, c = scale, m the maximum, f = 1 / sum).  A workgroup takes 256 * CH chunks of a row.
+// kernel has left (u = 1, c = scale, m the maximum, f = 1 / sum).  A workgroup of 256 takes THREADS * CH chunks of each of 256 / THREADS rows.
 // PAIRS: g comes from the row's pair, which each of its rows' workgroups adds up, and one more to a pair for the losses
 struct GradArgs {
   const void* z;
@@ -843,12 +848,16 @@ struct GradArgs {
   const float *lse, *dlogp;
   const f32x2* stats;
 };
-template <typename T, int CH, bool PAIRS>
+template <typename T, int THREADS, int CH, bool PAIRS>
 __global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a, std::conditional_t<PAIRS, PairArgs, None> pairs) {
   constexpr int N = Lanes<T>::N;
   typedef typename Lanes<T>::type Raw;
   // from the last row on: of logits that have just been read whole, the last ones may still be near
-  const int tid = threadIdx.x, block = a.rows * a.parts - 1 - (int)blockIdx.x, row = block < 0 ? 0 : block / a.parts, part = block - row * a.parts;
+  static_assert(THREADS == 256 || (THREADS == 64 && !PAIRS));
+  const int tid = THREADS == 256 ? threadIdx.x : threadIdx.x & 63;
+  const int block = a.rows * a.parts - 1 - (THREADS == 256 ? (int)blockIdx.x : (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  if (!PAIRS && block < 0) return;
+  const int row = block < 0 ? 0 : block / a.parts, part = block - row * a.parts;
   float dlogp = 0.f;
   if constexpr (PAIRS) {
     __shared__ double sums[2][4];
@@ -875,7 +884,7 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a, std::conditi
   const T* zr = static_cast<const T*>(a.z) + (size_t)row * a.stride;
   T* dr = static_cast<T*>(a.dz) + (size_t)row * a.grad_stride;
   const Cut<T> k(zr, a.vocab);
-  const int y = a.ids.column(row, a.vocab), first = part * 256 * CH + tid - k.lead;
+  const int y = a.ids.column(row, a.vocab), first = part * THREADS * CH + tid - k.lead;
   float g = dlogp * a.scale;
   const bool aligned = ((reinterpret_cast<uintptr_t>(dr) ^ reinterpret_cast<uintptr_t>(zr)) & 15) == 0;
   const bool counts = y != IGNORED && g != 0.f;
@@ -887,7 +896,7 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a, std::conditi
   if (counts) {
 #pragma unroll
     for (int j = 0; j < CH; j++) {
-      const int c = first + j * 256;
+      const int c = first + j * THREADS;
       if (k.has(c)) {
         const Raw* p = reinterpret_cast<const Raw*>(zr + k.head) + c;
         v[j] = __builtin_nontemporal_load(p);
@@ -896,7 +905,7 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a, std::conditi
   }
 #pragma unroll
   for (int j = 0; j < CH; j++) {
-    const int c = first + j * 256;
+    const int c = first + j * THREADS;
     if (!k.has(c)) continue;
     float x[N];
 #pragma unroll
@@ -993,7 +1002,7 @@ RowArgs row_args(const gx_logits_cfg& c, Kind kind, const void* logits, void* dl
 // 32768, 512 threads with 8 196, 256 with 16 202, read twice 212; of 50001, 512 with 16 279, read twice 319; 2048 rows of
 // 131072, 1024 threads with 16 210, read twice 231.
 // Only the last shape has a compute unit for one row alone.  With a teacher's entries, whose barriers nothing hides there, and for
-// log probabilities, which are not written, reading twice is better: 2048 x 131072, 64 entries, 247 and 274 us; log probabilities 96
+// log probabilities, which are not written, reading twice is better: 2048 x 131072, 64 entries, 253 and 274 us; log probabilities 96
 // and 118.  (The rule does not ask whether a gradient is wanted: a loss has the same bits with and without.)
 gx_status run_rows(const gx_logits_cfg& c, RowArgs a, bool again, hipStream_t s, const TopArgs& teacher = TopArgs{}) {
   if (!device_is_gfx950()) return GX_ERR_ARCH;
@@ -1052,12 +1061,16 @@ gx_status run_grad(const gx_logits_cfg& c, GradArgs a, const PairArgs* pairs, hi
   a.vocab = c.vocab;
   a.scale = c.scale;
   const int chunks = chunks_of(c, a.z, c.stride);
+  // short rows go one to a wavefront (the gradient of log probabilities, bf16: 16384 x 300 9.3 us, 19.3 with a workgroup each; x 1000 15.5
+  // and 20.1)
+  const bool wave = !pairs && chunks <= 64 * CH;
   a.parts = chunks > 0 ? cdiv(chunks, 256 * CH) : 1;
   if ((long)c.rows * a.parts > MAX_GRID) return GX_ERR_SHAPE;
-  const dim3 grid((unsigned)(c.rows * a.parts + (pairs ? pairs->pairs : 0)));
+  const dim3 grid((unsigned)(wave ? cdiv(c.rows, 4) : c.rows * a.parts + (pairs ? pairs->pairs : 0)));
   auto go = [&](auto kernel, auto more) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, more); };
-  if (pairs) bf ? go(loss_grad_kernel<bf16, CH, true>, *pairs) : go(loss_grad_kernel<float, CH, true>, *pairs);
-  else bf ? go(loss_grad_kernel<bf16, CH, false>, None()) : go(loss_grad_kernel<float, CH, false>, None());
+  if (pairs) bf ? go(loss_grad_kernel<bf16, 256, CH, true>, *pairs) : go(loss_grad_kernel<float, 256, CH, true>, *pairs);
+  else if (wave) bf ? go(loss_grad_kernel<bf16, 64, CH, false>, None()) : go(loss_grad_kernel<float, 64, CH, false>, None());
+  else bf ? go(loss_grad_kernel<bf16, 256, CH, false>, None()) : go(loss_grad_kernel<float, 256, CH, false>, None());
   return launched();
 }
 
