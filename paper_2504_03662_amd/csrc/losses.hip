@@ -17,6 +17,7 @@
 // (64 x 32000 8.7).
 #include "../../include/gx.h"
 #include "gx_kernels.h"
+#include <algorithm>
 #include <type_traits>
 
 namespace {
@@ -1052,20 +1053,23 @@ gx_status run_rows(const gx_logits_cfg& c, RowArgs a, bool again, hipStream_t s,
   return refused ? GX_ERR_LAUNCH : launched();
 }
 
+// Pieces of 256 * GRAD_CH chunks that the gradient's workgroups cut a row into
+constexpr int GRAD_CH = 4;
+int grad_parts(const gx_logits_cfg& c, const void* z) { return std::max(1, cdiv(chunks_of(c, z, c.stride), 256 * GRAD_CH)); }
+bool too_many_parts(const gx_logits_cfg& c, const void* z) { return (long)c.rows * grad_parts(c, z) > MAX_GRID; }
+
 gx_status run_grad(const gx_logits_cfg& c, GradArgs a, const PairArgs* pairs, hipStream_t s) {
-  constexpr int CH = 4;
+  constexpr int CH = GRAD_CH;
   const bool bf = c.dtype == GX_BF16;
   a.stride = (long)c.stride;
   a.grad_stride = (long)c.grad_stride;
   a.rows = c.rows;
   a.vocab = c.vocab;
   a.scale = c.scale;
-  const int chunks = chunks_of(c, a.z, c.stride);
   // short rows go one to a wavefront (the gradient of log probabilities, bf16: 16384 x 300 9.3 us, 19.3 with a workgroup each; x 1000 15.5
   // and 20.1)
-  const bool wave = !pairs && chunks <= 64 * CH;
-  a.parts = chunks > 0 ? cdiv(chunks, 256 * CH) : 1;
-  if ((long)c.rows * a.parts > MAX_GRID) return GX_ERR_SHAPE;
+  const bool wave = !pairs && chunks_of(c, a.z, c.stride) <= 64 * CH;
+  a.parts = grad_parts(c, a.z);
   const dim3 grid((unsigned)(wave ? cdiv(c.rows, 4) : c.rows * a.parts + (pairs ? pairs->pairs : 0)));
   auto go = [&](auto kernel, auto more) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, more); };
   if (pairs) bf ? go(loss_grad_kernel<bf16, 256, CH, true>, *pairs) : go(loss_grad_kernel<float, 256, CH, true>, *pairs);
@@ -1139,6 +1143,7 @@ gx_status gx_logp_bwd(const gx_logits_cfg* cfg, const void* logits, const void* 
   if (logits_misaligned(*cfg, logits) || logits_misaligned(*cfg, dlogits) || misaligned(ids, cfg->id_bytes) || misaligned(lse, 4) ||
       misaligned(dlogp, 4))
     return GX_ERR_ALIGN;
+  if (too_many_parts(*cfg, logits)) return GX_ERR_SHAPE;
   if (!device_is_gfx950()) return GX_ERR_ARCH;
   GradArgs a = {};
   a.z = logits;
@@ -1223,6 +1228,7 @@ gx_status gx_preference_loss(const gx_logits_cfg* cfg, const gx_pairs_cfg* pairs
       misaligned(workspace, 16))
     return GX_ERR_ALIGN;
   if (pairs->pairs == 0 && (!dlogits || cfg->rows == 0)) return GX_OK;
+  if (dlogits && too_many_parts(*cfg, logits)) return GX_ERR_SHAPE;
   if (!device_is_gfx950()) return GX_ERR_ARCH;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const PreferenceScratch l = preference_scratch(cfg->rows);

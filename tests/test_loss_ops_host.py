@@ -221,3 +221,11 @@ def test_work_goes_to_the_operators_gpu_or_nowhere(make, monkeypatch):
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
     with pytest.raises(ValueError, match="cuda:1"):
         make(10, device="cuda:1")._stream()
+
+
+@pytest.mark.parametrize("dtype,rows", [(gx.GX_F32, 1 << 17), (gx.GX_BF16, 1 << 18)])
+def test_too_many_pieces_are_refused_before_any_launch(dtype, rows):
+    """2^24 pieces of rows of 2^19 columns, in the two gradients that are cut into pieces"""
+    cfg = _cfg(rows=rows, vocab=1 << 19, stride=1 << 19, grad_stride=1 << 19, dtype=dtype)
+    assert gx.logp_bwd(cfg, P, P, P, P, P, check=False) == 2
+    assert gx.preference_loss(cfg, _pairs(rows=rows), gx.pairs_in(P, P, P, P), P, P, P, P, P, P, check=False) == 2
