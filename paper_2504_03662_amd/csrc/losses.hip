@@ -82,6 +82,11 @@ struct Ids {
   }
 };
 
+// A constant in scalar registers: of vector registers the series' coefficients took so many that a compute unit had a workgroup less
+GX_DEVINL double scalar(double x) {
+  asm("" : "+s"(x));
+  return x;
+}
 // Exponential and logarithm in fp64, to about 2^-50: a power of two, and a series in what is left of it (of exp up to the 12th power for
 // |r| <= log(2) / 2, of log m = 2 atanh((m - 1) / (m + 1)) up to the 19th for m between sqrt(1/2) and sqrt(2)).  Every
 // wavefront of a row computes a few of them: a quarter of the instructions of a library's.
@@ -91,7 +96,7 @@ GX_DEVINL double exp_f64(double x) {
   const double coef[12] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0,
                            1.0 / 6.0, 0.5, 1.0, 1.0};
 #pragma unroll
-  for (int i = 0; i < 12; i++) p = fma(p, r, coef[i]);
+  for (int i = 0; i < 12; i++) p = fma(p, r, scalar(coef[i]));
   return x == x ? ldexp(p, (int)n) : x;
 }
 GX_DEVINL double log_f64(double x) {                           // of 0, of positive normal numbers or of NaN
@@ -104,7 +109,7 @@ GX_DEVINL double log_f64(double x) {                           // of 0, of posit
   const double t = (m - 1.0) / (m + 1.0), t2 = t * t;
   double p = 2.0 / 19.0;
 #pragma unroll
-  for (int k = 17; k > 0; k -= 2) p = fma(p, t2, 2.0 / k);
+  for (int k = 17; k > 0; k -= 2) p = fma(p, t2, scalar(2.0 / k));
   return x == 0.0 ? -(double)INFINITY : fma((double)n, 0.69314718055994530942, p * t);
 }
 
@@ -159,10 +164,36 @@ GX_DEVINL float exp_gradient(float d, float c_hi, float c_lo) {
   return sizeof(T) == 2 ? __builtin_amdgcn_exp2f(d * c_hi) : exp_scaled(d, c_hi, c_lo);
 }
 
-GX_DEVINL double wave_sum_f64(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+// What N lanes have together (up to 16: of the first N, in lane order of no account), and what all 64 have, the same in every lane.  Lanes
+// exchange in registers (neighbours, pairs, mirrored halves and rows of 16), and the four rows of 16 through scalar registers: an exchange
+// through LDS is a round trip of some 100 cycles, and a row has about 40 of them one after another.
+template <int CTRL> GX_DEVINL int crossed(int x) { return __builtin_amdgcn_update_dpp(x, x, CTRL, 0xf, 0xf, false); }
+template <int CTRL> GX_DEVINL float crossed(float x) { return __builtin_bit_cast(float, crossed<CTRL>(__builtin_bit_cast(int, x))); }
+template <int CTRL> GX_DEVINL double crossed(double x) {
+  const unsigned long u = __builtin_bit_cast(unsigned long, x);
+  const unsigned lo = crossed<CTRL>((int)u), hi = crossed<CTRL>((int)(u >> 32));
+  return __builtin_bit_cast(double, (unsigned long)hi << 32 | lo);
+}
+GX_DEVINL float of_lane(float x, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane)); }
+GX_DEVINL double of_lane(double x, int lane) {
+  const unsigned long u = __builtin_bit_cast(unsigned long, x);
+  const unsigned lo = __builtin_amdgcn_readlane((int)u, lane), hi = __builtin_amdgcn_readlane((int)(u >> 32), lane);
+  return __builtin_bit_cast(double, (unsigned long)hi << 32 | lo);
+}
+template <int N, typename V, typename F>
+GX_DEVINL V of_lanes(V v, F f) {
+  static_assert(N == 64 || N == 16 || N == 8 || N == 4);
+  v = f(v, crossed<0xB1>(v));                                  // lane ^ 1
+  v = f(v, crossed<0x4E>(v));                                  // lane ^ 2
+  if (N > 4) v = f(v, crossed<0x141>(v));                      // 7 - lane of 8
+  if (N > 8) v = f(v, crossed<0x140>(v));                      // 15 - lane of 16
+  return N < 64 ? of_lane(v, 0) : f(f(of_lane(v, 0), of_lane(v, 16)), f(of_lane(v, 32), of_lane(v, 48)));
+}
+template <int N> GX_DEVINL float max_of_lanes(float v) {
+  return of_lanes<N>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int N> GX_DEVINL double sum_of_lanes(double v) {
+  return of_lanes<N>(v, [](double a, double b) { return a + b; });
 }
 
 GX_DEVINL float reference(float m) { return m == NO_LOGIT ? 0.f : m; }
@@ -174,24 +205,14 @@ GX_DEVINL double exp_exact(float d, const RowArgs& a) {
   double p = 1.0 / 40320.0;
   const double coef[8] = {1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
 #pragma unroll
-  for (int i = 0; i < 8; i++) {
-    double c = coef[i];
-    asm("" : "+s"(c));                                         // in scalar registers: in vector registers they cost a row's kernel a wavefront
-    p = fma(p, r, c);
-  }
+  for (int i = 0; i < 8; i++) p = fma(p, r, scalar(coef[i]));
   return d == d ? ldexp(p, (int)n) : (double)d;
 }
 GX_DEVINL double rescaled(Sums x, float m, const RowArgs& a) { return x.s == 0.0 ? 0.0 : x.s * exp_exact(x.m - m, a); }
-// What N lanes have (a power of two), for all
 template <int N>
 GX_DEVINL Sums joined_lanes(Sums x, const RowArgs& a) {
-  float m = x.m;
-#pragma unroll
-  for (int o = N / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  double s = rescaled(x, m, a);
-#pragma unroll
-  for (int o = N / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  return {m, s};
+  const float m = max_of_lanes<N>(x.m);
+  return {m, sum_of_lanes<N>(rescaled(x, m, a))};
 }
 GX_DEVINL float of_first_lane(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 GX_DEVINL double of_first_lane(double x) {
@@ -316,7 +337,7 @@ GX_DEVINL TopRow read_top(const TopArgs& a, int row, int tid, double* lds, doubl
     }
   }
   again = __any(again);
-  if (!a.lse) mt = wave_max(mt);
+  if (!a.lse) mt = max_of_lanes<64>(mt);
   if (WAVES > 1) {
     if ((tid & 63) == 0) {
       part[wave][0] = (double)mt;
@@ -344,7 +365,7 @@ GX_DEVINL TopRow read_top(const TopArgs& a, int row, int tid, double* lds, doubl
   }
 #pragma unroll
   for (int n = 0; n < 2; n++) {
-    sums[n] = wave_sum_f64(sums[n]);
+    sums[n] = sum_of_lanes<64>(sums[n]);
     if (WAVES > 1 && (tid & 63) == 0) part[wave][n] = sums[n];
   }
   all_here();
@@ -580,7 +601,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, TOP && CH <= 8 
 #pragma unroll
       for (int e = 0; e < N; e++) top_here = fmaxf(top_here, to_f32(v[j][e]));
     }
-    top_here = of_first_lane(wave_max(STREAM ? fmaxf(m, top_here) : top_here));
+    top_here = max_of_lanes<64>(STREAM ? fmaxf(m, top_here) : top_here);
     const float ref = reference(top_here);
     if (STREAM && m != top_here) s *= exp_exact(m - ref, a);
     m = top_here;
@@ -605,16 +626,16 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, TOP && CH <= 8 
     load(base, only_time);
   }
   if (has_end) s += exp_exact(end - reference(m), a);
-  Sums all = {m, wave_sum_f64(s)};
-  if (TOP && a.rest) most = wave_max(most);
-  if (WAVES > 1) {
+  Sums all = {m, sum_of_lanes<64>(s)};
+  if (TOP && a.rest) most = max_of_lanes<64>(most);
+  if constexpr (WAVES > 1) {
     __shared__ float most_part[TOP ? WAVES : 1];
     if (lane == 0) {
       part[wave] = all;
       if (TOP) most_part[wave] = most;
     }
     __syncthreads();
-    if (TOP) most = wave_max(lane < WAVES ? most_part[lane] : NO_LOGIT);
+    if (TOP) most = max_of_lanes<WAVES>(lane < WAVES ? most_part[lane] : NO_LOGIT);
     all = joined_lanes<WAVES>(lane < WAVES ? part[lane] : Sums{NO_LOGIT, 0.0}, a);
   }
   all = {of_first_lane(all.m), of_first_lane(all.s)};          // (one register for all lanes)
@@ -641,8 +662,8 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, TOP && CH <= 8 
       if (q != 0.0) q_z += q * (double)z;
       if (a.rest) taken.s += exp_exact(z - from, a);
     });
-    q_z = wave_sum_f64(q_z);
-    if (a.rest) taken.s = wave_sum_f64(taken.s);
+    q_z = sum_of_lanes<64>(q_z);
+    if (a.rest) taken.s = sum_of_lanes<64>(taken.s);
     if (WAVES > 1) {
       __shared__ double entries_part[WAVES][2];
       if (lane == 0) {
@@ -791,7 +812,7 @@ struct Pair {
         const float w = a.weights ? a.weights[t] : 1.f;
         s += w != 0.f ? (double)w * (logp - ref) : 0.0;
       }
-      s = wave_sum_f64(s);
+      s = sum_of_lanes<64>(s);
       if ((tid & 63) == 0) part[h][tid >> 6] = s;
     }
     __syncthreads();
