@@ -13,8 +13,8 @@
 // Measured, us (and TB/s of logits read and gradients written; a large copy moves 5.7): cross entropy with gradient, bf16, 8192 x 32768 198
 // (5.4), 8192 x 50001 282 (5.8), 2048 x 131072 208 (5.2), fp32 4096 x 32003 180 (5.8); 64 entries of a teacher, 8192 x 32768 215
 // (5.0), 2048 x 131072 253 (4.2); preference loss, which reads twice, 8192 x 32768 270 (6.0, the second time in part from
-// caches).  Small rows are bound by the instructions that every row costs (16384 x 1000 18, 3.6; 64 entries 47), few rows by latency
-// (64 x 32000 8.7).
+// caches).  Small rows are bound by the instructions that every row costs (16384 x 1000 18, 3.6; 64 entries 42), few rows by latency
+// (64 x 32000 8.2).
 #include "../../include/gx.h"
 #include "gx_kernels.h"
 #include <algorithm>
@@ -27,9 +27,6 @@ using namespace gx;
 // Limits of the interface.  Rows times 1024 threads, and workgroups of 256 threads, are launches of less than 2^32 threads
 constexpr int MAX_ROWS = 1 << 21, MAX_VOCAB = 1 << 19, MAX_TOP = 1024, MAX_PAIRS = 1 << 20;
 constexpr long MAX_GRID = (1 << 24) - 1;
-// So few rows read their teachers in the launch that does the rest; for more there is a launch before, which is quicker at it (16
-// entries of 32000 columns, 256 rows 15.4 us in one launch; 257 rows, two launches, 18.7)
-constexpr int READ_HERE = 256;
 // So few rows and pairs that a launch of its own for the pairs takes longer than adding them up for every row (131 rows of 1001 15.4 us,
 // 19 with the launch; 1001 rows of 5003 16.0, and 1025, with the launch, 18.9)
 constexpr int FEW_ROWS = 1024, FEW_PAIRS = 256;
@@ -1079,6 +1076,15 @@ constexpr int GRAD_CH = 4;
 int grad_parts(const gx_logits_cfg& c, const void* z) { return std::max(1, cdiv(chunks_of(c, z, c.stride), 256 * GRAD_CH)); }
 bool too_many_parts(const gx_logits_cfg& c, const void* z) { return (long)c.rows * grad_parts(c, z) > MAX_GRID; }
 
+// Whether rows read their teachers in the launch that does the rest.  Many have a launch before it, which is quicker at it where workgroups
+// wait for one another.  us, one launch and two, 64 entries, bf16: rows of a wavefront (1000 columns), 1024 of them 10.5 and 13.7, 16384
+// 41.8 and 45.3 (256 entries, 65536 rows, 435 and 406); of 256 threads (8000), 2048 24.2 and 25.8, 4096 41.4 and 41.2; of 512 (32000), 512
+// 20.0 and 21.9, 1024 35.2 and 32.5.
+bool reads_here(const gx_logits_cfg& c, const void* z) {
+  const int per_row = chunks_of(c, z, c.stride);
+  return c.rows <= (per_row <= 512 ? 1 << 15 : per_row <= 2048 ? 2048 : 512);
+}
+
 gx_status run_grad(const gx_logits_cfg& c, GradArgs a, const PairArgs* pairs, hipStream_t s) {
   constexpr int CH = GRAD_CH;
   const bool bf = c.dtype == GX_BF16;
@@ -1315,7 +1321,7 @@ gx_status gx_distill_loss(const gx_logits_cfg* cfg, const gx_distill_cfg* distil
   a.top = distill->top;
   a.rest = in->top_lse != nullptr;
   a.entries = t.entries;
-  if (t.rows > READ_HERE) {
+  if (!reads_here(*cfg, logits)) {
     a.top_rows = t.out;
     const int rows = t.top <= 64 ? 4 : 1;                      // of a workgroup
     auto read = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(cdiv(t.rows, rows)), dim3(256), rows * 4 * (size_t)top_words(t), s, t); };

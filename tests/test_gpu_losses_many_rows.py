@@ -20,6 +20,30 @@ def test_distillation(top, size, kind, rest, dtype):
     few.test_distillation(top, size, kind, rest, dtype)
 
 
+@pytest.mark.parametrize("dtype,rest,top,size", [("bf16", True, 64, (515, 16400, 0, 0)), ("f32", False, 65, (513, 8300, 4, 0)),
+                                                 ("bf16", False, 256, (2049, 4800, 0, 0)), ("f32", True, 9, (2051, 2200, 0, 0)),
+                                                 ("bf16", True, 66, (32769, 70, 0, 0)), ("f32", False, 5, (32771, 19, 2, 1))], ids=str)
+def test_distillation_of_so_many_rows_that_a_launch_reads_the_teachers(dtype, rest, top, size):
+    few.test_distillation(top, size, "twice", rest, dtype)
+
+
+@pytest.mark.parametrize("name", ["distill", "rest"])
+def test_captured_with_a_launch_for_the_teachers(name):
+    rows, vocab = 600, 17000
+    call = few._calls(vocab, "bf16", rows)[name]
+    z = (2 * torch.randn(rows, vocab, device=DEV)).bfloat16()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    call(z)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        out = call(z)
+    for _ in range(3):
+        z.copy_((2 * torch.randn(rows, vocab, device=DEV)).bfloat16())
+        graph.replay()
+        torch.cuda.synchronize()
+        assert few._same(out, call(z))
+
+
 @pytest.mark.parametrize("name", few.NAMES)
 def test_captured_and_replayed(name):
     """Replays with other logits between eager calls of the same object, on the same stream"""
