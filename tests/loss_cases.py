@@ -1,7 +1,7 @@
 """Inputs and error bounds shared by the tests of the losses.
 
-Bounds, in units of half a step of fp32, u = 2^-24, from the arithmetic that the header states (fp32 over a thread's elements, fp64
-from there on):
+Bounds, in units of half a step of fp32, u = 2^-24, from fp32 sums over a thread's elements and fp64 from there on (the kernels go over to
+fp64 sooner, after 16 bytes of logits):
   a term of a sum of exponentials, or p: its argument is rounded twice (the difference, the product), |a - max| u each, the
   exponential is off by two u, and the sum adds at most vocab / 256 + 64 terms one after another.  Weighted with p the
   arguments' part is at most about the entropy, log(vocab).  So lse is off by at most `delta`, and p by (2 |a - lse| + 8) u + delta of itself.
