@@ -474,7 +474,8 @@ gx_status gx_policy_loss(const gx_logits_cfg* cfg, const gx_policy_cfg* policy, 
  *     reward[j] = beta * sum over its rows of w (logp - ref_logp),     x = reward[2 i] - reward[2 i + 1] - margin
  *     loss[i] = pair weight * (-(1 - smoothing) log sigmoid(x) - smoothing log sigmoid(-x))
  * ref_logp (NULL: zeros) fp32 [rows]; pair_weights (NULL: ones) fp32 [pairs]; rewards fp32 [2 pairs], may be NULL.  Rows that do not
- * count, with weight 0 or of no sequence have a gradient of zeros; so has a pair of weight 0, and a loss of 0.
+ * count, with weight 0 or of no sequence have a gradient of zeros; so has a pair of weight 0, and a loss of 0.  A token of probability 0
+ * makes x infinite: the loss is 0 or infinite then, and the gradient finite; in both sequences of a pair it makes them NaN.
  * gx_pairs_loss is the part after the log probabilities (which may come from shards): dlogp fp32 [rows] (NULL to skip) is the
  * gradient by logp, for gx_logp_bwd.  gx_preference_loss takes the logits; its log probabilities are fp64.
  * rows is that of the logits; at most 2^20 pairs.  Workspace: gx_preference_workspace_bytes(cfg), 0 for an invalid cfg. */

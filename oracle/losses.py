@@ -95,8 +95,9 @@ def pairs_loss(lp, starts, ref=None, weights=None, pair_weights=None, beta=0.1, 
         if pw == 0:
             continue
         x = rewards[2 * i] - rewards[2 * i + 1] - margin
-        loss[i] = pw * ((1 - smoothing) * np.logaddexp(0, -x) + smoothing * np.logaddexp(0, x))
-        slope = pw * beta * (smoothing - 1.0 / (1.0 + np.exp(x)))
+        # a part of factor 0 is none, also where x is infinite
+        loss[i] = pw * sum(f * np.logaddexp(0, y) for f, y in ((1 - smoothing, -x), (smoothing, x)) if f)
+        slope = pw * beta * (smoothing - np.exp(-np.logaddexp(0, x)))
         d[at[2 * i]:at[2 * i + 1]] = slope
         d[at[2 * i + 1]:at[2 * i + 2]] = -slope
     return loss, rewards, d * w

@@ -822,7 +822,8 @@ struct Pair {
   }
   GX_DEVINL void write(const PairArgs& a, int pair) const {
     const double low = log1p(exp_f64(-fabs(x))), sm = (double)a.smoothing;       // low: -log sigmoid(|x|)
-    const double l = (1.0 - sm) * (low + fmax(-x, 0.0)) + sm * (low + fmax(x, 0.0));
+    // x is infinite where a token of one sequence has probability 0: a part of factor 0 is none then either
+    const double l = (sm < 1.0 ? (1.0 - sm) * (low + fmax(-x, 0.0)) : 0.0) + (sm > 0.0 ? sm * (low + fmax(x, 0.0)) : 0.0);
     a.loss[pair] = weight != 0.f ? (float)((double)weight * (x == x ? l : x)) : 0.f;
     if (a.rewards) {
       a.rewards[2 * pair] = (float)reward[0];
