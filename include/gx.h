@@ -424,10 +424,11 @@ gx_status gx_cross_bwd(const gx_cross_cfg* cfg, const gx_cross_in* in, const gx_
  *   of tokens) make sums means.  A row that does not count, or has weight 0, has loss 0, logp 0 and a gradient of zeros, whatever
  *   its logits and other inputs hold: they are not read.  An id of no row of the vocabulary makes the row's results NaN.
  *   Vocabulary shards: a rank holds columns [first_id, first_id + vocab) of whole_vocab (0: vocab, the whole of it).  lse is then the
- *   shard's; a token of another shard has logp = -lse.  The whole vocabulary's are lse = log sum exp of the ranks' lse and
- *   logp = sum over the ranks of (logp + lse) - lse of the whole.  Only gx_logp_* take shards.
- * Logits of -inf are columns of probability 0.  A row of nothing else has lse = -inf and NaN for the rest, as has a row with NaN
- * or +inf.  Sums are fp32 over 16 bytes of logits, then fp64; losses are rounded once; gradients are fp32, rounded once.
+ *   shard's; a token of another shard has logp = -lse.  In a row of which the shard has nothing but -inf, lse is -inf and is not taken off:
+ *   logp is 0 for a token of another shard and -inf for one of its own.  The whole vocabulary's are lse = log sum exp of the ranks' lse and
+ *   logp = sum over the ranks of (logp + lse, or logp where lse is -inf) - lse of the whole.  Only gx_logp_* take shards.
+ * Logits of -inf are columns of probability 0.  A row of nothing else (over the whole vocabulary) has lse = -inf and NaN for the rest; a
+ * row with NaN or +inf has NaN for all.  Sums are fp32 over 16 bytes of logits, then fp64; losses are rounded once; gradients are fp32, rounded once.
  * rows 0 .. 2^21, vocab 1 .. 2^19, scale 2^-20 .. 2^20; dlogits of gx_logp_bwd and gx_preference_loss in less than 2^24 pieces of
  * 8192 (bf16) or 4096 (fp32) columns.  Pointers are aligned to their elements.  Errors: GX_ERR_NULL, GX_ERR_SHAPE, GX_ERR_DTYPE
  * (dtype, id_bytes, top_dtype), GX_ERR_ALIGN, GX_ERR_FLAGS, GX_ERR_ARCH, GX_ERR_LAUNCH. */

@@ -18,13 +18,13 @@ def _row(z, scale):
 
 
 def logp(z, ids, scale=1.0, ignore=IGNORE, first=0):
-    """(logp, lse) by row; a token of another shard has -lse"""
+    """(logp, lse) by row; a token of another shard has -lse, and in a shard of nothing but -inf lse is not taken from anything"""
     out = np.zeros((2, len(ids)))
     for t, i in enumerate(ids):
         if i != ignore:
             a = _row(z[t], scale)
-            lse = softmax(a)[1]
-            out[:, t] = (a[i - first] if first <= i < first + len(a) else 0.0) - lse, lse
+            lse = softmax(a)[1] if a.max() != -np.inf else -np.inf
+            out[:, t] = (a[i - first] if first <= i < first + len(a) else 0.0) - (lse if lse != -np.inf else 0.0), lse
     return out[0], out[1]
 
 

@@ -763,12 +763,15 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, TOP && CH <= 8 
     log_s = log_f64(all.s);
     logp = scale * ((double)zy - (double)all.m) - log_s;
   }
+  const float lse = (float)(scale * (double)all.m + log_s);
   if (y == ELSEWHERE) logp = -(scale * (double)all.m + log_s);
+  // a shard of nothing but -inf has no log sum to take from the token's logit, or to take from nothing
+  if (a.ids.whole != a.vocab && lse == -INFINITY) logp = y == ELSEWHERE ? 0.0 : scale * (double)zy;
   if (y == INVALID) logp = __builtin_nan("");
   if (dr && tid == y_tid) dr[y] = from_f32<T>(own * a.scale * -expm1f((float)logp));        // g scale (1 - p), without the difference
   if (tid > 0) return;
   if (a.logp) a.logp[row] = (float)logp;
-  if (a.lse) a.lse[row] = (float)(scale * (double)all.m + log_s);
+  if (a.lse) a.lse[row] = lse;
   if (a.logp64) {
     a.logp64[row] = logp;
     a.stats[row] = f32x2{all.m, (float)(1.0 / all.s)};

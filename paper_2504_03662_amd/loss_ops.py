@@ -85,7 +85,8 @@ class DeviceTokenLoss(_LogitsOperator):
 
     def logp(self, logits, ids):
         """logits [..., vocab], ids [...] -> (logp, lse), fp32.  Over a shard lse is the shard's, and logp -lse where the token is another
-        shard's: of the whole vocabulary lse = logsumexp of all lse, logp = sum of all (logp + lse) - lse."""
+        shard's: of the whole vocabulary lse = logsumexp of all lse, logp = sum of all (logp + lse) - lse.  A shard that has nothing but -inf in a
+        row has lse = -inf and logp without it, which goes into the sum alone: logp + lse.masked_fill(lse == -inf, 0)."""
         stride, shape = self._rows("logits", logits), logits.shape[:-1]
         cfg = self._cfg(ids.numel(), self._ids(ids, shape), stride, stride)
         logp = self._new(shape, torch.float32)
