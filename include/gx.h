@@ -428,7 +428,8 @@ gx_status gx_cross_bwd(const gx_cross_cfg* cfg, const gx_cross_in* in, const gx_
  *   logp is 0 for a token of another shard and -inf for one of its own.  The whole vocabulary's are lse = log sum exp of the ranks' lse and
  *   logp = sum over the ranks of (logp + lse, or logp where lse is -inf) - lse of the whole.  Only gx_logp_* take shards.
  * Logits of -inf are columns of probability 0.  A row of nothing else (over the whole vocabulary) has lse = -inf and NaN for the rest; a
- * row with NaN or +inf has NaN for all.  Sums are fp32 over 16 bytes of logits, then fp64; losses are rounded once; gradients are fp32, rounded once.
+ * row with NaN or +inf has NaN for all.  Sums are fp32 over 16 bytes of logits, then fp64; losses are rounded once; gradients are fp32, rounded once,
+ * and 1 - p at the token is no difference (expm1 of logp), so that it is there where p is nearly 1.
  * rows 0 .. 2^21, vocab 1 .. 2^19, scale 2^-20 .. 2^20; dlogits of gx_logp_bwd and gx_preference_loss in less than 2^24 pieces of
  * 8192 (bf16) or 4096 (fp32) columns.  Pointers are aligned to their elements.  Errors: GX_ERR_NULL, GX_ERR_SHAPE, GX_ERR_DTYPE
  * (dtype, id_bytes, top_dtype), GX_ERR_ALIGN, GX_ERR_FLAGS, GX_ERR_ARCH, GX_ERR_LAUNCH. */

@@ -870,6 +870,7 @@ struct GradArgs {
   Ids ids;
   const float *lse, *dlogp;
   const f32x2* stats;
+  const double* logp;                                          // with stats: the tokens' log probabilities
 };
 template <typename T, int THREADS, int CH, bool PAIRS>
 __global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a, std::conditional_t<PAIRS, PairArgs, None> pairs) {
@@ -915,6 +916,8 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a, std::conditi
   const f32x2 st = !counts ? f32x2{0.f, 0.f} : a.stats ? a.stats[row] : f32x2{a.lse[row], 1.f};
   const float slope = -g * st[1];
   auto at = [&](float z) { return slope * exp_gradient<T>(fmaf(z, a.unit, -st[0]), a.c_hi, a.c_lo); };
+  // g (1 - p) at the token, without the difference, which a p near 1 would leave nothing of
+  auto at_token = [&](float z) { return -g * expm1f(a.logp ? (float)a.logp[row] : fmaf(z, a.unit, -st[0])); };
   Raw v[CH];
   if (counts) {
 #pragma unroll
@@ -935,16 +938,32 @@ __global__ void __launch_bounds__(256) loss_grad_kernel(GradArgs a, std::conditi
     for (int e = 0; e < N; e++) x[e] = 0.f;
     if (counts) {
 #pragma unroll
-      for (int e = 0; e < N; e++) {
-        x[e] = at(to_f32(v[j][e]));
-        if (k.head + c * N + e == y) x[e] += g;
-      }
+      for (int e = 0; e < N; e++) x[e] = at(to_f32(v[j][e]));
     }
     store_chunk(dr + k.head + (size_t)c * N, rounded<T>(x), aligned);
   }
+  // the thread that has stored the chunk around y overwrites y after that
+  const int at_y = y - k.head;
+  if (counts && at_y >= 0 && at_y < k.body * N) {
+    float zy = 0.f;
+    bool mine = false;
+#pragma unroll
+    for (int j = 0; j < CH; j++) {
+      if (first + j * THREADS != at_y / N) continue;
+      mine = true;
+#pragma unroll
+      for (int e = 0; e < N; e++) zy = at_y % N == e ? to_f32(v[j][e]) : zy;
+    }
+    if (mine) dr[y] = from_f32<T>(at_token(zy));
+  }
   if (part == 0 && tid < k.ends) {
     const int col = k.end_at(tid);
-    dr[col] = from_f32<T>(counts ? at(to_f32(zr[col])) + (col == y ? g : 0.f) : 0.f);
+    float x = 0.f;
+    if (counts) {
+      const float z = to_f32(zr[col]);
+      x = col == y ? at_token(z) : at(z);
+    }
+    dr[col] = from_f32<T>(x);
   }
 }
 
@@ -1283,6 +1302,7 @@ gx_status gx_preference_loss(const gx_logits_cfg* cfg, const gx_pairs_cfg* pairs
   set_scale(cfg->scale, g.c_hi, g.c_lo);
   g.ids = a.ids;
   g.stats = a.stats;
+  g.logp = a.logp64;
   g.dlogp = dlogp;
   return run_grad(*cfg, g, few ? &p : nullptr, s);
 }
