@@ -422,7 +422,7 @@ gx_status gx_cross_bwd(const gx_cross_cfg* cfg, const gx_cross_in* in, const gx_
  *   ids [rows] : int32 or int64 (id_bytes 4 or 8).  A row whose id is ignore_id does not count.
  *   A row counts with weights[t] (fp32, NULL for ones): losses and gradients are multiplied by it, so weights of mask / (number
  *   of tokens) make sums means.  A row that does not count, or has weight 0, has loss 0, logp 0 and a gradient of zeros, whatever
- *   its logits and other inputs hold: they are not read.  An id of no row of the vocabulary makes the row's results NaN.
+ *   its logits and other inputs hold: they are not read.  An id of no row of the vocabulary makes the row's results NaN, but for lse.
  *   Vocabulary shards: a rank holds columns [first_id, first_id + vocab) of whole_vocab (0: vocab, the whole of it).  lse is then the
  *   shard's; a token of another shard has logp = -lse.  In a row of which the shard has nothing but -inf, lse is -inf and is not taken off:
  *   logp is 0 for a token of another shard and -inf for one of its own.  The whole vocabulary's are lse = log sum exp of the ranks' lse and

@@ -265,6 +265,7 @@ GX_DEVINL float policy_slope(const RowArgs& a, double logp, float old, float ref
   return g;
 }
 GX_DEVINL double policy_loss(const RowArgs& a, double logp, float old, float ref, float adv) {
+  if (logp != logp) return logp;                               // no such token, or no distribution: whatever the advantage
   const double r = exp_f64(logp - (double)old);
   double l = 0.0;
   if (adv != 0.f) {
