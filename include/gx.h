@@ -506,8 +506,8 @@ gx_status gx_preference_loss(const gx_logits_cfg* cfg, const gx_pairs_cfg* pairs
  *   outcome where there is no such column, or all of them are -inf.)
  *     dlogits = w * scale * ((sum of q + r) p - q at the entries' columns - r exp(a - lse of the others) elsewhere)
  * A term with q = 0 is 0.  An id that comes twice is two entries of one column.  A row without an entry has loss 0 and a gradient of
- * zeros.  ignore_id is not used: rows are left out by weights of 0.  Workspace: gx_distill_workspace_bytes, 0 for an invalid
- * configuration. */
+ * zeros, whatever its logits hold.  ignore_id is not used: rows are left out by weights of 0 or by having no entry.  Workspace:
+ * gx_distill_workspace_bytes, 0 for an invalid configuration. */
 typedef struct {
   int32_t top, top_dtype;
   int32_t flags;              /* 0 */

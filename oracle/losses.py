@@ -120,7 +120,7 @@ def distill_loss(z, top_ids, top_logits, top_lse=None, weights=None, scale=1.0):
     for t in range(n):
         w = 1.0 if weights is None else np.float64(weights[t])
         on = (top_ids[t] >= 0) & (top_ids[t] < vocab)
-        if w == 0 or (not on.any() and top_lse is None):
+        if w == 0 or not on.any():
             continue
         at = top_ids[t][on]
         logq = scale * top_logits[t][on].astype(np.float64)

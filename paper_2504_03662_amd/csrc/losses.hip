@@ -555,6 +555,12 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, TOP && CH <= 8 
       else reinterpret_cast<unsigned*>(columns)[element(at)] = 0xffffffffu;
     });
     all_here();
+    // no entry: nothing to learn, whatever the logits hold
+    if (__builtin_amdgcn_readfirstlane((int)*end_marks | *slots_taken) == 0) {
+      if (dr) clear_row(dr, a.vocab, tid, THREADS);
+      if (tid == 0) a.loss[row] = 0.f;
+      return;
+    }
     if (has_end) end_value[tid] = end;
   }
   int slot = TOP ? slots[tid] : 0;

@@ -25,3 +25,10 @@ def test_shards_of_nothing():
     whole = sum(p[0] + np.where(p[1] == -np.inf, 0.0, p[1]) for p in parts) - lse
     assert whole[1] == lp[1] == -np.inf
     np.testing.assert_allclose(whole[[0, 2, 3]], lp[[0, 2, 3]], rtol=1e-12)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+def test_distillation_without_an_entry(rest):
+    z = np.array([[1.0, np.nan, -np.inf], [0.5, 0.0, 2.0]])
+    loss, d = O.distill_loss(z, np.array([[-1, 3], [-1, 2]]), np.zeros((2, 2)), np.array([np.nan, 1.0]) if rest else None)
+    assert loss[0] == 0 and not d[0].any() and loss[1] > 0 and d[1].all()
