@@ -988,7 +988,7 @@ gx_status check(const gx_logits_cfg* c) {
   const int64_t far = (int64_t)1 << 40;
   if (c->rows < 0 || c->rows > MAX_ROWS || c->vocab <= 0 || c->vocab > MAX_VOCAB || c->stride < c->vocab || c->stride > far ||
       c->grad_stride < c->vocab || c->grad_stride > far || !(c->scale >= MIN_SCALE && c->scale <= 1.f / MIN_SCALE) || c->first_id < 0 ||
-      c->whole_vocab < 0 || c->whole_vocab > far || (c->whole_vocab && c->first_id + c->vocab > c->whole_vocab) ||
+      c->whole_vocab < 0 || c->whole_vocab > far || (c->whole_vocab && c->first_id > c->whole_vocab - c->vocab) ||
       (!c->whole_vocab && c->first_id))
     return GX_ERR_SHAPE;
   return GX_OK;
