@@ -10,11 +10,12 @@
 // fp64, which costs nothing that could be measured: losses are small differences of log sums, and a sequence's reward adds up
 // over thousands of tokens.  A log sum of 32768 logits (bf16) is off by 2e-8, and by 1e-9 at the mean.
 //
-// Measured, us (and TB/s of logits read and gradients written; a large copy moves 5.7): cross entropy with gradient, bf16, 8192 x 32768 198
-// (5.4), 8192 x 50001 282 (5.8), 2048 x 131072 208 (5.2), fp32 4096 x 32003 180 (5.8); 64 entries of a teacher, 8192 x 32768 215
-// (5.0), 2048 x 131072 253 (4.2); preference loss, which reads twice, 8192 x 32768 270 (6.0, the second time in part from
-// caches).  Small rows are bound by the instructions that every row costs (16384 x 1000 18, 3.6; 64 entries 42), few rows by latency
-// (64 x 32000 8.2).
+// Measured, us (and TB/s of logits read and gradients written; a large copy moves 5.7), all rows counting, inputs of 1.2 GB in turn: cross
+// entropy with gradient, bf16, 8192 x 32768 198 (5.4), 8192 x 50001 282 (5.8), 2048 x 131072 206 (5.2), 1024 x 262144, read twice, 236 (4.6),
+// fp32 4096 x 32003 182 (5.8); 64 entries of a teacher, 8192 x 32768 212 (5.1), 2048 x 131072, read twice, 253 (4.2); preference
+// loss, which reads twice, 8192 x 32768 264 (6.1, the second time in part from caches).  Small rows are bound by the instructions that every
+// row costs (16384 x 1000 19, 3.4; 64 entries 42), few rows by latency (64 x 32000 8.4).  Below, figures next to a choice are both sides
+// of it in one run, of the code as it was then; runs differ by up to 4 %.
 #include "../../include/gx.h"
 #include "gx_kernels.h"
 #include <algorithm>
@@ -28,7 +29,8 @@ using namespace gx;
 constexpr int MAX_ROWS = 1 << 21, MAX_VOCAB = 1 << 19, MAX_TOP = 1024, MAX_PAIRS = 1 << 20;
 constexpr long MAX_GRID = (1 << 24) - 1;
 // So few rows and pairs that a launch of its own for the pairs takes longer than adding them up for every row (131 rows of 1001 15.4 us,
-// 19 with the launch; 1001 rows of 5003 16.0, and 1025, with the launch, 18.9)
+// 19 with the launch; 1001 rows of 5003 16.0, and 1025, with the launch, 18.9).  The rule does not ask for the length of rows: each of the
+// workgroups of a long one adds its pair up before it asks for logits (1024 rows of 262144 304, and 2048 of 131072, with the launch, 271)
 constexpr int FEW_ROWS = 1024, FEW_PAIRS = 256;
 constexpr float NO_LOGIT = -INFINITY, MIN_SCALE = 1.f / (1 << 20);
 
@@ -84,7 +86,8 @@ GX_DEVINL double scalar(double x) {
   asm("" : "+s"(x));
   return x;
 }
-// Exponential and logarithm in fp64, to about 2^-50: a power of two, and a series in what is left of it (of exp up to the 12th power for
+// Exponential and logarithm in fp64, to about 2^-50 (the exponential for |x| up to 25; log(2) is one number whose rounding counts n times, so
+// that it is off by 3e-14 at 700): a power of two, and a series in what is left of it (of exp up to the 12th power for
 // |r| <= log(2) / 2, of log m = 2 atanh((m - 1) / (m + 1)) up to the 19th for m between sqrt(1/2) and sqrt(2)).  Every
 // wavefront of a row computes a few of them: a quarter of the instructions of a library's.
 GX_DEVINL double exp_f64(double x) {
@@ -1109,7 +1112,8 @@ bool too_many_parts(const gx_logits_cfg& c, const void* z) { return (long)c.rows
 // Whether rows read their teachers in the launch that does the rest.  Many have a launch before it, which is quicker at it where workgroups
 // wait for one another.  us, one launch and two, 64 entries, bf16: rows of a wavefront (1000 columns), 1024 of them 10.5 and 13.7, 16384
 // 41.8 and 45.3 (256 entries, 65536 rows, 435 and 406); of 256 threads (8000), 2048 24.2 and 25.8, 4096 41.4 and 41.2; of 512 (32000), 512
-// 20.0 and 21.9, 1024 35.2 and 32.5.
+// 20.0 and 21.9, 1024 35.2 and 32.5.  The rule does not ask for the number of entries; between 64 and 256 the sides of short rows come closer, and
+// more than 256 were not timed.
 bool reads_here(const gx_logits_cfg& c, const void* z) {
   const int per_row = chunks_of(c, z, c.stride);
   return c.rows <= (per_row <= 512 ? 1 << 15 : per_row <= 2048 ? 2048 : 512);
